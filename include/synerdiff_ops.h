@@ -177,6 +177,91 @@ sd_status synerdiff_op_conv_out_cfg_ddim(int32_t dtype, const void* d_x, int32_t
                                          const float* d_lat_in, float* d_lat_out, float* d_eps_out,
                                          void* hip_stream);
 
+/* ---- Operators on texts of their own lengths and on few-bit weights ----
+ * Further element type of these operators: OCP e4m3 (4 exponent bits, 3
+ * fraction bits, largest value 448, no infinities). */
+#define SD_E4M3 2
+
+/* Root-mean-square norm over the last axis, with the residual's addition and
+ * an 8-bit output when asked for (the norms around a text encoder's or a
+ * transformer's sublayers):
+ *   h[t, c] = x[t, c] + resid[t, c]        (x alone when resid is NULL)
+ *   y[t, c] = h[t, c] / sqrt(mean_c(h[t, c]^2) + eps) * gamma[c]
+ * x, resid, sum in `dtype`; row t of each starts at t * its ld (elements, >=
+ * C).  h is kept in fp32 for the norm; d_sum (may be NULL; NULL without
+ * resid) receives it rounded to dtype.  gamma fp32 [C] or NULL (all ones).
+ * y_type = dtype: y is rounded to dtype.  y_type = SD_E4M3: per row, or per
+ * block of 128 channels of a row (the last block may be narrower),
+ *   s = max(max|y|, 2^-100) / 448,   y8 = e4m3(y / s),   y ~ y8 * s,
+ * d_scale fp32 [tokens, blocks] with scale_group = 128, or [tokens] with
+ * scale_group = 0; a NaN in a row makes all its y and scales NaN.
+ * sum may equal x or resid, and y (of y_type dtype) may equal x or resid,
+ * with the same ld; otherwise outputs overlap nothing.  Any alignment and ld; buffers whose
+ * rows all start at multiples of 16 bytes (y8: 8) and C a multiple of 8 move
+ * in 16-byte pieces.  1 <= C <= 16384 (SD_ERR_UNSUPPORTED past it), eps >= 0.
+ * tokens = 0 does nothing. */
+sd_status synerdiff_op_rmsnorm(int32_t dtype, const void* d_x, int64_t x_ld, const void* d_resid, int64_t resid_ld,
+                               void* d_sum, int64_t sum_ld, const float* d_gamma, float eps, int64_t tokens,
+                               int32_t C, int32_t y_type, void* d_y, int64_t y_ld, float* d_scale,
+                               int32_t scale_group, void* hip_stream);
+
+/* synerdiff_op_linear_rows with weights of 4 bits in groups along K:
+ *   out[m, n] = act_out(bias[n] + add[m, n] + sum_k act_in(x[m, k]) * w[n, k])
+ *   w[n, k] = scale[n, k / group] * (q[n, k] - zero[n, k / group])
+ * q: 4-bit codes 0..15, two a byte along K (the even k in the low half), [N,
+ * K / 2] bytes, rows at multiples of 4 bytes.  group 32, 64 or 128 (the last
+ * group of a row may be narrower); scale [N, ceil(K / group)] in scale_type
+ * (SD_F32 or SD_BF16); zero bytes 0..15 of the same shape, or NULL (8).
+ * x [M, K] in x_type SD_F32, SD_BF16 or SD_E4M3, row m at m * x_ld
+ * (elements); e4m3 rows stand for x8 * x_scale, fp32 [M] with x_group = 0 or
+ * [M, ceil(K / 128)] with x_group = 128, as synerdiff_op_rmsnorm writes them
+ * (x_scale NULL and x_group 0 for the other types).  act_* = SiLU where silu_* = 1,
+ * else the identity (silu_in not with e4m3: SD_ERR_UNSUPPORTED).  out [M, N]
+ * in out_type SD_F32 or SD_BF16, row m at m * out_ld; bias fp32 [N], add
+ * fp32 [M, N], may be NULL; add may equal an fp32 out of out_ld = N; out
+ * overlaps nothing else.  Products and sums are fp32-accurate for every
+ * x_type.  A row of x with an infinity or NaN gives no finite value.
+ * K a multiple of 8; x and its rows 16-byte aligned (e4m3: 8).  The rows of a
+ * result do not depend on M.  M = 0 or N = 0 does nothing. */
+sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* d_x, int64_t x_ld, const float* d_x_scale,
+                                      int32_t x_group, int32_t M, int32_t K, const uint8_t* d_w, int32_t group,
+                                      int32_t scale_type, const void* d_scale, const uint8_t* d_zero,
+                                      const float* d_bias, const float* d_add, int32_t silu_in, int32_t silu_out,
+                                      int32_t out_type, void* d_out, int64_t out_ld, int32_t N, void* hip_stream);
+
+/* Attention of each row's queries over a text of its own length:
+ *   o[i, t, h] = sum_j p_j v[j, g] / sum_j p_j,  p_j = exp(scale * q[i, t, h] . k[j, g])
+ * over the keys j of row i's context that take part, g = h / (heads /
+ * kv_heads).  Row i reads context c = kv_index[i] (NULL: c = i, n_ctx >= n); key j < kv_len[c] (NULL: max_len for all) takes part if its mask byte is not
+ * 0 (NULL: all do).  Keys that take no part are not read: they may hold
+ * anything.  A row without a key, or whose kv_index lies outside [0, n_ctx),
+ * gives zeros.
+ * Layouts: element (i, t, h, e) of q is at q + i * q_img + t * q_ld + h *
+ * q_head + e, o likewise.  Contexts one after another (d_kv_start not NULL):
+ * key j of context c is row kv_start[c] + j of k: k + row * k_ld + g *
+ * k_head + e, and mask byte `row` of [kv_tokens]; a context that starts
+ * outside [0, kv_tokens) is empty, one that ends past it is cut there.  Padded contexts (d_kv_start NULL): k + c * k_ctx + j *
+ * k_ld + g * k_head + e, and mask byte c * max_len + j.  v likewise.  A
+ * kv_len past max_len counts as max_len, a negative one as 0.  Strides in
+ * elements, not negative (0 for a shared head).
+ * Constraints: d a multiple of 8, <= 256; heads a multiple of kv_heads; q,
+ * k, v, o and all their strides at multiples of 16 bytes.  o overlaps
+ * nothing.  Few queries over long texts are split along the keys: d_scratch
+ * (fp32, 16-byte aligned) has to hold synerdiff_op_cross_attention_scratch_floats(...) floats
+ * then (SD_ERR_WORKSPACE if smaller; 0 = none needed), and belongs to this call
+ * until it has run.  The bits of a row depend on its own inputs, n_q, heads,
+ * kv_heads and d, not on the other rows or max_len.  n = 0 or n_q = 0 does nothing. */
+int64_t synerdiff_op_cross_attention_scratch_floats(int32_t dtype, int32_t n, int32_t heads, int32_t kv_heads,
+                                                    int32_t d, int32_t n_q, int32_t max_len);
+sd_status synerdiff_op_cross_attention(int32_t dtype, const void* d_q, int64_t q_ld, int64_t q_head, int64_t q_img,
+                                       const void* d_k, int64_t k_ld, int64_t k_head, int64_t k_ctx, const void* d_v,
+                                       int64_t v_ld, int64_t v_head, int64_t v_ctx, int64_t kv_tokens, int32_t n_ctx,
+                                       int32_t max_len, const int32_t* d_kv_start, const int32_t* d_kv_len,
+                                       const int32_t* d_kv_index, const uint8_t* d_mask, void* d_o, int64_t o_ld,
+                                       int64_t o_head, int64_t o_img, int32_t n, int32_t heads, int32_t kv_heads,
+                                       int32_t d, int32_t n_q, float scale, float* d_scratch, int64_t scratch_floats,
+                                       void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

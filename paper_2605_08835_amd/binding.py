@@ -13,6 +13,7 @@ LIB_PATH = os.path.join(_HERE, "libsynerdiff.so")
 _LIB = None
 
 SD_F32, SD_BF16 = 0, 1
+SD_E4M3 = 2  # rmsnorm's output and linear_rows_w4's input only
 SCHEDULES = {"linear": 0, "scaled_linear": 1}
 STATUS = {0: "SD_OK", -1: "SD_ERR_INVALID_ARG", -2: "SD_ERR_UNSUPPORTED", -3: "SD_ERR_CAPACITY",
           -4: "SD_ERR_WORKSPACE", -5: "SD_ERR_HIP"}
@@ -128,6 +129,18 @@ _SIG = {
                                            ctypes.c_int32, _P, ctypes.c_int32, _P, _P, _P]),
     "synerdiff_op_linear_rows": (ctypes.c_int, [ctypes.c_int32, _P, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P,
                                                 ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P]),
+    "synerdiff_op_rmsnorm": (ctypes.c_int, [ctypes.c_int32, _P, ctypes.c_int64, _P, ctypes.c_int64, _P, ctypes.c_int64,
+                                            _P, ctypes.c_float, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P,
+                                            ctypes.c_int64, _P, ctypes.c_int32, _P]),
+    "synerdiff_op_linear_rows_w4": (ctypes.c_int, [ctypes.c_int32, _P, ctypes.c_int64, _P] + [ctypes.c_int32] * 3 +
+                                    [_P, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P] + [ctypes.c_int32] * 3 +
+                                    [_P, ctypes.c_int64, ctypes.c_int32, _P]),
+    "synerdiff_op_cross_attention_scratch_floats": (ctypes.c_int64, [ctypes.c_int32] * 7),
+    "synerdiff_op_cross_attention": (ctypes.c_int, [ctypes.c_int32] + [_P, ctypes.c_int64, ctypes.c_int64,
+                                                                       ctypes.c_int64] * 3 +
+                                     [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P, _P] +
+                                     [ctypes.c_int64] * 3 + [ctypes.c_int32] * 5 + [ctypes.c_float, _P,
+                                                                                   ctypes.c_int64, _P]),
 }
 
 

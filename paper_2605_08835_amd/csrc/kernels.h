@@ -174,4 +174,58 @@ hipError_t launch_cfg_ddim(const float* eps_rows, const float* lat_in, float* la
                            float* eps_out, int n_req, int lc, int hw, const int* req_row_u,
                            const float* req_coef, hipStream_t s);
 
+// Root-mean-square norm of rows of x (+ resid), see synerdiff_op_rmsnorm.
+struct RmsNormArgs {
+  const void* x; long x_ld;
+  const void* resid; long resid_ld;  // or null
+  void* sum; long sum_ld;            // or null
+  const float* gamma;                // [C] or null
+  float eps;
+  long tokens;
+  int C;
+  int y8;                            // 1: y is e4m3, with scale[t * blocks + b]
+  void* y; long y_ld;
+  float* scale;
+  int blocks, group;                 // scale blocks per row, channels per block (C: one per row)
+};
+hipError_t launch_rmsnorm(DType dt, const RmsNormArgs& a, hipStream_t s);
+constexpr int RMSNORM_MAX_C = 16384;
+
+// Linear layer over a few rows with 4-bit weights, see synerdiff_op_linear_rows_w4.
+struct LinearW4Args {
+  const void* x; long x_ld;      // fp32, bf16 or e4m3 rows (x_type 0, 1, 2)
+  int x_type;
+  const float* x_scale;          // e4m3: [M, x_blocks]
+  int x_blocks;                  // 1: one scale a row, else one per 128 k
+  int M, K, N;
+  const uint8_t* w;              // [N, K / 2]
+  int group, groups;             // 32, 64 or 128; ceil(K / group)
+  const void* scale; int scale_f32;
+  const uint8_t* zero;           // or null (8)
+  const float* bias;             // [N] or null
+  const float* add;              // [M, N] or null
+  int silu_in, silu_out;
+  void* out; long out_ld; int out_f32;
+};
+hipError_t launch_linear_w4(const LinearW4Args& a, hipStream_t s);
+
+// Attention over contexts of their own lengths, see synerdiff_op_cross_attention.
+struct CrossArgs {
+  const void* q; long q_ld, q_head, q_img;
+  const void* k; long k_ld, k_head, k_ctx;
+  const void* v; long v_ld, v_head, v_ctx;
+  long kv_tokens;
+  int n_ctx, max_len;
+  const int* kv_start;  // null: padded contexts
+  const int* kv_len;    // or null
+  const int* kv_index;  // or null
+  const uint8_t* mask;  // or null
+  void* o; long o_ld, o_head, o_img;
+  int n, heads, kv_heads, rep, d, n_q;
+  float scale;
+  float* scratch;
+};
+hipError_t launch_cross_attention(DType dt, const CrossArgs& a, hipStream_t s);
+long cross_attention_scratch_floats(DType dt, int n, int heads, int kv_heads, int d, int n_q, int max_len);
+
 }  // namespace sd

@@ -285,4 +285,129 @@ sd_status synerdiff_op_conv_out_cfg_ddim(int32_t dtype, const void* x, int32_t H
   return op_hip(launch_out_cfg_ddim(a, (hipStream_t)stream), "conv_out_cfg_ddim");
 }
 
+sd_status synerdiff_op_rmsnorm(int32_t dtype, const void* x, int64_t x_ld, const void* resid, int64_t resid_ld,
+                               void* sum, int64_t sum_ld, const float* gamma, float eps, int64_t tokens, int32_t C,
+                               int32_t y_type, void* y, int64_t y_ld, float* scale, int32_t scale_group,
+                               void* stream) {
+  if (bad_dtype(dtype)) return op_fail(SD_ERR_INVALID_ARG, "bad dtype");
+  if (y_type != dtype && y_type != SD_E4M3) return op_fail(SD_ERR_INVALID_ARG, "y_type must be dtype or SD_E4M3");
+  if (tokens < 0 || C < 1) return op_fail(SD_ERR_INVALID_ARG, "bad shape");
+  if (C > RMSNORM_MAX_C || tokens > 0x7FFFFFFF) return op_fail(SD_ERR_UNSUPPORTED, "rows past 16384 wide or past 2^31");
+  if (!(eps >= 0.f)) return op_fail(SD_ERR_INVALID_ARG, "eps must be >= 0");
+  if (sum && !resid) return op_fail(SD_ERR_INVALID_ARG, "sum without resid");
+  if (y_type == SD_E4M3 ? scale_group != 0 && scale_group != 128 : scale || scale_group)
+    return op_fail(SD_ERR_INVALID_ARG, "scale_group is 0 or 128, scales only with an e4m3 output");
+  if (tokens == 0) return SD_OK;
+  if (!x || !y || (y_type == SD_E4M3 && !scale)) return op_fail(SD_ERR_INVALID_ARG, "NULL argument");
+  if (x_ld < C || y_ld < C || (resid && resid_ld < C) || (sum && sum_ld < C))
+    return op_fail(SD_ERR_INVALID_ARG, "a row stride is below C");
+  const uintptr_t el = dtype == SD_BF16 ? 1 : 3;
+  if (((uintptr_t)x | (uintptr_t)resid | (uintptr_t)sum | (y_type == SD_E4M3 ? 0 : (uintptr_t)y)) & el ||
+      ((uintptr_t)gamma | (uintptr_t)scale) & 3)
+    return op_fail(SD_ERR_INVALID_ARG, "a buffer is not aligned to its element");
+  const auto same = [](const void* a, int64_t la, const void* b, int64_t lb) { return a && a == b && la != lb; };
+  if (same(sum, sum_ld, x, x_ld) || same(sum, sum_ld, resid, resid_ld) || same(y, y_ld, x, x_ld) ||
+      same(y, y_ld, resid, resid_ld) || (y_type == SD_E4M3 && (y == x || y == resid)) || (sum && sum == y))
+    return op_fail(SD_ERR_INVALID_ARG, "outputs overlap inputs or each other");
+  RmsNormArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = x; a.x_ld = x_ld; a.resid = resid; a.resid_ld = resid_ld; a.sum = sum; a.sum_ld = sum_ld;
+  a.gamma = gamma; a.eps = eps; a.tokens = tokens; a.C = C;
+  a.y8 = y_type == SD_E4M3; a.y = y; a.y_ld = y_ld; a.scale = scale;
+  a.group = scale_group ? scale_group : C;
+  a.blocks = (C + a.group - 1) / a.group;
+  return op_hip(launch_rmsnorm((DType)dtype, a, (hipStream_t)stream), "rmsnorm");
+}
+
+sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* x, int64_t x_ld, const float* x_scale,
+                                      int32_t x_group, int32_t M, int32_t K, const uint8_t* w, int32_t group,
+                                      int32_t scale_type, const void* scale, const uint8_t* zero, const float* bias,
+                                      const float* add, int32_t silu_in, int32_t silu_out, int32_t out_type,
+                                      void* out, int64_t out_ld, int32_t N, void* stream) {
+  if ((bad_dtype(x_type) && x_type != SD_E4M3) || bad_dtype(scale_type) || bad_dtype(out_type))
+    return op_fail(SD_ERR_INVALID_ARG, "bad dtype");
+  if (M < 0 || N < 0 || K <= 0 || K % 8) return op_fail(SD_ERR_INVALID_ARG, "bad shape (K a multiple of 8)");
+  if (group != 32 && group != 64 && group != 128) return op_fail(SD_ERR_INVALID_ARG, "group must be 32, 64 or 128");
+  if (x_type == SD_E4M3 ? x_group != 0 && x_group != 128 : x_scale || x_group)
+    return op_fail(SD_ERR_INVALID_ARG, "x_group is 0 or 128, x scales only with e4m3 rows");
+  if (x_type == SD_E4M3 && silu_in) return op_fail(SD_ERR_UNSUPPORTED, "silu_in on e4m3 rows");
+  if (M == 0 || N == 0) return SD_OK;
+  if (!x || !w || !scale || !out || (x_type == SD_E4M3 && !x_scale)) return op_fail(SD_ERR_INVALID_ARG, "NULL argument");
+  if (x_ld < K || out_ld < N) return op_fail(SD_ERR_INVALID_ARG, "a row stride is below its row");
+  const int64_t piece = x_type == SD_F32 ? 4 : 8;  // elements of 16 bytes (e4m3: 8)
+  if ((uintptr_t)x % (x_type == SD_E4M3 ? 8 : 16) || x_ld % piece || (uintptr_t)w % 4)
+    return op_fail(SD_ERR_INVALID_ARG, "x rows must be 16-byte aligned (e4m3: 8), w 4-byte");
+  if (((uintptr_t)scale & (scale_type == SD_F32 ? 3 : 1)) || ((uintptr_t)out & (out_type == SD_F32 ? 3 : 1)) ||
+      ((uintptr_t)bias | (uintptr_t)add | (uintptr_t)x_scale) & 3)
+    return op_fail(SD_ERR_INVALID_ARG, "a buffer is not aligned to its element");
+  if (add && add == out && (out_type != SD_F32 || out_ld != N)) return op_fail(SD_ERR_INVALID_ARG, "add overlaps out");
+  if (out == x) return op_fail(SD_ERR_INVALID_ARG, "out overlaps x");
+  LinearW4Args a;
+  memset(&a, 0, sizeof(a));
+  a.x = x; a.x_ld = x_ld; a.x_type = x_type; a.x_scale = x_scale; a.x_blocks = x_group ? (K + 127) / 128 : 1;
+  a.M = M; a.K = K; a.N = N; a.w = w; a.group = group; a.groups = (K + group - 1) / group;
+  a.scale = scale; a.scale_f32 = scale_type == SD_F32; a.zero = zero; a.bias = bias; a.add = add;
+  a.silu_in = silu_in ? 1 : 0; a.silu_out = silu_out ? 1 : 0;
+  a.out = out; a.out_ld = out_ld; a.out_f32 = out_type == SD_F32;
+  return op_hip(launch_linear_w4(a, (hipStream_t)stream), "linear_rows_w4");
+}
+
+static bool cross_shape_ok(int32_t dtype, int32_t n, int32_t heads, int32_t kv_heads, int32_t d, int32_t n_q,
+                           int32_t max_len) {
+  return !bad_dtype(dtype) && n >= 0 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0 && d >= 8 && d % 8 == 0 &&
+         d <= 256 && n_q >= 0 && max_len >= 0;
+}
+
+int64_t synerdiff_op_cross_attention_scratch_floats(int32_t dtype, int32_t n, int32_t heads, int32_t kv_heads,
+                                                    int32_t d, int32_t n_q, int32_t max_len) {
+  if (!cross_shape_ok(dtype, n, heads, kv_heads, d, n_q, max_len)) return 0;
+  return cross_attention_scratch_floats((DType)dtype, n, heads, kv_heads, d, n_q, max_len);
+}
+
+sd_status synerdiff_op_cross_attention(int32_t dtype, const void* q, int64_t q_ld, int64_t q_head, int64_t q_img,
+                                       const void* k, int64_t k_ld, int64_t k_head, int64_t k_ctx, const void* v,
+                                       int64_t v_ld, int64_t v_head, int64_t v_ctx, int64_t kv_tokens, int32_t n_ctx,
+                                       int32_t max_len, const int32_t* kv_start, const int32_t* kv_len,
+                                       const int32_t* kv_index, const uint8_t* mask, void* o, int64_t o_ld,
+                                       int64_t o_head, int64_t o_img, int32_t n, int32_t heads, int32_t kv_heads,
+                                       int32_t d, int32_t n_q, float scale, float* scratch, int64_t scratch_floats,
+                                       void* stream) {
+  if (bad_dtype(dtype)) return op_fail(SD_ERR_INVALID_ARG, "bad dtype");
+  if (!cross_shape_ok(dtype, n, heads, kv_heads, d, n_q, max_len))
+    return op_fail(d > 256 ? SD_ERR_UNSUPPORTED : SD_ERR_INVALID_ARG, "bad shape (d a multiple of 8 up to 256, heads of kv_heads)");
+  if (n_ctx < 0 || kv_tokens < 0 || kv_tokens > 0x7FFFFFFF) return op_fail(SD_ERR_INVALID_ARG, "bad context count or length");
+  if (!kv_index && n_ctx < n) return op_fail(SD_ERR_INVALID_ARG, "fewer contexts than rows");
+  if (!(scale == scale) || scale - scale != 0.f) return op_fail(SD_ERR_INVALID_ARG, "scale must be finite");
+  if (n == 0 || n_q == 0) return SD_OK;
+  const bool keys = n_ctx > 0 && max_len > 0 && (!kv_start || kv_tokens > 0);
+  if (!q || !o || (keys && (!k || !v))) return op_fail(SD_ERR_INVALID_ARG, "NULL argument");
+  const int64_t strides[] = {q_ld, q_head, q_img, k_ld, k_head, kv_start ? 0 : k_ctx, v_ld, v_head,
+                             kv_start ? 0 : v_ctx, o_ld, o_head, o_img};
+  const int64_t piece = dtype == SD_BF16 ? 8 : 4;
+  for (int64_t s : strides)
+    if (s < 0 || s % piece) return op_fail(SD_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15)
+    return op_fail(SD_ERR_INVALID_ARG, "q, k, v, o must be 16-byte aligned");
+  if ((n_q > 1 && o_ld == 0) || (heads > 1 && o_head == 0) || (n > 1 && o_img == 0))
+    return op_fail(SD_ERR_INVALID_ARG, "o overlaps itself");
+  if (((uintptr_t)kv_start | (uintptr_t)kv_len | (uintptr_t)kv_index) & 3)
+    return op_fail(SD_ERR_INVALID_ARG, "an index array is not aligned");
+  if (o == q || o == k || o == v) return op_fail(SD_ERR_INVALID_ARG, "o overlaps an input");
+  const int64_t need = cross_attention_scratch_floats((DType)dtype, n, heads, kv_heads, d, n_q, max_len);
+  if (need < 0) return op_fail(SD_ERR_UNSUPPORTED, "too many rows, heads and queries");
+  if (need > 0 && (!scratch || scratch_floats < need)) return op_fail(SD_ERR_WORKSPACE, "scratch is too small");
+  if ((uintptr_t)scratch & 15) return op_fail(SD_ERR_INVALID_ARG, "scratch must be 16-byte aligned");
+  CrossArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = q; a.q_ld = q_ld; a.q_head = q_head; a.q_img = q_img;
+  a.k = k; a.k_ld = k_ld; a.k_head = k_head; a.k_ctx = k_ctx;
+  a.v = v; a.v_ld = v_ld; a.v_head = v_head; a.v_ctx = v_ctx;
+  a.kv_tokens = kv_tokens; a.n_ctx = n_ctx; a.max_len = keys ? max_len : 0;
+  a.kv_start = kv_start; a.kv_len = kv_len; a.kv_index = kv_index; a.mask = mask;
+  a.o = o; a.o_ld = o_ld; a.o_head = o_head; a.o_img = o_img;
+  a.n = n; a.heads = heads; a.kv_heads = kv_heads; a.rep = heads / kv_heads; a.d = d; a.n_q = n_q;
+  a.scale = scale; a.scratch = need > 0 ? scratch : nullptr;
+  return op_hip(launch_cross_attention((DType)dtype, a, (hipStream_t)stream), "cross_attention");
+}
+
 }  // extern "C"
