@@ -331,6 +331,7 @@ sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* x, int64_t x_l
   if (x_type == SD_E4M3 ? x_group != 0 && x_group != 128 : x_scale || x_group)
     return op_fail(SD_ERR_INVALID_ARG, "x_group is 0 or 128, x scales only with e4m3 rows");
   if (x_type == SD_E4M3 && silu_in) return op_fail(SD_ERR_UNSUPPORTED, "silu_in on e4m3 rows");
+  if (M > 1 << 20 || K > 1 << 24) return op_fail(SD_ERR_UNSUPPORTED, "more than 2^20 rows or 2^24 columns");
   if (M == 0 || N == 0) return SD_OK;
   if (!x || !w || !scale || !out || (x_type == SD_E4M3 && !x_scale)) return op_fail(SD_ERR_INVALID_ARG, "NULL argument");
   if (x_ld < K || out_ld < N) return op_fail(SD_ERR_INVALID_ARG, "a row stride is below its row");

@@ -143,28 +143,31 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _enqueue(fn, like, args, *others):
-    """fn(*args, stream) on the device of `like`, which the tensors `others` share."""
-    dev = like.device
+def _enqueue(fn, like, args, others):
+    """fn(*args, stream) on the device of `like`, which the tensors `others` (or
+    None) share.  (The raw-stream and device queries cost 0.2 us together, the
+    public ones 3, of a call of about 8.)"""
+    dev = like.get_device()
     for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device}")
-    if dev.type != "cuda":
-        raise ValueError(f"tensors on {dev}: the kernels run on the GPU")
-    if dev.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors on {like.device} and {t.device}")
+    if dev < 0:
+        raise ValueError(f"tensors on {like.device}: the kernels run on the GPU")
+    stream = torch._C._cuda_getCurrentRawStream(dev)
+    if dev == torch._C._cuda_getDevice():
+        _check(fn(*args, stream))
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+            _check(fn(*args, stream))
 
 
 def _row_stride(t, what):
     """Distance between the rows (last axis) of t, whose rows lie evenly."""
     if t.dim() == 2:
-        s0, s1 = t.stride()
         rows, c = t.shape
+        s0, s1 = t.stride()
         _need(s1 == 1 or c == 1, f"{what}: the last axis must be contiguous")
-        return s0 if rows > 1 and s0 > c else c if rows <= 1 else s0
+        return s0 if rows > 1 else c
     _need(t.dim() >= 1 and t.is_contiguous(), f"{what}: more than two axes must be contiguous")
     return t.shape[-1]
 
@@ -185,7 +188,7 @@ def rmsnorm(x, gamma=None, eps=1e-6, resid=None, sum_out=None, out=None, fp8=Fal
     if resid is not None:
         _need(resid.shape == x.shape and resid.dtype is x.dtype, "resid has another shape or type than x")
         if sum_out is None:
-            sum_out = torch.empty(x.shape, device=x.device, dtype=x.dtype)
+            sum_out = torch.empty_like(x)
         else:
             _need(sum_out.shape == x.shape and sum_out.dtype is x.dtype, "sum_out has another shape or type than x")
     else:
@@ -194,18 +197,18 @@ def rmsnorm(x, gamma=None, eps=1e-6, resid=None, sum_out=None, out=None, fp8=Fal
         _need(gamma.dtype is torch.float32 and gamma.shape == (C,) and gamma.is_contiguous(), "gamma must be fp32 [C]")
     _need(scale_group in (0, 128) and (fp8 or not scale_group), "scale_group is 0 or 128, and 128 only with fp8")
     if out is None:
-        out = torch.empty(x.shape, device=x.device, dtype=y_type)
+        out = torch.empty_like(x, dtype=y_type) if fp8 else torch.empty_like(x)
     else:
         _need(out.shape == x.shape and out.dtype is y_type, "out has another shape or type than the result")
     scale = None
     if fp8:
         blocks = -(-C // 128) if scale_group else 1
-        scale = torch.empty(x.shape[:-1] + (blocks,), device=x.device, dtype=torch.float32)
+        scale = x.new_empty(x.shape[:-1] + (blocks,), dtype=torch.float32)
     _enqueue(lib().synerdiff_op_rmsnorm, x,
              (_TYPE[x.dtype], x.data_ptr(), x_ld, _ptr(resid), 0 if resid is None else _row_stride(resid, "resid"),
               _ptr(sum_out), 0 if sum_out is None else _row_stride(sum_out, "sum_out"), _ptr(gamma), float(eps), rows, C,
               _TYPE[y_type], out.data_ptr(), _row_stride(out, "out"), _ptr(scale), scale_group),
-             resid, sum_out, gamma, out)
+             (resid, sum_out, gamma, out))
     got = (out, scale) if fp8 else (out,)
     if resid is not None:
         got += (sum_out,)
@@ -249,14 +252,14 @@ def linear_rows_w4(x, w, scale, group, zero=None, x_scale=None, bias=None, add=N
     if add is not None:
         _need(add.dtype is torch.float32 and add.shape == (M, N) and add.is_contiguous(), "add must be fp32 [M, N]")
     if out is None:
-        out = torch.empty(M, N, device=x.device, dtype=out_dtype)
+        out = x.new_empty((M, N), dtype=out_dtype)
     else:
         _need(out.shape == (M, N) and out.dtype is out_dtype, "out has another shape or type than the result")
     _enqueue(lib().synerdiff_op_linear_rows_w4, x,
              (t, x.data_ptr(), _row_stride(x, "x"), _ptr(x_scale), x_group, M, K, w.data_ptr(), group,
               _TYPE[scale.dtype], scale.data_ptr(), _ptr(zero), _ptr(bias), _ptr(add), 1 if silu_in else 0,
               1 if silu_out else 0, _TYPE[out_dtype], out.data_ptr(), _row_stride(out, "out"), N),
-             w, scale, zero, x_scale, bias, add, out)
+             (w, scale, zero, x_scale, bias, add, out))
     return out
 
 
@@ -295,18 +298,18 @@ def cross_attention(q, k, v, max_len, kv_start=None, kv_len=None, kv_index=None,
         _need(mask.dtype in (torch.bool, torch.uint8) and mask.shape == k.shape[:-2] and mask.is_contiguous(),
               "mask must be bool or uint8, one value per token")
     if out is None:
-        out = torch.empty(n, n_q, heads, d, device=q.device, dtype=q.dtype)
+        out = q.new_empty((n, n_q, heads, d))
         os = (n_q * heads * d, heads * d, d)
     else:
         _need(out.shape == q.shape and out.dtype is q.dtype and out.stride(3) == 1, "out must have q's shape and type, d contiguous")
         os = out.stride()
     L, t = lib(), _TYPE[q.dtype]
     floats = L.synerdiff_op_cross_attention_scratch_floats(t, n, heads, kv_heads, d, n_q, max_len)
-    scratch = torch.empty(floats, device=q.device) if floats > 0 else None
+    scratch = q.new_empty(floats, dtype=torch.float32) if floats > 0 else None
     _enqueue(L.synerdiff_op_cross_attention, q,
              (t, q.data_ptr(), qs[1], qs[2], qs[0], k.data_ptr(), ks[-3], ks[-2], k_ctx, v.data_ptr(), vs[-3], vs[-2],
               v_ctx, tokens, n_ctx, max_len, _ptr(kv_start), _ptr(kv_len), _ptr(kv_index), _ptr(mask), out.data_ptr(),
               os[1], os[2], os[0], n, heads, kv_heads, d, n_q, d ** -0.5 if scale is None else float(scale),
               _ptr(scratch), floats),
-             k, v, kv_start, kv_len, kv_index, mask, out)
+             (k, v, kv_start, kv_len, kv_index, mask, out))
     return out
