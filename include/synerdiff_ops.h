@@ -221,7 +221,7 @@ sd_status synerdiff_op_rmsnorm(int32_t dtype, const void* d_x, int64_t x_ld, con
  * fp32 [M, N], may be NULL; add may equal an fp32 out of out_ld = N; out
  * overlaps nothing else.  Products and sums are fp32-accurate for every
  * x_type.  A row of x with an infinity or NaN gives no finite value.
- * K a multiple of 8, <= 2^24, M <= 2^20; x and its rows 16-byte aligned (e4m3: 8).  The rows of a
+ * K a multiple of 8, x_ld <= 2^24, M <= 2^20; x and its rows 16-byte aligned (e4m3: 8).  The rows of a
  * result do not depend on M.  M = 0 or N = 0 does nothing. */
 sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* d_x, int64_t x_ld, const float* d_x_scale,
                                       int32_t x_group, int32_t M, int32_t K, const uint8_t* d_w, int32_t group,

@@ -23,6 +23,8 @@
 // The waves of a block split K in chunks of 128 and are summed through LDS in
 // order.  The split depends on K and N, never on M: a row's bits do not
 // depend on the rows beside it.
+#include <type_traits>
+
 #include "device_common.h"
 #include "kernels.h"
 
@@ -54,57 +56,79 @@ __device__ __forceinline__ void transpose_groups(u32x4& r) {
 #endif
 }
 
-// 8 codes -> bf16, in the order k = 0 2 4 6 1 3 5 7.
+// 8 codes -> bf16, in the order of k.
 __device__ __forceinline__ u32x4 codes_bf16(uint32_t w) {
   u32x4 r = {0, 0, 0, 0};
 #if defined(__HIP_DEVICE_COMPILE__)
   const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
-  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(even, 512.f, false));
-  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(even, 512.f, true));
-  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, 512.f, false));
-  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, 512.f, true));
+  const uint32_t lo = __builtin_amdgcn_perm(odd, even, 0x05010400u), hi = __builtin_amdgcn_perm(odd, even, 0x07030602u);
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.f, false));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.f, true));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.f, false));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.f, true));
 #endif
   return r;
 }
 
-// The high (low) halves of a (first) and b as one dword.
+// The high halves of a (first) and b as one dword.
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 
-// Codes of a tile of T x 16 weight rows, and the scale and zero point of a
-// (row, group).  Offsets past the tile's last row read as zero; a row past N
-// takes row N - 1's scales and is not stored.
-template <int T, int G>
-struct Weights {
-  __amdgpu_buffer_rsrc_t rsrc;
-  int off[T];
-  long at[T];
-  __device__ __forceinline__ Weights(const LinearW4Args& a, int n0, int col, int grp) {
-    const int rowb = a.K >> 1;
-    rsrc = make_rsrc(a.w + (long)n0 * rowb, (long)min(16 * T, a.N - n0) * rowb);
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-      off[t] = (16 * t + col) * rowb + grp * 16;
-      at[t] = (long)min(n0 + 16 * t + col, a.N - 1) * a.groups;
-    }
-  }
-  __device__ __forceinline__ u32x4 codes(int t, int c) const {
-    return __builtin_bit_cast(u32x4, buf_load16(rsrc, off[t] + c * (KC / 2)));
-  }
-  __device__ __forceinline__ void scales(const LinearW4Args& a, int t, int c, float (&s)[KC / G], float (&z)[KC / G]) const {
-#pragma unroll
-    for (int g = 0; g < KC / G; ++g) {
-      const long i = at[t] + min(c * (KC / G) + g, a.groups - 1);
-      s[g] = a.scale_f32 ? ((const float*)a.scale)[i] : (float)((const bf16*)a.scale)[i];
-      z[g] = a.zero ? (float)(a.zero[i] & 15) : 8.0f;
+// A wave's work in order: chunks wave, wave + nw, ... of the block's tiles of
+// weight rows (blockIdx.x, + gridDim.x, ...), one sequence, so that loads run
+// ahead across tiles.
+struct Item {
+  int tile, c;
+  __device__ __forceinline__ void next(int wave, int nw, int chunks, int stride) {
+    c += nw;
+    if (c >= chunks) {
+      c = wave;
+      tile += stride;
     }
   }
 };
 
-// The sum of nw partial tiles of LDS ([wave][T][MT][4][64] accumulators) in
-// order, and the epilogue, on rows of 16 T columns.
+// Codes, scales and zero points of T x 16 weight rows.  Codes: four lanes a
+// row, 16 bytes each.  Scales: lane (col, g) loads those of row col and the
+// chunk's group g, and every lane of the column asks it.  (Offsets past a
+// resource's end, of rows past N, read as zero.)
+template <int T, int G>
+struct Weights {
+  static constexpr int GC = KC / G;
+  int woff, col, grp;
+  __device__ __forceinline__ Weights(const LinearW4Args& a, int lane) : col(lane & 15), grp(lane >> 4) {
+    woff = (lane >> 2) * (a.K >> 1) + (lane & 3) * 16;
+  }
+  __device__ __forceinline__ void codes(const LinearW4Args& a, const Item& it, u32x4 (&w)[T]) const {
+    const int n0 = it.tile * 16 * T, rowb = a.K >> 1;
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.w + (long)n0 * rowb, (long)min(16 * T, a.N - n0) * rowb);
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+      w[t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, woff + 16 * t * rowb, it.c * (KC / 2), 0));
+  }
+  __device__ __forceinline__ void scales(const LinearW4Args& a, const Item& it, float (&s)[T], int (&z)[T]) const {
+    const int n0 = it.tile * 16 * T;
+    const long first = (long)n0 * a.groups, count = (long)min(16 * T, a.N - n0) * a.groups;
+    if (grp < GC) {
+      const int g = min(it.c * GC + grp, a.groups - 1);
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        const int i = (16 * t + col) * a.groups + g;
+        if (a.scale_f32)
+          s[t] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(make_rsrc((const float*)a.scale + first, count * 4), i * 4, 0, 0));
+        else
+          s[t] = __uint_as_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b16(make_rsrc((const bf16*)a.scale + first, count * 2), i * 2, 0, 0) << 16);
+        if (a.zero) z[t] = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(a.zero + first, count), i, 0, 0);
+      }
+    }
+  }
+  template <typename V>
+  __device__ __forceinline__ V at(V v, int g) const { return __shfl(v, col + 16 * g, 64); }
+};
+
+// The sum of nw waves' tiles ([T][MT][4][64] accumulators, `apart` floats apart)
+// in order, and the epilogue, on rows of 16 T columns.
 template <int T, int MT>
-__device__ __forceinline__ void finish(const LinearW4Args& a, const float* red, int nw, int n0, int m0, int tid, int nt,
+__device__ __forceinline__ void finish(const LinearW4Args& a, const float* red, int apart, int nw, int n0, int m0, int tid, int nt,
                                        bool row_scale) {
   constexpr int TILE = T * MT * 256;
   for (int e = tid; e < TILE; e += nt) {
@@ -112,11 +136,10 @@ __device__ __forceinline__ void finish(const LinearW4Args& a, const float* red, 
     const int n = n0 + nl, m = m0 + ml;
     if (n >= a.N || m >= a.M) continue;
     const int at = (((nl >> 4) * MT + (ml >> 4)) * 4 + (ml & 3)) * 64 + ((ml & 15) >> 2) * 16 + (nl & 15);
+    const float b = a.bias ? a.bias[n] : 0.f, ad = a.add ? a.add[(long)m * a.N + n] : 0.f, xs = row_scale ? a.x_scale[m] : 1.f;
     float v = red[at];
-    for (int u = 1; u < nw; ++u) v += red[u * TILE + at];
-    if (row_scale) v *= a.x_scale[m];
-    if (a.bias) v += a.bias[n];
-    if (a.add) v += a.add[(long)m * a.N + n];
+    for (int u = 1; u < nw; ++u) v += red[u * apart + at];
+    v = fmaf(v, xs, b) + ad;
     if (a.silu_out) v = silu_f(v);
     if (a.out_f32)
       ((float*)a.out)[m * a.out_ld + n] = v;
@@ -127,145 +150,365 @@ __device__ __forceinline__ void finish(const LinearW4Args& a, const float* red, 
 
 }  // namespace
 
-// bf16 (E8 = 0) and e4m3 (E8 = 1) x: every wave loads its own operands of x
-// (through L1) for MT tiles of 16 rows and T of 16 weight rows.
+// bf16 (E8 = 0) and e4m3 (E8 = 1) x, for MT tiles of 16 rows and T of 16 weight
+// rows.  Neighbouring lanes load neighbouring bytes of a row (a lane per row,
+// as the MFMA wants it, takes the L1 one cycle per lane: 8192 x 8192, 16 rows
+// 18.8 us); a wave's own piece of LDS turns them into operands, without a
+// barrier.
+template <bool E8, int MT, int T>
+__host__ __device__ constexpr int w4_wave_bytes() { return T * 16 * 80 + MT * 16 * 17 * (E8 ? 8 : 16); }
+template <int T>
+__host__ __device__ constexpr int w4_f32_wave_bytes() { return T * 16 * 80 + 3 * 16 * (KC + 16); }
+
 template <bool E8, int MT, int T, int G>
 __global__ __launch_bounds__(1024) void linear_w4_kernel(LinearW4Args a) {
   constexpr int GC = KC / G, JG = G / 32;  // groups per chunk; MFMA steps per group
-  extern __shared__ float red[];           // [waves][T][MT][4][64]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  const int n0 = blockIdx.x * 16 * T, m0 = blockIdx.y * 16 * MT;
+  constexpr int PF = 2;                    // chunks whose codes are in flight
+  constexpr int XB = E8 ? 8 : 16;          // bytes of 8 k of x
+  constexpr int WROW = 80, XROW = 16 * XB + XB;  // LDS rows of codes and x: padded against bank conflicts
+  constexpr int WAVE = w4_wave_bytes<E8, MT, T>();
+  typedef typename std::conditional<E8, uint2, u32x4>::type XPiece;
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
+  const int m0 = blockIdx.y * 16 * MT, tiles = (a.N + 16 * T - 1) / (16 * T);
   const int col = lane & 15, grp = lane >> 4;
-  const Weights<T, G> wt(a, n0, col, grp);
-  const int chunks = (a.K + KC - 1) / KC;
-  const uint8_t* xm[MT];
+  uint8_t* wl = smem + wave * WAVE;
+  uint8_t* xl = wl + T * 16 * WROW;
+  const int wput = (lane >> 2) * WROW + (lane & 3) * 16, wget = col * WROW + grp * 16;
+  const int xput = grp * XROW + col * XB, xget = col * XROW + grp * XB;
+  const int ldb = (int)a.x_ld * (XB / 8), chunks = (a.K + KC - 1) / KC, rows = min(16 * MT, a.M - m0);
+  const __amdgpu_buffer_rsrc_t xr = make_rsrc((const uint8_t*)a.x + (long)m0 * ldb, (long)(rows - 1) * ldb + a.K * (XB / 8));
+  const Weights<T, G> wt(a, lane);
+  // x: piece i of a lane is row 4 i + lane / 16, 8 k from 8 (lane % 16) on
+  const int xoff = grp * ldb + col * XB;
+  const bool xblocks = E8 && a.x_blocks > 1;
+
+  float sn[T], xsn[MT];  // (xsn: row col of each tile of x)
+  int zn[T];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) xm[i] = (const uint8_t*)a.x + (long)min(m0 + 16 * i + col, a.M - 1) * a.x_ld * (E8 ? 1 : 2);
+  for (int i = 0; i < MT; ++i) xsn[i] = 1.0f;
+  auto load_x = [&](int c, XPiece (&x)[4 * MT]) __attribute__((always_inline)) {
+    // (K is a multiple of 8: a lane's 8 k are all in or all out)
+    const int at = c * KC + 8 * col < a.K ? xoff : OOB;
+#pragma unroll
+    for (int i = 0; i < 4 * MT; ++i) {
+      if (4 * i >= rows) break;  // (rows past M hold anything: they reach only their own results)
+      const int soff = c * 16 * XB;
+      if constexpr (E8)
+        x[i] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(xr, at + i * 4 * ldb, soff, 0));
+      else
+        x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, at + i * 4 * ldb, soff, 0));
+    }
+    if (xblocks)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) xsn[i] = a.x_scale[(long)min(m0 + 16 * i + col, a.M - 1) * a.x_blocks + c];
+  };
 
   f32x4 acc[T][MT];
 #pragma unroll
   for (int t = 0; t < T; ++t)
 #pragma unroll
     for (int i = 0; i < MT; ++i) acc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 wn[T];
+  u32x4 w[PF][T];
+  XPiece xn[4 * MT] = {};
+  Item it = {(int)blockIdx.x, wave}, it1 = it, itw;  // this chunk, the next, the one whose codes are loaded next
+  it1.next(wave, nw, chunks, gridDim.x);
+  itw = it1;
+  wt.codes(a, it, w[0]);  // (nw <= chunks: every wave has a chunk of every tile)
+  load_x(it.c, xn);
+  wt.scales(a, it, sn, zn);
 #pragma unroll
-  for (int t = 0; t < T; ++t) wn[t] = wt.codes(t, wave);  // (nw <= chunks)
-  for (int c = wave; c < chunks; c += nw) {
-    u32x4 w[T], x[MT][4];
+  for (int u = 1; u < PF; ++u) {
+    if (itw.tile < tiles) wt.codes(a, itw, w[u]);
+    itw.next(wave, nw, chunks, gridDim.x);
+  }
+  auto chunk = [&](u32x4 (&w)[T]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < T; ++t) w[t] = wn[t];
+    for (int t = 0; t < T; ++t) *(u32x4*)(wl + t * 16 * WROW + wput) = w[t];
+#pragma unroll
+    for (int i = 0; i < 4 * MT; ++i) *(XPiece*)(xl + i * 4 * XROW + xput) = xn[i];
+    float s[T], xs[MT];
+    int z[T];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xs[i] = xsn[i];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      s[t] = sn[t];
+      z[t] = zn[t];
+    }
+    asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
+    u32x4 q[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) q[t] = *(const u32x4*)(wl + t * 16 * WROW + wget);
+    XPiece xp[MT][4];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int k = c * KC + 32 * j + 8 * grp;  // (K is a multiple of 8: a lane's 8 k are all in or all out)
-        u32x4 v = {0, 0, 0, 0};
-        if (k < a.K) {
-          if constexpr (E8) {
-            const uint2 u = *(const uint2*)(xm[i] + k);
-            v[0] = u.x; v[1] = u.y;
-          } else {
-            v = *(const u32x4*)(xm[i] + 2 * k);
-          }
-        }
-        x[i][j] = v;
-      }
-    float s[T][GC], z[T][GC];
+      for (int j = 0; j < 4; ++j) xp[i][j] = *(const XPiece*)(xl + i * 16 * XROW + j * 4 * XB + xget);
+    if (it1.tile < tiles) {
+      load_x(it1.c, xn);
+      wt.scales(a, it1, sn, zn);
+    }
+    if (itw.tile < tiles) wt.codes(a, itw, w);
 #pragma unroll
-    for (int t = 0; t < T; ++t) wt.scales(a, t, c, s[t], z[t]);
-    if (c + nw < chunks)
-#pragma unroll
-      for (int t = 0; t < T; ++t) wn[t] = wt.codes(t, c + nw);
-#pragma unroll
-    for (int t = 0; t < T; ++t) transpose_groups(w[t]);
+    for (int t = 0; t < T; ++t) transpose_groups(q[t]);
 
     f32x4 part[T][MT];  // e4m3: the chunk's sums, until its scale of x multiplies them
 #pragma unroll
     for (int g = 0; g < GC; ++g) {
       f32x4 d[T][MT], sx[MT];
+      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+      const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
 #pragma unroll
       for (int j = g * JG; j < (g + 1) * JG; ++j) {
-        u32x4 q[T];
-#pragma unroll
-        for (int t = 0; t < T; ++t) q[t] = codes_bf16(w[t][j]);
-        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+        const bool first = j == g * JG;
+        u32x4 b[MT];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          u32x4 b = {0, 0, 0, 0};  // the lane's 8 k in the order of codes_bf16
           if constexpr (E8) {
 #if defined(__HIP_DEVICE_COMPILE__)
-            const auto e0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][j][0], false), e1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][j][0], true);
-            const auto e2 = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][j][1], false), e3 = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i][j][1], true);
-            b[0] = high_halves(__float_as_uint(e0[0]), __float_as_uint(e1[0]));
-            b[1] = high_halves(__float_as_uint(e2[0]), __float_as_uint(e3[0]));
-            b[2] = high_halves(__float_as_uint(e0[1]), __float_as_uint(e1[1]));
-            b[3] = high_halves(__float_as_uint(e2[1]), __float_as_uint(e3[1]));
+            b[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xp[i][j].x, 1.f, false));
+            b[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xp[i][j].x, 1.f, true));
+            b[i][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xp[i][j].y, 1.f, false));
+            b[i][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xp[i][j].y, 1.f, true));
+#else
+            b[i] = ones;
 #endif
           } else {
-            b[0] = low_halves(x[i][j][0], x[i][j][1]);
-            b[1] = low_halves(x[i][j][2], x[i][j][3]);
-            b[2] = high_halves(x[i][j][0], x[i][j][1]);
-            b[3] = high_halves(x[i][j][2], x[i][j][3]);
+            b[i] = xp[i][j];
           }
-          const bool first = j == g * JG;
-          sx[i] = mfma(b, ones, first ? zero : sx[i]);
+          sx[i] = mfma(b[i], ones, first ? zero : sx[i]);
+        }
 #pragma unroll
-          for (int t = 0; t < T; ++t) d[t][i] = mfma(b, q[t], first ? zero : d[t][i]);
+        for (int t = 0; t < T; ++t) {
+          const u32x4 qb = codes_bf16(q[t][j]);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) d[t][i] = mfma(b[i], qb, first ? zero : d[t][i]);
         }
       }
 #pragma unroll
-      for (int t = 0; t < T; ++t)
+      for (int t = 0; t < T; ++t) {
+        const float sg = wt.at(s[t], g), zg = a.zero ? (float)(wt.at(z[t], g) & 15) : 8.0f;
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float v = fmaf(-z[t][g], sx[i][e], d[t][i][e]);
+            const float v = fmaf(-zg, sx[i][e], d[t][i][e]);
             if constexpr (E8)
-              part[t][i][e] = g == 0 ? s[t][g] * v : fmaf(s[t][g], v, part[t][i][e]);
+              part[t][i][e] = g == 0 ? sg * v : fmaf(sg, v, part[t][i][e]);
             else
-              acc[t][i][e] = fmaf(s[t][g], v, acc[t][i][e]);
+              acc[t][i][e] = fmaf(sg, v, acc[t][i][e]);
           }
+      }
     }
     if constexpr (E8) {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int m = min(m0 + 16 * i + 4 * grp + e, a.M - 1);
-          const float xs = a.x_blocks > 1 ? a.x_scale[(long)m * a.x_blocks + c] : 1.0f;
+          const float x = __shfl(xs[i], 4 * grp + e, 64);
 #pragma unroll
-          for (int t = 0; t < T; ++t) acc[t][i][e] = fmaf(xs, part[t][i][e], acc[t][i][e]);
+          for (int t = 0; t < T; ++t) acc[t][i][e] = fmaf(x, part[t][i][e], acc[t][i][e]);
         }
     }
-  }
+    if (it1.tile != it.tile) {  // the tile's last chunk
+      float* red = (float*)wl;  // (the wave's own operands are used up)
 #pragma unroll
-  for (int t = 0; t < T; ++t)
+      for (int t = 0; t < T; ++t)
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) red[((wave * T + t) * MT + i) * 256 + e * 64 + lane] = acc[t][i][e];
-  __syncthreads();
-  finish<T, MT>(a, red, nw, n0, m0, threadIdx.x, blockDim.x, E8 && a.x_blocks == 1);
+          for (int e = 0; e < 4; ++e) {
+            red[(t * MT + i) * 256 + e * 64 + lane] = acc[t][i][e];
+            acc[t][i][e] = 0.f;
+          }
+      __syncthreads();
+      finish<T, MT>(a, (const float*)smem, WAVE / 4, nw, it.tile * 16 * T, m0, threadIdx.x, blockDim.x, E8 && !xblocks);
+      __syncthreads();
+    }
+    it = it1;
+    it1.next(wave, nw, chunks, gridDim.x);
+    itw.next(wave, nw, chunks, gridDim.x);
+  };
+  while (it.tile < tiles)
+#pragma unroll
+    for (int u = 0; u < PF; ++u)
+      if (it.tile < tiles) chunk(w[u]);
 }
 
-// fp32 x, and any x under SiLU.  The activation and the cut into parts cost
-// many times what a code does, so WN waves side by side (16 weight rows each)
-// share one staging of x in LDS; wave rows wk split K.
-template <int MT, int WN, int G>
+// fp32 x, and any x under SiLU, for 16 rows and T tiles of 16 weight rows.  As
+// above, but x goes through LDS half a chunk at a time, cut into its parts on
+// the way.  (Sharing that pass among 2 to 8 waves side by side left too few
+// waves along K and made all of them wait for it: 8192 x 8192, 1 row 40 us.)
+template <int T, int G>
 __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
-  constexpr int GC = KC / G, JG = G / 32, LD = KC + 8;  // LDS rows 272 bytes apart: no bank conflicts over 16 rows
+  constexpr int GC = KC / G, HC = KC / 2, WROW = 80, XROW = HC * 2 + 16, PART = 16 * XROW;
+  constexpr int WAVE = w4_f32_wave_bytes<T>();
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
+  const int m0 = blockIdx.y * 16, tiles = (a.N + 16 * T - 1) / (16 * T);
+  const int col = lane & 15, grp = lane >> 4;
+  uint8_t* wl = smem + wave * WAVE;
+  uint8_t* xl = wl + T * 16 * WROW;  // [3][16] rows
+  const int wput = (lane >> 2) * WROW + (lane & 3) * 16, wget = col * WROW + grp * 16;
+  const int xput = (lane >> 3) * XROW + (lane & 7) * 16, xget = col * XROW + grp * 16;
+  const int xs = a.x_type == 0 ? 4 : 2, ldb = (int)a.x_ld * xs;
+  const int chunks = (a.K + KC - 1) / KC, rows = min(16, a.M - m0);
+  const __amdgpu_buffer_rsrc_t xr = make_rsrc((const uint8_t*)a.x + (long)m0 * ldb, (long)(rows - 1) * ldb + a.K * xs);
+  const Weights<T, G> wt(a, lane);
+  const int xoff = (lane >> 3) * ldb + (lane & 7) * 8 * xs;  // 8 lanes a row, 8 rows a load
+
+  // half h of chunk c
+  auto load_x = [&](int c, int h, u32x4 (&x)[2][2]) __attribute__((always_inline)) {
+    const int k = c * KC + h * HC;
+    const int at = k + 8 * (lane & 7) < a.K ? xoff : OOB;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (8 * i >= rows) break;
+      const int off = at + i * 8 * ldb;
+      x[i][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, off, k * xs, 0));
+      if (a.x_type == 0) x[i][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, off + 16, k * xs, 0));
+    }
+  };
+  auto put_x = [&](const u32x4 (&x)[2][2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (8 * i >= rows) break;
+      uint32_t part[3][8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float v;
+        if (a.x_type == 0)
+          v = __uint_as_float(x[i][e >> 2][e & 3]);
+        else
+          v = __uint_as_float(e & 1 ? x[i][0][e >> 1] & 0xFFFF0000u : x[i][0][e >> 1] << 16);
+        if (a.silu_in) v = silu_f(v);
+        // (an infinity or NaN leaves a NaN in the second part)
+        part[0][e] = __float_as_uint(v);
+        v -= __uint_as_float(part[0][e] & 0xFFFF0000u);
+        part[1][e] = __float_as_uint(v);
+        v -= __uint_as_float(part[1][e] & 0xFFFF0000u);
+        part[2][e] = __float_as_uint(v);
+      }
+#pragma unroll
+      for (int u = 0; u < 3; ++u) {
+        u32x4 b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = high_halves(part[u][2 * e], part[u][2 * e + 1]);
+        *(u32x4*)(xl + u * PART + i * 8 * XROW + xput) = b;
+      }
+    }
+  };
+
+  f32x4 acc[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 wn[T], xn[2][2] = {};
+  float sn[T];
+  int zn[T];
+  Item it = {(int)blockIdx.x, wave};
+  wt.codes(a, it, wn);  // (nw <= chunks: every wave has a chunk of every tile)
+  load_x(it.c, 0, xn);
+  wt.scales(a, it, sn, zn);
+  while (it.tile < tiles) {
+    Item it1 = it;
+    it1.next(wave, nw, chunks, gridDim.x);
+    float s[T];
+    int z[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      *(u32x4*)(wl + t * 16 * WROW + wput) = wn[t];
+      s[t] = sn[t];
+      z[t] = zn[t];
+    }
+    u32x4 q[T];
+    f32x4 d[T], e[T], sx, sy;  // products and sums of x: of the first part, of the others
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      put_x(xn);
+      asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
+      if (h == 0) {
+#pragma unroll
+        for (int t = 0; t < T; ++t) q[t] = *(const u32x4*)(wl + t * 16 * WROW + wget);
+        load_x(it.c, 1, xn);
+        if (it1.tile < tiles) wt.codes(a, it1, wn);
+      } else if (it1.tile < tiles) {
+        load_x(it1.c, 0, xn);
+        wt.scales(a, it1, sn, zn);
+      }
+      if (h == 0)
+#pragma unroll
+        for (int t = 0; t < T; ++t) transpose_groups(q[t]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int jc = 2 * h + j, g = jc * 32 / G;  // step and group within the chunk
+        u32x4 x[3];
+#pragma unroll
+        for (int u = 0; u < 3; ++u) x[u] = *(const u32x4*)(xl + u * PART + j * 64 + xget);
+        if (jc * 32 % G == 0) {
+          sx = sy = zero;
+#pragma unroll
+          for (int t = 0; t < T; ++t) d[t] = e[t] = zero;
+        }
+        sy = mfma(x[1], ones, mfma(x[2], ones, sy));
+        sx = mfma(x[0], ones, sx);
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+          const u32x4 b = codes_bf16(q[t][jc]);
+          e[t] = mfma(x[1], b, mfma(x[2], b, e[t]));
+          d[t] = mfma(x[0], b, d[t]);
+        }
+        if ((jc + 1) * 32 % G == 0)
+#pragma unroll
+          for (int t = 0; t < T; ++t) {
+            const float sg = wt.at(s[t], g), zg = a.zero ? (float)(wt.at(z[t], g) & 15) : 8.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(sg, fmaf(-zg, sx[i] + sy[i], d[t][i] + e[t][i]), acc[t][i]);
+          }
+      }
+      asm volatile("" ::: "memory");
+    }
+    if (it1.tile != it.tile) {  // the tile's last chunk
+      float* red = (float*)wl;  // (the wave's own operands are used up)
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          red[t * 256 + i * 64 + lane] = acc[t][i];
+          acc[t][i] = 0.f;
+        }
+      __syncthreads();
+      finish<T, 1>(a, (const float*)smem, WAVE / 4, nw, it.tile * 16 * T, m0, threadIdx.x, blockDim.x, false);
+      __syncthreads();
+    }
+    it = it1;
+  }
+}
+
+// The same for wide layers: WN waves side by side (16 weight rows each) share
+// one pass of x through LDS, wave rows wk split K.  (20160 x 1280, fp32 under
+// SiLU: 1 row 11.3 us against 14.1 above, 32 rows 18.5 against 29; narrower
+// layers leave it too few waves along K: 8192 x 8192, 1 row 40 us against 20.)
+template <int MT, int G>
+__global__ __launch_bounds__(1024) void linear_w4_wide_kernel(LinearW4Args a) {
+  constexpr int WN = 8, GC = KC / G, JG = G / 32, LD = KC + 8;  // LDS rows 272 bytes apart: no bank conflicts over 16 rows
   constexpr int ROWS = 16 * MT, NT = 64 * WN, PIECES = ROWS * (KC / 8), PPT = (PIECES + NT - 1) / NT;
   constexpr int XB = 3 * ROWS * LD;  // bf16 of one wave row's chunk
   extern __shared__ float lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nwk = blockDim.x / NT;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nwk = blockDim.x / NT;
   const int wn = wave % WN, wk = wave / WN, tid = threadIdx.x % NT;
   bf16* xs = (bf16*)lds + wk * XB;                               // [3][ROWS][LD]
   float* xsum = lds + nwk * (XB / 2) + wk * ROWS * GC;           // [GC][ROWS]
   const int n0 = blockIdx.x * 16 * WN, m0 = blockIdx.y * ROWS;
   const int col = lane & 15, grp = lane >> 4;
   const bool tile_on = n0 + 16 * wn < a.N;
-  const Weights<1, G> wt(a, tile_on ? n0 + 16 * wn : n0, col, grp);
+  const int tile = tile_on ? n0 / 16 + wn : n0 / 16;
+  const int rowb = a.K >> 1;
+  const __amdgpu_buffer_rsrc_t wr = make_rsrc(a.w + (long)tile * 16 * rowb, (long)min(16, a.N - 16 * tile) * rowb);
+  const int woff = col * rowb + grp * 16;
+  const long sat = (long)min(16 * tile + col, a.N - 1) * a.groups;
   const int chunks = (a.K + KC - 1) / KC;
 
   // A thread stages 8 k of a row at a time, 16 threads a row.
@@ -305,11 +548,9 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
       }
 #pragma unroll
       for (int u = 0; u < 3; ++u) {
-        u32x4 b;  // the order of codes_bf16
-        b[0] = high_halves(part[u][0], part[u][2]);
-        b[1] = high_halves(part[u][4], part[u][6]);
-        b[2] = high_halves(part[u][1], part[u][3]);
-        b[3] = high_halves(part[u][5], part[u][7]);
+        u32x4 b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = high_halves(part[u][2 * e], part[u][2 * e + 1]);
         *(u32x4*)(xs + (u * ROWS + row) * LD + 8 * (idx % 16)) = b;
       }
 #pragma unroll
@@ -322,21 +563,28 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
 #pragma unroll
   for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   fetch(wk);  // (nwk <= chunks)
-  u32x4 wnext = wt.codes(0, wk);
+  // (codes and scales: a lane per row.  The turn through LDS of the kernels
+  // above, and scales a round ahead, cost these barriers 2 us.)
+  u32x4 wnext = __builtin_bit_cast(u32x4, buf_load16(wr, woff + wk * (KC / 2)));
   const int rounds = (chunks + nwk - 1) / nwk;
   for (int r = 0; r < rounds; ++r) {
     const int c = r * nwk + wk;
-    u32x4 w = wnext;
     if (r) __syncthreads();  // the last round's operands have been read
     if (c < chunks) stage();
     __syncthreads();
+    u32x4 w = wnext;
     float s[GC], z[GC];
-    wt.scales(a, 0, min(c, chunks - 1), s, z);
+#pragma unroll
+    for (int g = 0; g < GC; ++g) {
+      const long i = sat + min(c * GC + g, a.groups - 1);
+      s[g] = a.scale_f32 ? ((const float*)a.scale)[i] : (float)((const bf16*)a.scale)[i];
+      z[g] = a.zero ? (float)(a.zero[i] & 15) : 8.0f;
+    }
     if (c + nwk < chunks) {
       fetch(c + nwk);
-      wnext = wt.codes(0, c + nwk);
+      wnext = __builtin_bit_cast(u32x4, buf_load16(wr, woff + (c + nwk) * (KC / 2)));
     }
-    if (c >= chunks) continue;
+    if (c >= chunks) continue;  // (the last round)
     transpose_groups(w);
 #pragma unroll
     for (int g = 0; g < GC; ++g) {
@@ -365,60 +613,85 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
     for (int e = 0; e < 4; ++e) lds[((wn * nwk + wk) * MT + i) * 256 + e * 64 + lane] = acc[i][e];
   __syncthreads();
   // wave row wk finishes what it can of its column's tile
-  if (tile_on) finish<1, MT>(a, lds + wn * nwk * MT * 256, nwk, n0 + 16 * wn, m0, wk * 64 + lane, nwk * 64, false);
+  if (tile_on) finish<1, MT>(a, lds + wn * nwk * MT * 256, MT * 256, nwk, n0 + 16 * wn, m0, wk * 64 + lane, nwk * 64, false);
 }
 
-template <bool E8, int MT, int T>
+// Blocks: as many as run at once (16 waves a CU at up to 128 registers), each
+// over several tiles where there are more (bf16, 16 rows, 20160 x 1280: 12.2 ->
+// 10.5 us; 64 rows 34.6 -> 27).  A wave's sums take the place of its operands in LDS.
+static dim3 w4_grid(int tiles, int rows, int nw) {
+  const int once = 256 * (16 / nw);
+  return dim3((unsigned)(tiles < once ? tiles : once), (unsigned)rows);
+}
+
+template <bool E8, int MT, int T, int G>
 static void launch_tile(const LinearW4Args& a, hipStream_t s) {
-  const int chunks = (a.K + KC - 1) / KC, nw = chunks < 16 ? chunks : 16;
-  const dim3 grid((unsigned)((a.N + 16 * T - 1) / (16 * T)), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
-  const size_t lds = (size_t)nw * T * MT * 1024;
-  if (a.group == 32)
-    linear_w4_kernel<E8, MT, T, 32><<<grid, 64 * nw, lds, s>>>(a);
-  else if (a.group == 64)
-    linear_w4_kernel<E8, MT, T, 64><<<grid, 64 * nw, lds, s>>>(a);
-  else
-    linear_w4_kernel<E8, MT, T, 128><<<grid, 64 * nw, lds, s>>>(a);
+  constexpr int MOST = 16;
+  constexpr size_t wave = w4_wave_bytes<E8, MT, T>();
+  static_assert(MOST * wave <= 160 * 1024 && wave >= T * MT * 1024, "the LDS holds 16 waves");
+  const int chunks = (a.K + KC - 1) / KC, nw = chunks < MOST ? chunks : MOST;
+  const dim3 grid = w4_grid((a.N + 16 * T - 1) / (16 * T), (a.M + 16 * MT - 1) / (16 * MT), nw);
+  linear_w4_kernel<E8, MT, T, G><<<grid, 64 * nw, nw * wave, s>>>(a);
 }
 
-template <bool E8>
+// Two tiles of x rows past 16 rows, two of weight rows where there are plenty
+// (half the traffic of x), as far as 128 registers hold them: groups of 32
+// take one by one, e4m3 in groups of 64 one tile of x.
+template <bool E8, int G>
 static void launch_x(const LinearW4Args& a, hipStream_t s) {
-  if (a.M > 16)
-    launch_tile<E8, 2, 1>(a, s);
-  else if (a.N >= 8192)
-    launch_tile<E8, 1, 2>(a, s);
+  constexpr int MT = G == 128 || (G == 64 && !E8) ? 2 : 1, T = G == 32 ? 1 : 2;
+  if (MT == 2 && a.M > 16)
+    launch_tile<E8, MT, 1, G>(a, s);
+  else if (T == 2 && a.N >= 8192)
+    launch_tile<E8, 1, T, G>(a, s);
   else
-    launch_tile<E8, 1, 1>(a, s);
+    launch_tile<E8, 1, 1, G>(a, s);
 }
 
-template <int MT, int WN>
-static void launch_f32(const LinearW4Args& a, hipStream_t s) {
-  constexpr int MOST = 16 / WN;  // wave rows
+template <int T, int G>
+static void launch_f32_tile(const LinearW4Args& a, hipStream_t s) {
+  constexpr int MOST = 16;
+  constexpr size_t wave = w4_f32_wave_bytes<T>();
+  static_assert(MOST * wave <= 160 * 1024 && wave >= T * 1024, "the LDS holds 16 waves");
+  const int chunks = (a.K + KC - 1) / KC, nw = chunks < MOST ? chunks : MOST;
+  const dim3 grid = w4_grid((a.N + 16 * T - 1) / (16 * T), (a.M + 15) / 16, nw);
+  linear_w4_f32_kernel<T, G><<<grid, 64 * nw, nw * wave, s>>>(a);
+}
+
+template <int MT, int G>
+static void launch_wide(const LinearW4Args& a, hipStream_t s) {
+  constexpr int WN = 8, MOST = 2;
   const int chunks = (a.K + KC - 1) / KC, nwk = chunks < MOST ? chunks : MOST;
   const dim3 grid((unsigned)((a.N + 16 * WN - 1) / (16 * WN)), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
-  const size_t stage = (size_t)nwk * (3 * 16 * MT * (KC + 8) * 2 + 16 * MT * (KC / a.group) * 4), sum = (size_t)nwk * WN * MT * 1024;
-  const size_t lds = stage > sum ? stage : sum;
-  if (a.group == 32)
-    linear_w4_f32_kernel<MT, WN, 32><<<grid, 64 * WN * nwk, lds, s>>>(a);
-  else if (a.group == 64)
-    linear_w4_f32_kernel<MT, WN, 64><<<grid, 64 * WN * nwk, lds, s>>>(a);
+  // operands of x and their sums; the waves' sums take their place
+  constexpr size_t row = 3 * 16 * MT * (KC + 8) * 2 + 16 * MT * (KC / G) * 4;
+  static_assert(row >= WN * MT * 1024 && MOST * row <= 160 * 1024, "the sums fit, and all of it the LDS");
+  linear_w4_wide_kernel<MT, G><<<grid, 64 * WN * nwk, nwk * row, s>>>(a);
+}
+
+// (the kernel follows N alone, so that a row's bits do not depend on M)
+template <int G>
+static void launch_f32(const LinearW4Args& a, hipStream_t s) {
+  if (a.N < 16384) {
+    if (G == 128 && a.N >= 8192)  // (two tiles of weight rows spill at smaller groups)
+      launch_f32_tile<G == 128 ? 2 : 1, G>(a, s);
+    else
+      launch_f32_tile<1, G>(a, s);
+  }
+  else if (a.M > 16)
+    launch_wide<2, G>(a, s);
   else
-    linear_w4_f32_kernel<MT, WN, 128><<<grid, 64 * WN * nwk, lds, s>>>(a);
+    launch_wide<1, G>(a, s);
 }
 
 hipError_t launch_linear_w4(const LinearW4Args& a, hipStream_t s) {
   if (a.M <= 0 || a.N <= 0) return hipSuccess;
   if (a.x_type == 0 || a.silu_in) {
-    if (a.N < 4096)
-      launch_f32<1, 2>(a, s);  // (8 wave rows' operands of 32 rows of x would pass the LDS)
-    else if (a.N < 16384)
-      a.M > 16 ? launch_f32<2, 4>(a, s) : launch_f32<1, 4>(a, s);
-    else
-      a.M > 16 ? launch_f32<2, 8>(a, s) : launch_f32<1, 8>(a, s);
+    a.group == 32 ? launch_f32<32>(a, s) : a.group == 64 ? launch_f32<64>(a, s) : launch_f32<128>(a, s);
   } else if (a.x_type == 1) {
-    launch_x<false>(a, s);
+    a.group == 32 ? launch_x<false, 32>(a, s) : a.group == 64 ? launch_x<false, 64>(a, s) : launch_x<false, 128>(a, s);
   } else {
-    launch_x<true>(a, s);
+    a.group == 32 ? launch_x<true, 32>(a, s) : a.group == 64 ? launch_x<true, 64>(a, s) : launch_x<true, 128>(a, s);
   }
   return hipGetLastError();
 }

@@ -335,6 +335,7 @@ sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* x, int64_t x_l
   if (M == 0 || N == 0) return SD_OK;
   if (!x || !w || !scale || !out || (x_type == SD_E4M3 && !x_scale)) return op_fail(SD_ERR_INVALID_ARG, "NULL argument");
   if (x_ld < K || out_ld < N) return op_fail(SD_ERR_INVALID_ARG, "a row stride is below its row");
+  if (x_ld > 1 << 24) return op_fail(SD_ERR_UNSUPPORTED, "rows of x more than 2^24 elements apart");
   const int64_t piece = x_type == SD_F32 ? 4 : 8;  // elements of 16 bytes (e4m3: 8)
   if ((uintptr_t)x % (x_type == SD_E4M3 ? 8 : 16) || x_ld % piece || (uintptr_t)w % 4)
     return op_fail(SD_ERR_INVALID_ARG, "x rows must be 16-byte aligned (e4m3: 8), w 4-byte");

@@ -182,13 +182,13 @@ def _w4_ref(x, xs, w, scale, z, group, bias=None, add=None, silu_in=False):
 
 
 # fp32: each of up to K roundings of a group's partial sums, whose terms are
-# at most 62 scales (codes and zero points moved by 16) against a result of
-# rms 4.6: a random walk of 2^-24 * 0.29 * 26 * sqrt(group) at most, relative
+# at most 62 scales (twice a code or zero point of up to 31) against a result
+# of rms 4.6: a random walk of 2^-24 * 0.29 * 26 * sqrt(group) at most, relative
 # to the rms of the result; 8 times that for the largest of 10^5 values.
 W4 = 8 * 0.29 * 26 * math.sqrt(128) * U32
 
 W4_SHAPES = [(1, 8, 1), (1, 32, 16), (2, 24, 5), (1, 320, 1280), (3, 40, 17), (5, 136, 63), (15, 128, 64), (16, 1280, 65),
-             (17, 2816, 257), (33, 1288, 100), (64, 512, 130), (65, 264, 48), (130, 96, 33), (7, 8192, 40), (2, 16, 2500)]
+             (17, 2816, 257), (33, 1288, 100), (64, 512, 130), (65, 264, 48), (130, 96, 33), (7, 8192, 40), (2, 16, 2500), (3, 264, 16401), (20, 328, 16385), (5, 136, 8200)]
 
 
 @pytest.mark.parametrize("xt", ["f32", "bf16", "e4m3row", "e4m3"])

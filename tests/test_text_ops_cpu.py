@@ -61,6 +61,7 @@ W4 = dict(x_type=BF16, x=A[0], x_ld=64, x_scale=None, x_group=0, M=0, K=64, w=A[
     (dict(x_type=3), -1, "dtype"), (dict(scale_type=2), -1, "dtype"), (dict(out_type=2), -1, "dtype"),
     (dict(K=0), -1, "shape"), (dict(K=60), -1, "shape"), (dict(M=-1), -1, "shape"), (dict(N=-1), -1, "shape"),
     (dict(M=(1 << 20) + 1), -2, "2^20"), (dict(K=(1 << 24) + 8), -2, "2^24"),
+    (dict(M=4, x_ld=(1 << 24) + 8), -2, "2^24"),
     (dict(group=0), -1, "group"), (dict(group=48), -1, "group"), (dict(group=256), -1, "group"),
     (dict(x_scale=A[7]), -1, "x_group"), (dict(x_group=128), -1, "x_group"),
     (dict(x_type=E4M3, x_scale=A[7], x_group=64), -1, "x_group"), (dict(x_type=E4M3, x_scale=A[7], silu_in=1), -2, "silu"),
