@@ -1,78 +1,853 @@
-// Attention of each row's queries over a text of its own length.
+// Attention of each row's queries over a text of its own length:
+//   o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j)
+// over the keys of the row's context that take part.
+//
+// A "row" below is one (query, head) pair of a K/V head: with rep heads to a
+// K/V head, row r of an image and K/V head g is query r / rep, head g rep +
+// r % rep, so shared heads fill the tiles like further queries.
+//
+//  * Many rows (bf16): flash attention on MFMA.  A wave owns 32 QG rows, the
+//    block shares tiles of 64 keys in LDS.  Scores are computed transposed,
+//    S^T = K Q^T, so that a lane holds one row's scores: its maximum and
+//    rescale are per-lane, and P^T feeds O^T = V^T P^T from the registers.
+//    V lies in LDS as it came (key by key); the transposing LDS read hands
+//    each lane four keys of one channel.
+//  * fp32: the same on fp32 MFMAs.
+//  * Few rows (at most 8): no tile to fill, bound by the bytes of K and V.
+//    Lanes share a key's channels, every lane group runs its own online
+//    softmax over the keys that come its way, and the groups are joined at
+//    the end.
+//  * Few rows over long texts are split along the keys into ranges of a fixed
+//    length, whose unnormalised results a second kernel joins in order.  The
+//    ranges start at the text's own first key: a row's bits depend neither on
+//    the batch nor on the longest text in it.
+// Keys that take no part are never read (their memory may hold NaN): masks
+// become a bit per key of a tile before its loads are issued.
+#include <type_traits>
+
 #include "device_common.h"
 #include "kernels.h"
 
 namespace sd {
 
-// The rows of K / V that row `img` reads: first row, count and the mask bytes from the first row on.
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float TAU = 8.0f;  // the running maximum moves when a tile's passes it by this much (log2 units)
+
+// What image `img` reads: its context's first key (elements of K and V, mask byte) and the count.
 struct Text {
-  long k0, v0;   // element offset of key 0 (without the head)
-  long m0;       // mask byte of key 0
-  int len;       // 0: nothing to read
+  long k0, v0, m0;
+  int len;
 };
-__device__ inline Text text_of(const CrossArgs& a, int img) {
+__device__ __forceinline__ Text text_of(const CrossArgs& a, int img) {
   Text t = {0, 0, 0, 0};
   const int c = a.kv_index ? a.kv_index[img] : img;
   if (c < 0 || c >= a.n_ctx) return t;
   int len = a.kv_len ? a.kv_len[c] : a.max_len;
   len = min(max(len, 0), a.max_len);
   if (a.kv_start) {
-    long start = a.kv_start[c];
+    const long start = a.kv_start[c];
     if (start < 0 || start >= a.kv_tokens) return t;
     len = (int)min((long)len, a.kv_tokens - start);
     t.k0 = start * a.k_ld;
     t.v0 = start * a.v_ld;
     t.m0 = start;
   } else {
-    t.k0 = c * a.k_ctx;
-    t.v0 = c * a.v_ctx;
+    t.k0 = (long)c * a.k_ctx;
+    t.v0 = (long)c * a.v_ctx;
     t.m0 = (long)c * a.max_len;
   }
   t.len = len;
   return t;
 }
 
-// One wave per (row, query, head): lanes over the head's channels.
-template <typename T>
-__global__ __launch_bounds__(256) void cross_simple_kernel(CrossArgs a) {
-  const int lane = threadIdx.x & 63;
-  const long e = blockIdx.x * 4L + (threadIdx.x >> 6);
-  if (e >= (long)a.n * a.n_q * a.heads) return;
-  const int h = (int)(e % a.heads), t = (int)(e / a.heads % a.n_q), img = (int)(e / a.heads / a.n_q);
-  const Text tx = text_of(a, img);
-  const T* q = (const T*)a.q + img * a.q_img + t * a.q_ld + h * a.q_head;
-  const T* k = (const T*)a.k + tx.k0 + (h / a.rep) * a.k_head;
-  const T* v = (const T*)a.v + tx.v0 + (h / a.rep) * a.v_head;
-  float qv[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-  for (int i = 0; i < 4; ++i) qv[i] = lane + 64 * i < a.d ? to_f(q[lane + 64 * i]) * a.scale : 0.f;
-  for (int j = 0; j < tx.len; ++j) {
-    if (a.mask && !a.mask[tx.m0 + j]) continue;
-    float s = 0.f;
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < a.d) s += qv[i] * to_f(k[j * a.k_ld + lane + 64 * i]);
-    s = wave_sum(s);
-    const float mn = fmaxf(m, s), al = expf(m - mn), p = expf(s - mn);
-    l = l * al + p;
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < a.d) o[i] = o[i] * al + p * to_f(v[j * a.v_ld + lane + 64 * i]);
-    m = mn;
-  }
-  T* out = (T*)a.o + img * a.o_img + t * a.o_ld + h * a.o_head;
-  for (int i = 0; i < 4; ++i)
-    if (lane + 64 * i < a.d) out[lane + 64 * i] = from_f<T>(l > 0.f ? o[i] / l : 0.f);
+// Block -> (K/V head, row tile, split, image).  Consecutive blocks go to the 8
+// XCDs in turn; the K/V heads of one row tile stay on one XCD, next to each
+// other in time, since their rows share cache lines of q, o, K and V.
+struct Place {
+  int g, tile, split, img;
+  bool on;
+};
+__device__ __forceinline__ Place place_of(int kv_heads, int tiles, int splits, int n) {
+  const unsigned id = blockIdx.x, xcd = id & 7, i = id >> 3;
+  Place p;
+  p.g = i % kv_heads;
+  const unsigned t = i / kv_heads * 8 + xcd;
+  p.on = t < (unsigned)tiles * splits * n;
+  p.tile = t % tiles;
+  p.split = t / tiles % splits;
+  p.img = t / tiles / splits;
+  return p;
+}
+static long place_blocks(long kv_heads, long tiles, long splits, long n) { return (tiles * splits * n + 7) / 8 * 8 * kv_heads; }
+
+// How a call is split: `keys` per range (0: not split).
+struct Plan {
+  int kind;  // 0: few rows, 1: one wave of 32 rows, 2: four waves
+  int keys, splits;
+};
+constexpr int FEW = 8;
+static Plan plan_of(int rep, int n_q, int max_len) {
+  const long rows = (long)rep * n_q;
+  Plan p;
+  p.kind = rows <= FEW ? 0 : rows <= 64 ? 1 : 2;
+  p.keys = p.kind == 0 ? 512 : p.kind == 1 ? 256 : rows <= 256 ? 2048 : 0;
+  p.splits = p.keys && max_len > p.keys ? (max_len + p.keys - 1) / p.keys : 1;
+  return p;
 }
 
-long cross_attention_scratch_floats(DType dt, int n, int heads, int kv_heads, int d, int n_q, int max_len) { return 0; }
+// Scratch of a split call: per (image, K/V head, row, split) d floats of
+// sum p v, then behind all of them (m, l): p = exp2(score - m), l = sum p.
+struct Scratch {
+  float *o, *ml;
+};
+__device__ __forceinline__ Scratch scratch_at(const CrossArgs& a, int img, int g, int row, int split, int splits) {
+  const long rows = (long)a.rep * a.n_q, at = (((long)img * a.kv_heads + g) * rows + row) * splits + split;
+  return {a.scratch + at * a.d, a.scratch + (long)a.n * a.kv_heads * rows * splits * a.d + 2 * at};
+}
+
+__device__ __forceinline__ float2 half_swap(float v) {  // (v of lanes l and l ^ 32)
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+#else
+  return make_float2(v, v);
+#endif
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------ few rows
+// RB rows (a power of two) per K/V head.  LPK lanes (a power of two) hold a key's
+// channels, 8 each; a wave has 64 / LPK key groups, U keys of each in flight.
+// Measured (4 images, 20 heads of 64, 9000 to 16384 keys): see launch.
+template <typename T, int RB, int LPK>
+__global__ __launch_bounds__(512) void cross_few_kernel(CrossArgs a, int keys, int splits) {
+  constexpr int U = RB <= 2 ? 4 : 2, NG = 64 / LPK, NW = 8, STEP = NW * NG * U;
+  const Place p = place_of(a.kv_heads, 1, splits, a.n);
+  if (!p.on) return;
+  const Text tx = text_of(a, p.img);
+  const int k_begin = p.split * keys, k_end = splits > 1 ? min(tx.len, k_begin + keys) : tx.len;
+  if (splits > 1 && k_begin >= tx.len) return;  // (the join knows the text's length)
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ch = (lane % LPK) * 8, grp = lane / LPK;
+  const int rows = a.rep * a.n_q;
+  const bool has = ch < a.d;
+  const T* K = (const T*)a.k + tx.k0 + p.g * a.k_head + ch;
+  const T* V = (const T*)a.v + tx.v0 + p.g * a.v_head + ch;
+  const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
+
+  float q[RB][8], o[RB][8], m[RB], l[RB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[r][e] = o[r][e] = 0.f;
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+    if (r < rows && has) {
+      const int t = r / a.rep, h = p.g * a.rep + r % a.rep;
+      load8f((const T*)a.q + (long)p.img * a.q_img + t * a.q_ld + h * a.q_head + ch, q[r]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q[r][e] *= a.scale * LOG2E;
+    }
+  }
+  // key u of this lane group in the step from k on
+  auto key_of = [&](int k, int u) { return k + (u * NW + wave) * NG + grp; };
+  auto part = [&](int key) { return key < k_end && (!mask || mask[key]); };
+  bool on[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) on[u] = part(key_of(k_begin, u));
+  for (int k = k_begin; k < k_end; k += STEP) {
+    float kf[U][8], vf[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) kf[u][e] = vf[u][e] = 0.f;
+      const long key = key_of(k, u);
+      if (on[u] && has) {
+        load8f(K + key * a.k_ld, kf[u]);
+        load8f(V + key * a.v_ld, vf[u]);
+      }
+    }
+    bool next[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = part(key_of(k + STEP, u));
+    float s[RB][U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        float d = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d = fmaf(q[r][e], kf[u][e], d);
+#pragma unroll
+        for (int x = 1; x < LPK; x <<= 1) d += __shfl_xor(d, x, 64);
+        s[r][u] = on[u] ? d : -INFINITY;
+      }
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      float mn = m[r];
+#pragma unroll
+      for (int u = 0; u < U; ++u) mn = fmaxf(mn, s[r][u]);
+      const float ref = mn == -INFINITY ? 0.f : mn;  // (no key yet: every p is 0)
+      const float al = __builtin_amdgcn_exp2f(m[r] - ref);
+      m[r] = mn;
+      l[r] *= al;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[r][e] *= al;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float pr = __builtin_amdgcn_exp2f(s[r][u] - ref);
+        l[r] += pr;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[r][e] = fmaf(pr, vf[u][e], o[r][e]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) on[u] = next[u];
+  }
+  // Join the key groups of the wave, then the waves through LDS, in order.
+  __shared__ float so[NW][RB][LPK * 8], sm[NW][RB], sl[NW][RB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    float mw = m[r];
+#pragma unroll
+    for (int x = LPK; x < 64; x <<= 1) mw = fmaxf(mw, __shfl_xor(mw, x, 64));
+    const float f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[r] - mw);
+    float lw = l[r] * f;
+#pragma unroll
+    for (int x = LPK; x < 64; x <<= 1) lw += __shfl_xor(lw, x, 64);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float v = o[r][e] * f;
+#pragma unroll
+      for (int x = LPK; x < 64; x <<= 1) v += __shfl_xor(v, x, 64);
+      if (grp == 0) so[wave][r][ch + e] = v;
+    }
+    if (lane == 0) {
+      sm[wave][r] = mw;
+      sl[wave][r] = lw;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * a.d; i += 64 * NW) {
+    const int r = i / a.d, c = i - r * a.d;
+    float mt = sm[0][r];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) mt = fmaxf(mt, sm[w][r]);
+    float v = 0.f, lt = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = sm[w][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][r] - mt);
+      v = fmaf(f, so[w][r][c], v);
+      lt = fmaf(f, sl[w][r], lt);
+    }
+    if (splits > 1) {
+      const Scratch sc = scratch_at(a, p.img, p.g, r, p.split, splits);
+      sc.o[c] = v;
+      if (c == 0) {
+        sc.ml[0] = mt;
+        sc.ml[1] = lt;
+      }
+    } else {
+      const int t = r / a.rep, h = p.g * a.rep + r % a.rep;
+      ((T*)a.o)[(long)p.img * a.o_img + t * a.o_ld + h * a.o_head + c] = from_f<T>(lt == 0.f ? 0.f : v * (1.0f / lt));
+    }
+  }
+}
+
+// ------------------------------------------------------------------ join
+// One wave per row: the splits of its text in order.
+template <typename T>
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a, int keys, int splits) {
+  const int lane = threadIdx.x & 63;
+  const long rows = (long)a.rep * a.n_q, e = blockIdx.x * 4L + (threadIdx.x >> 6);
+  if (e >= (long)a.n * a.kv_heads * rows) return;
+  const int r = (int)(e % rows), g = (int)(e / rows % a.kv_heads), img = (int)(e / rows / a.kv_heads);
+  const int ns = (text_of(a, img).len + keys - 1) / keys;
+  const Scratch sc = scratch_at(a, img, g, r, 0, splits);
+  float mt = -INFINITY;
+  for (int s = lane; s < ns; s += 64) mt = fmaxf(mt, sc.ml[2 * s]);
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) mt = fmaxf(mt, __shfl_xor(mt, x, 64));
+  float v[4] = {0.f, 0.f, 0.f, 0.f}, lt = 0.f;
+  for (int s = 0; s < ns; ++s) {
+    const float f = sc.ml[2 * s] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sc.ml[2 * s] - mt);
+    lt = fmaf(f, sc.ml[2 * s + 1], lt);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (lane + 64 * i < a.d) v[i] = fmaf(f, sc.o[(long)s * a.d + lane + 64 * i], v[i]);
+  }
+  const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+  T* o = (T*)a.o + (long)img * a.o_img + (r / a.rep) * a.o_ld + (g * a.rep + r % a.rep) * a.o_head;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (lane + 64 * i < a.d) o[lane + 64 * i] = from_f<T>(v[i] * inv);
+}
+
+// ------------------------------------------------------------------ many rows, bf16
+namespace {
+
+constexpr int KT = 64;  // keys per tile
+
+// LDS row of V: a multiple of 16 channels whose four rows a transposing read
+// takes lie in different banks (an odd number of 32-byte units, or a row that
+// fills a multiple of 64 but not of 128 or 256 bytes).
+__host__ __device__ constexpr int v_row(int d16) { return d16 * 2 % 128 == 0 ? d16 + 16 : d16; }
+
+// Four keys (LDS rows) of one channel for each lane of a group of 16: lane i
+// names the 8 bytes of row i / 4, channels 4 (i % 4) on, and gets channel i of rows 0 to 3.
+__device__ __forceinline__ bf16x4 read_transposed(const bf16* p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+#else
+  return *(const bf16x4*)p;
+#endif
+}
+
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+
+}  // namespace
+
+// D16: head width rounded up to a width the kernel is built for.  SF: d < D16, so that channel d
+// of V in LDS is free: it holds ones, and row d of O^T becomes the sum of the
+// (rounded) probabilities.  NW waves of QG groups of 32 rows.
+template <int D16, bool SF, int NW, int QG>
+__global__ __launch_bounds__(64 * NW, NW == 1 || D16 > 96 ? 1 : 2) void cross_bf16_kernel(CrossArgs a, int keys, int tiles, int splits) {
+  constexpr int NJ = D16 / 16, ND = (D16 + 31) / 32, NT = 64 * NW, LDK = D16 + 8, LDV = v_row(D16);
+  constexpr int CH = KT * (D16 / 8), CPT = (CH + NT - 1) / NT;  // 16-byte pieces of K (and of V) per tile, per thread
+  __shared__ __attribute__((aligned(16))) bf16 Ks[2][KT * LDK];
+  __shared__ __attribute__((aligned(16))) bf16 Vs[2][KT * LDV + 32];  // (the last rows are read past their end where D16 % 32)
+  const Place p = place_of(a.kv_heads, tiles, splits, a.n);
+  if (!p.on) return;
+  const Text tx = text_of(a, p.img);
+  const int k_begin = p.split * keys, k_end = splits > 1 ? min(tx.len, k_begin + keys) : tx.len;
+  if (splits > 1 && k_begin >= tx.len) return;  // (the join knows the text's length)
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lq = lane & 31, lh = lane >> 5;
+  const int rows = a.rep * a.n_q, r0 = p.tile * (32 * NW * QG) + wave * (32 * QG), d = a.d;
+  const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
+  // (a scale of 0 or below: uniform weights, or -q, under a positive one)
+  const float sl2 = a.scale == 0.f ? LOG2E : fabsf(a.scale) * LOG2E;
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+
+  // Q^T fragments (B operand): row r0 + 32 g + lq, channels 16 j + 8 lh + [0, 8)
+  bf16x8 qf[QG][NJ];
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    const int r = r0 + 32 * g + lq, t = r / a.rep, h = p.g * a.rep + r - t * a.rep;
+    const bf16* Q = (const bf16*)a.q + (long)p.img * a.q_img + t * a.q_ld + h * a.q_head;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int c = 16 * j + 8 * lh;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (r < rows && c < d && a.scale != 0.f) v = *(const uint4*)(Q + c);
+      v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
+      qf[g][j] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+  if constexpr (SF)  // ones in channel d of every key of both buffers
+    for (int i = tid; i < 2 * KT; i += NT) {
+      bf16x8 v = {};
+      v[0] = (bf16)1.0f;
+      *(bf16x8*)&Vs[i / KT][(i % KT) * LDV + d] = v;
+    }
+  f32x16 o[QG][ND];
+  float m_run[QG], l_run[QG];
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[g][t][r] = 0.f;
+    m_run[g] = -INFINITY;
+    l_run[g] = 0.f;
+  }
+
+  // A thread's pieces of a tile: key and channel, and their offsets (past a
+  // resource's end, as those of channels from d on, they read as zero).
+  int pk[CPT], ko[CPT], vo[CPT];
+#pragma unroll
+  for (int i = 0; i < CPT; ++i) {
+    const int idx = tid + NT * i, c = CH % NT == 0 || idx < CH ? idx % (D16 / 8) * 8 : d;
+    pk[i] = min(idx / (D16 / 8), KT - 1);
+    ko[i] = c < d ? (pk[i] * (int)a.k_ld + c) * 2 : OOB;
+    vo[i] = c < d ? (pk[i] * (int)a.v_ld + c) * 2 : OOB;
+  }
+  const bf16* K = (const bf16*)a.k + tx.k0 + p.g * a.k_head;
+  const bf16* V = (const bf16*)a.v + tx.v0 + p.g * a.v_head;
+  bf16x8 rk[CPT], rv[CPT];
+  auto fetch = [&](int k0, uint64_t bits) __attribute__((always_inline)) {
+    const int n = min(KT, k_end - k0);
+    const __amdgpu_buffer_rsrc_t kr = make_rsrc(K + (long)k0 * a.k_ld, ((n - 1) * (long)a.k_ld + d) * 2);
+    const __amdgpu_buffer_rsrc_t vr = make_rsrc(V + (long)k0 * a.v_ld, ((n - 1) * (long)a.v_ld + d) * 2);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      const bool on = (bits >> pk[i]) & 1;
+      rk[i] = buf_load16(kr, on ? ko[i] : OOB);
+      rv[i] = buf_load16(vr, on ? vo[i] : OOB);
+    }
+  };
+  auto stage = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      if (CH % NT != 0 && tid + NT * i >= CH) break;
+      const int c = (tid + NT * i) % (D16 / 8) * 8;
+      *(bf16x8*)&Ks[b][pk[i] * LDK + c] = rk[i];
+      if (!SF || c < d) *(bf16x8*)&Vs[b][pk[i] * LDV + c] = rv[i];
+    }
+  };
+  // which of the 64 keys from k0 on take part: lane's own, as loaded; then a bit per key
+  auto own_key = [&](int k0) -> bool {
+    const int k = k0 + lane;
+    return k < k_end && (!mask || mask[k]);
+  };
+
+  // NKT: 32-key halves of the tile that hold keys at all.
+  auto tile = [&](auto nkt, int b, uint64_t bits) __attribute__((always_inline)) {
+    constexpr int NKT = decltype(nkt)::value;
+    const bf16 *Kb = Ks[b], *Vb = Vs[b];
+    f32x16 s[QG][NKT];
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const bf16x8 kf = *(const bf16x8*)&Kb[(kt * 32 + lq) * LDK + 16 * j + 8 * lh];
+#pragma unroll
+        for (int g = 0; g < QG; ++g) {
+          const f32x16 zero = {};
+          s[g][kt] = mfma32(kf, qf[g][j], j ? s[g][kt] : zero);
+        }
+      }
+    // register r of half kt: key 32 kt + 8 (r / 4) + 4 lh + r % 4
+    if (bits != (NKT == 2 ? ~0ull : 0xFFFFFFFFull)) {
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) {
+        const uint32_t bm = (uint32_t)(bits >> (32 * kt)) >> (4 * lh);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!(bm >> (8 * (r >> 2) + (r & 3)) & 1)) {
+#pragma unroll
+            for (int g = 0; g < QG; ++g) s[g][kt][r] = -INFINITY;
+          }
+      }
+    }
+    float mt[QG];
+    bool any = false;
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+      float v = s[g][0][0];
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v = fmaxf(v, s[g][kt][r]);
+      const float2 h = half_swap(v);
+      mt[g] = fmaxf(h.x, h.y) * sl2;
+      any = any || mt[g] > m_run[g] + TAU;
+    }
+    if (__any(any)) {
+#pragma unroll
+      for (int g = 0; g < QG; ++g) {
+        // (where a row's maximum stays, its sums are multiplied by one)
+        const bool need = mt[g] > m_run[g] + TAU;
+        const float al = need ? __builtin_amdgcn_exp2f(m_run[g] - mt[g]) : 1.0f;
+        m_run[g] = need ? mt[g] : m_run[g];
+        l_run[g] *= al;
+#pragma unroll
+        for (int t = 0; t < ND; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[g][t][r] *= al;
+      }
+    }
+    // O^T += V^T P^T, 16 keys at a time: slot (lh, i) of slice u is key 16 u +
+    // 8 (i / 4) + 4 lh + i % 4, register 8 (u % 2) + i of half u / 2.  The
+    // probabilities are rounded to bf16 (half a step, 2^-9 of each) and
+    // summed as rounded, so that the rounding cancels where one key prevails.
+#pragma unroll
+    for (int u = 0; u < 2 * NKT; ++u) {
+      bf16x8 vf[ND];
+#pragma unroll
+      for (int t = 0; t < ND; ++t) {
+        const bf16* at = &Vb[(16 * u + 4 * lh + ((lane & 15) >> 2)) * LDV + t * 32 + (lane & 16) + 4 * (lane & 3)];
+        const bf16x4 lo = read_transposed(at), hi = read_transposed(at + 8 * LDV);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          vf[t][e] = lo[e];
+          vf[t][4 + e] = hi[e];
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < QG; ++g) {
+        bf16x8 pf;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          pf[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[g][u >> 1][8 * (u & 1) + i], sl2, -m_run[g]));
+        if constexpr (!SF)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) l_run[g] += (float)pf[i];
+#pragma unroll
+        for (int t = 0; t < ND; ++t) o[g][t] = mfma32(vf[t], pf, o[g][t]);
+      }
+    }
+  };
+
+  if (k_begin < k_end) {
+    uint64_t bits = __ballot(own_key(k_begin));
+    fetch(k_begin, bits);
+    bool nk = own_key(k_begin + KT);
+    stage(0);
+    __syncthreads();
+    for (int k0 = k_begin, b = 0; k0 < k_end; k0 += KT, b ^= 1) {
+      uint64_t next = 0;
+      const bool more = k0 + KT < k_end;
+      if (more) {
+        next = __ballot(nk);
+        fetch(k0 + KT, next);
+        nk = own_key(k0 + 2 * KT);
+      }
+      if (bits >> 32)
+        tile(std::integral_constant<int, 2>{}, b, bits);
+      else if (bits)
+        tile(std::integral_constant<int, 1>{}, b, bits);
+      if (more) stage(b ^ 1);
+      __syncthreads();
+      bits = next;
+    }
+  }
+
+  // O^T: lane holds channels 32 t + 8 (r / 4) + 4 lh + r % 4 of its row.
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    float l = l_run[g];
+    if constexpr (SF) {
+      l = 0.f;
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * t + 8 * (r >> 2) + 4 * lh + (r & 3) == d) l = o[g][t][r];
+    }
+    const float2 h = half_swap(l);
+    l = h.x + h.y;
+    const int r = r0 + 32 * g + lq;
+    if (splits > 1) {
+      if (r < rows) {
+        const Scratch sc = scratch_at(a, p.img, p.g, r, p.split, splits);
+#pragma unroll
+        for (int t = 0; t < ND; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int c = 32 * t + 8 * i + 4 * lh;
+            if (c < d) *(float4*)(sc.o + c) = make_float4(o[g][t][4 * i], o[g][t][4 * i + 1], o[g][t][4 * i + 2], o[g][t][4 * i + 3]);
+          }
+        if (lh == 0) {
+          sc.ml[0] = m_run[g];
+          sc.ml[1] = l;
+        }
+      }
+      continue;
+    }
+    // Rows are laid out in LDS (K's tiles are done with) and leave 16 bytes a lane.
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    bf16* R = &Ks[0][0] + wave * 32 * LDK;
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 32 * t + 8 * i + 4 * lh;
+        if (c < d) {
+          bf16x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = (bf16)(o[g][t][4 * i + e] * inv);
+          *(bf16x4*)(R + lq * LDK + c) = w;
+        }
+      }
+    asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
+    const int d8 = d >> 3;
+    for (int i = lane; i < 32 * d8; i += 64) {
+      const int row = i / d8, c = (i - row * d8) * 8, rr = r0 + 32 * g + row;
+      if (rr < rows) {
+        const int t = rr / a.rep, hd = p.g * a.rep + rr - t * a.rep;
+        *(bf16x8*)((bf16*)a.o + (long)p.img * a.o_img + t * a.o_ld + hd * a.o_head + c) = *(const bf16x8*)(R + row * LDK + c);
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
+// ------------------------------------------------------------------ many rows, fp32
+// The same on fp32 MFMAs (32 x 32 x 2), tiles of 32 keys, a wave per 32 rows.
+// Channels are summed in the order that makes a lane's share of them four
+// consecutive ones (half lh takes 8 i + 4 lh + [0, 4)); a key's probability
+// meets its V row straight from the register it was computed in, since the two
+// k of an MFMA are the two lane halves' keys.  Bound by the fp32 matrix rate.
+namespace {
+constexpr int FT = 32;
+__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+}  // namespace
+
+template <int D32, int NW>
+__global__ __launch_bounds__(64 * NW, D32 <= 64 ? 2 : 1) void cross_f32_kernel(CrossArgs a, int keys, int tiles, int splits) {
+  constexpr int NI = D32 / 8, ND = D32 / 32, NT = 64 * NW, LDK = D32 + 4, LDV = D32 + 8;  // (rows apart by banks)
+  constexpr int CPT = FT * (D32 / 4) / NT;
+  __shared__ __attribute__((aligned(16))) float Ks[2][FT * LDK];
+  __shared__ __attribute__((aligned(16))) float Vs[2][FT * LDV];
+  const Place p = place_of(a.kv_heads, tiles, splits, a.n);
+  if (!p.on) return;
+  const Text tx = text_of(a, p.img);
+  const int k_begin = p.split * keys, k_end = splits > 1 ? min(tx.len, k_begin + keys) : tx.len;
+  if (splits > 1 && k_begin >= tx.len) return;  // (the join knows the text's length)
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lq = lane & 31, lh = lane >> 5;
+  const int rows = a.rep * a.n_q, r = p.tile * (32 * NW) + wave * 32 + lq, d = a.d;
+  const int t_q = r / a.rep, h_q = p.g * a.rep + r - t_q * a.rep;
+  const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
+  const float qs = a.scale * LOG2E;
+
+  f32x4 qf[NI];
+  {
+    const float* Q = (const float*)a.q + (long)p.img * a.q_img + t_q * a.q_ld + h_q * a.q_head;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int c = 8 * i + 4 * lh;
+      qf[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (r < rows && c < d) qf[i] = *(const f32x4*)(Q + c) * qs;
+    }
+  }
+  f32x16 o[ND];
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+  float m_run = -INFINITY, l = 0.f;
+
+  const float* K = (const float*)a.k + tx.k0 + p.g * a.k_head;
+  const float* V = (const float*)a.v + tx.v0 + p.g * a.v_head;
+  uint4 rk[CPT], rv[CPT];
+  auto fetch = [&](int k0, uint32_t bits) __attribute__((always_inline)) {
+    const int n = min(FT, k_end - k0);
+    const __amdgpu_buffer_rsrc_t kr = make_rsrc(K + (long)k0 * a.k_ld, ((n - 1) * (long)a.k_ld + d) * 4);
+    const __amdgpu_buffer_rsrc_t vr = make_rsrc(V + (long)k0 * a.v_ld, ((n - 1) * (long)a.v_ld + d) * 4);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      const int idx = tid + NT * i, key = idx / (D32 / 4), c = idx % (D32 / 4) * 4;
+      const bool on = (bits >> key & 1) && c < d;
+      rk[i] = __builtin_bit_cast(uint4, buf_load16(kr, on ? (key * (int)a.k_ld + c) * 4 : OOB));
+      rv[i] = __builtin_bit_cast(uint4, buf_load16(vr, on ? (key * (int)a.v_ld + c) * 4 : OOB));
+    }
+  };
+  auto stage = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      const int idx = tid + NT * i, key = idx / (D32 / 4), c = idx % (D32 / 4) * 4;
+      *(uint4*)&Ks[b][key * LDK + c] = rk[i];
+      *(uint4*)&Vs[b][key * LDV + c] = rv[i];
+    }
+  };
+  auto own_key = [&](int k0) -> bool {
+    const int k = k0 + lq;
+    return k < k_end && (!mask || mask[k]);
+  };
+  if (k_begin < k_end) {
+    uint32_t bits = (uint32_t)__ballot(own_key(k_begin));
+    fetch(k_begin, bits);
+    bool nk = own_key(k_begin + FT);
+    stage(0);
+    __syncthreads();
+    for (int k0 = k_begin, b = 0; k0 < k_end; k0 += FT, b ^= 1) {
+      uint32_t next = 0;
+      const bool more = k0 + FT < k_end;
+      if (more) {
+        next = (uint32_t)__ballot(nk);
+        fetch(k0 + FT, next);
+        nk = own_key(k0 + 2 * FT);
+      }
+      if (bits) {
+        f32x16 s = {};
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          if (8 * i >= d) break;
+          const f32x4 kf = *(const f32x4*)&Ks[b][lq * LDK + 8 * i + 4 * lh];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s = mfma_f32(kf[e], qf[i][e], s);
+        }
+        // register i: key 8 (i / 4) + 4 lh + i % 4
+        if (bits != ~0u) {
+          const uint32_t bm = bits >> (4 * lh);
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!(bm >> (8 * (i >> 2) + (i & 3)) & 1)) s[i] = -INFINITY;
+        }
+        float v = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) v = fmaxf(v, s[i]);
+        const float2 hv = half_swap(v);
+        const float mt = fmaxf(hv.x, hv.y);
+        const bool need = mt > m_run + TAU;
+        if (__any(need)) {
+          const float al = need ? __builtin_amdgcn_exp2f(m_run - mt) : 1.0f;
+          m_run = need ? mt : m_run;
+          l *= al;
+#pragma unroll
+          for (int t = 0; t < ND; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] *= al;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float pr = __builtin_amdgcn_exp2f(s[i] - m_run);
+          l += pr;
+          const float* vr = &Vs[b][(8 * (i >> 2) + 4 * lh + (i & 3)) * LDV + lq];
+#pragma unroll
+          for (int t = 0; t < ND; ++t) o[t] = mfma_f32(vr[32 * t], pr, o[t]);
+        }
+      }
+      if (more) stage(b ^ 1);
+      __syncthreads();
+      bits = next;
+    }
+  }
+  const float2 hl = half_swap(l);
+  l = hl.x + hl.y;
+  if (r >= rows) return;
+  float* out = (float*)a.o + (long)p.img * a.o_img + t_q * a.o_ld + h_q * a.o_head;
+  float f = l == 0.f ? 0.f : 1.0f / l;
+  if (splits > 1) {
+    const Scratch sc = scratch_at(a, p.img, p.g, r, p.split, splits);
+    if (lh == 0) {
+      sc.ml[0] = m_run;
+      sc.ml[1] = l;
+    }
+    out = sc.o;
+    f = 1.0f;
+  }
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = 32 * t + 8 * i + 4 * lh;
+      if (c < d) *(float4*)(out + c) = make_float4(o[t][4 * i] * f, o[t][4 * i + 1] * f, o[t][4 * i + 2] * f, o[t][4 * i + 3] * f);
+    }
+}
+
+// ------------------------------------------------------------------ launch
+template <typename T, int RB>
+static void launch_few(const CrossArgs& a, const Plan& p, hipStream_t s) {
+  const unsigned grid = (unsigned)place_blocks(a.kv_heads, 1, p.splits, a.n);
+  if (a.d <= 32)
+    cross_few_kernel<T, RB, 4><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
+  else if (a.d <= 64)
+    cross_few_kernel<T, RB, 8><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
+  else if (a.d <= 128)
+    cross_few_kernel<T, RB, 16><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
+  else
+    cross_few_kernel<T, RB, 32><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
+}
+
+template <typename T>
+static void launch_few_rows(const CrossArgs& a, const Plan& p, hipStream_t s) {
+  const int rows = a.rep * a.n_q;
+  if (rows == 1) launch_few<T, 1>(a, p, s);
+  else if (rows == 2) launch_few<T, 2>(a, p, s);
+  else if (rows <= 4) launch_few<T, 4>(a, p, s);
+  else launch_few<T, 8>(a, p, s);
+}
+
+template <int D16, bool SF, int NW, int QG>
+static void launch_bf16(const CrossArgs& a, const Plan& p, hipStream_t s) {
+  const long rows = (long)a.rep * a.n_q;
+  const int tiles = (int)((rows + 32 * NW * QG - 1) / (32 * NW * QG));
+  cross_bf16_kernel<D16, SF, NW, QG><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits);
+}
+
+template <int D16, bool SF>
+static void launch_sum(const CrossArgs& a, const Plan& p, hipStream_t s) {
+  if (p.kind == 1) {
+    launch_bf16<D16, SF, 1, 1>(a, p, s);
+    return;
+  }
+  if constexpr (D16 <= 64)
+    if ((long)a.rep * a.n_q > 128) {
+      launch_bf16<D16, SF, 4, 2>(a, p, s);
+      return;
+    }
+  launch_bf16<D16, SF, 4, 1>(a, p, s);
+}
+
+template <int D16>
+static void launch_width(const CrossArgs& a, const Plan& p, hipStream_t s) {
+  if (a.d < D16)
+    launch_sum<D16, true>(a, p, s);
+  else
+    launch_sum<D16, false>(a, p, s);
+}
+
+template <int D32>
+static void launch_f32(const CrossArgs& a, const Plan& p, hipStream_t s) {
+  const long rows = (long)a.rep * a.n_q;
+  if (p.kind == 1) {
+    const int tiles = (int)((rows + 31) / 32);
+    cross_f32_kernel<D32, 1><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 64, 0, s>>>(a, p.keys, tiles, p.splits);
+  } else {
+    const int tiles = (int)((rows + 127) / 128);
+    cross_f32_kernel<D32, 4><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 256, 0, s>>>(a, p.keys, tiles, p.splits);
+  }
+}
+
+long cross_attention_scratch_floats(DType dt, int n, int heads, int kv_heads, int d, int n_q, int max_len) {
+  const Plan p = plan_of(heads / kv_heads, n_q, max_len);
+  const double rows = (double)heads * n_q * n;
+  if (rows * p.splits > 2.0e9 || (double)heads / kv_heads * n_q > 2.0e9) return -1;  // (grids and row indices are 32 bits)
+  return p.splits > 1 ? (long)rows * p.splits * (d + 2) : 0;
+}
 
 hipError_t launch_cross_attention(DType dt, const CrossArgs& a, hipStream_t s) {
-  const long waves = (long)a.n * a.n_q * a.heads;
-  if (waves <= 0) return hipSuccess;
-  if (waves > 0x7FFFFFFFL) return hipErrorInvalidValue;
-  const unsigned blocks = (unsigned)((waves + 3) / 4);
-  if (dt == BF16)
-    cross_simple_kernel<bf16><<<blocks, 256, 0, s>>>(a);
-  else
-    cross_simple_kernel<float><<<blocks, 256, 0, s>>>(a);
+  const long rows = (long)a.rep * a.n_q;
+  if (a.n <= 0 || rows <= 0) return hipSuccess;
+  const Plan p = plan_of(a.rep, a.n_q, a.max_len);
+  if (p.splits > 1 && !a.scratch) return hipErrorInvalidValue;
+  if (p.kind == 0) {
+    if (dt == BF16)
+      launch_few_rows<bf16>(a, p, s);
+    else
+      launch_few_rows<float>(a, p, s);
+  } else if (dt == BF16) {
+    if (a.d <= 32) launch_width<32>(a, p, s);
+    else if (a.d <= 48) launch_width<48>(a, p, s);
+    else if (a.d <= 64) launch_width<64>(a, p, s);
+    else if (a.d <= 80) launch_width<80>(a, p, s);
+    else if (a.d <= 96) launch_width<96>(a, p, s);
+    else if (a.d <= 128) launch_width<128>(a, p, s);
+    else if (a.d <= 160) launch_width<160>(a, p, s);
+    else if (a.d <= 192) launch_width<192>(a, p, s);
+    else launch_width<256>(a, p, s);
+  } else {
+    if (a.d <= 32) launch_f32<32>(a, p, s);
+    else if (a.d <= 64) launch_f32<64>(a, p, s);
+    else if (a.d <= 96) launch_f32<96>(a, p, s);
+    else if (a.d <= 128) launch_f32<128>(a, p, s);
+    else if (a.d <= 160) launch_f32<160>(a, p, s);
+    else if (a.d <= 192) launch_f32<192>(a, p, s);
+    else launch_f32<256>(a, p, s);
+  }
+  if (p.splits > 1) {
+    const unsigned grid = (unsigned)((a.n * a.kv_heads * rows + 3) / 4);
+    if (dt == BF16)
+      cross_join_kernel<bf16><<<grid, 256, 0, s>>>(a, p.keys, p.splits);
+    else
+      cross_join_kernel<float><<<grid, 256, 0, s>>>(a, p.keys, p.splits);
+  }
   return hipGetLastError();
 }
 

@@ -88,7 +88,8 @@ XA = dict(dtype=BF16, q=A[0], q_ld=128, q_head=64, q_img=1280, k=A[1], k_ld=128,
 @pytest.mark.parametrize("over,status,word", [
     (dict(), 0, ""), (dict(n=0, n_q=5), 0, ""),
     (dict(dtype=2), -1, "dtype"), (dict(heads=3), -1, "shape"), (dict(d=60), -1, "shape"), (dict(d=0), -1, "shape"),
-    (dict(d=264), -2, "shape"), (dict(n=-1), -1, "shape"), (dict(n_q=-1), -1, "shape"), (dict(max_len=-1), -1, "shape"),
+    (dict(d=264), -2, "shape"), (dict(heads=1 << 17), -2, "2^16"), (dict(max_len=(1 << 30) + 1), -2, "2^30"),
+    (dict(k_ld=(1 << 23) + 8), -2, "2^23"), (dict(n_q=1 << 30), -2, "too many"), (dict(n=-1), -1, "shape"), (dict(n_q=-1), -1, "shape"), (dict(max_len=-1), -1, "shape"),
     (dict(kv_heads=0), -1, "shape"), (dict(n_ctx=-1), -1, "context"), (dict(kv_tokens=-1), -1, "context"),
     (dict(kv_tokens=1 << 31), -1, "context"), (dict(n_ctx=2), -1, "fewer contexts"),
     (dict(scale=float("nan")), -1, "scale"), (dict(scale=float("inf")), -1, "scale"),
