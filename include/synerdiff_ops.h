@@ -245,7 +245,7 @@ sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* d_x, int64_t x
  * kv_len past max_len counts as max_len, a negative one as 0.  Strides in
  * elements, not negative (0 for a shared head).
  * Constraints: d a multiple of 8, <= 256; heads a multiple of kv_heads, <=
- * 2^16; max_len <= 2^30; k_ld, v_ld <= 2^23; n * n_q * heads (times the
+ * 2^16; max_len <= 2^30; q_ld, k_ld, v_ld, o_ld <= 2^23; n * n_q * heads (times the
  * splits) <= 2 * 10^9; q, k, v, o and all their strides at multiples of 16
  * bytes.  o overlaps nothing.  Few queries over long texts are split along the keys: d_scratch
  * (fp32, 16-byte aligned) has to hold synerdiff_op_cross_attention_scratch_floats(...) floats

@@ -107,6 +107,16 @@ __device__ __forceinline__ Scratch scratch_at(const CrossArgs& a, int img, int g
   return {a.scratch + at * a.d, a.scratch + (long)a.n * a.kv_heads * rows * splits * a.d + 2 * at};
 }
 
+// Row r of a K/V head: its query, and its head among the rep that share.
+struct RowAt {
+  int t, h;
+};
+__device__ __forceinline__ RowAt row_at(const CrossArgs& a, int r) {
+  if (a.rep == 1) return {r, 0};
+  const int t = (int)(__umulhi((unsigned)r, a.rep_mul) >> a.rep_shift);
+  return {t, r - t * a.rep};
+}
+
 __device__ __forceinline__ float2 half_swap(float v) {  // (v of lanes l and l ^ 32)
 #if defined(__HIP_DEVICE_COMPILE__)
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -316,42 +326,68 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 
 }  // namespace
 
-// D16: head width rounded up to a width the kernel is built for.  SF: d < D16, so that channel d
-// of V in LDS is free: it holds ones, and row d of O^T becomes the sum of the
-// (rounded) probabilities.  NW waves of QG groups of 32 rows.
-template <int D16, bool SF, int NW, int QG>
-__global__ __launch_bounds__(64 * NW, NW == 1 || D16 > 96 ? 1 : 2) void cross_bf16_kernel(CrossArgs a, int keys, int tiles, int splits) {
+// D16: head width rounded up to a width the kernel is built for.  SF: d < D16,
+// so that channel d of V in LDS is free: it holds ones, and row d of O^T
+// becomes the sum of the (rounded) probabilities.  NW waves of QG groups of 32
+// rows.  SHORT: no text is longer than the two tiles that LDS holds; they are
+// staged once, and the waves pass `passes` groups of rows each over them without
+// meeting again.  (Its arithmetic on a row is the same.)
+template <int D16, bool SF, int NW, int QG, bool SHORT>
+__global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1) : NW == 1 || D16 > 96 ? 1 : 2) void cross_bf16_kernel(
+    CrossArgs a, int keys, int tiles, int splits, int passes) {
+  static_assert(!SHORT || QG == 1, "one group at a time");
   constexpr int NJ = D16 / 16, ND = (D16 + 31) / 32, NT = 64 * NW, LDK = D16 + 8, LDV = v_row(D16);
-  constexpr int CH = KT * (D16 / 8), CPT = (CH + NT - 1) / NT;  // 16-byte pieces of K (and of V) per tile, per thread
+  // A tile is moved by passes of NT / LPR keys, LPR lanes (a power of two) a key
+  constexpr int LPR = D16 <= 32 ? 4 : D16 <= 64 ? 8 : D16 <= 128 ? 16 : 32, RPP = NT / LPR < KT ? NT / LPR : KT, CPT = KT / RPP;
   __shared__ __attribute__((aligned(16))) bf16 Ks[2][KT * LDK];
   __shared__ __attribute__((aligned(16))) bf16 Vs[2][KT * LDV + 32];  // (the last rows are read past their end where D16 % 32)
+  __shared__ __attribute__((aligned(16))) bf16 Os[SHORT ? NW * 32 * D16 : 8];
   const Place p = place_of(a.kv_heads, tiles, splits, a.n);
   if (!p.on) return;
   const Text tx = text_of(a, p.img);
   const int k_begin = p.split * keys, k_end = splits > 1 ? min(tx.len, k_begin + keys) : tx.len;
   if (splits > 1 && k_begin >= tx.len) return;  // (the join knows the text's length)
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lq = lane & 31, lh = lane >> 5;
-  const int rows = a.rep * a.n_q, r0 = p.tile * (32 * NW * QG) + wave * (32 * QG), d = a.d;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, lh = lane >> 5;
+  const int rows = a.rep * a.n_q, d = a.d;
+  int r0 = (p.tile * passes * NW + wave) * (32 * QG);  // (uniform)
   const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
   // (a scale of 0 or below: uniform weights, or -q, under a positive one)
   const float sl2 = a.scale == 0.f ? LOG2E : fabsf(a.scale) * LOG2E;
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
 
   // Q^T fragments (B operand): row r0 + 32 g + lq, channels 16 j + 8 lh + [0, 8)
-  bf16x8 qf[QG][NJ];
+  auto load_q = [&](int r0, bf16x8 (&qf)[QG][NJ]) __attribute__((always_inline)) {
 #pragma unroll
-  for (int g = 0; g < QG; ++g) {
-    const int r = r0 + 32 * g + lq, t = r / a.rep, h = p.g * a.rep + r - t * a.rep;
-    const bf16* Q = (const bf16*)a.q + (long)p.img * a.q_img + t * a.q_ld + h * a.q_head;
+    for (int g = 0; g < QG; ++g) {
+      uint4 v[NJ];
+      const int rg = r0 + 32 * g, n = a.scale == 0.f ? 0 : min(32, rows - rg);
+      if (a.rep == 1) {  // (32 rows from one address on; what lies past them, and channels from d on, read as zero)
+        const bf16* Q = (const bf16*)a.q + (long)p.img * a.q_img + (long)rg * a.q_ld + p.g * a.q_head;
+        const __amdgpu_buffer_rsrc_t qr = make_rsrc(Q, n <= 0 ? 0 : ((n - 1) * (long)a.q_ld + d) * 2);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int c = 16 * j + 8 * lh;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (r < rows && c < d && a.scale != 0.f) v = *(const uint4*)(Q + c);
-      v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
-      qf[g][j] = __builtin_bit_cast(bf16x8, v);
+        for (int j = 0; j < NJ; ++j)
+          v[j] = __builtin_bit_cast(uint4, buf_load16(qr, 16 * j + 8 * lh < d ? (lq * (int)a.q_ld + 16 * j + 8 * lh) * 2 : OOB));
+      } else {
+        const RowAt at = row_at(a, rg + lq);
+        const bf16* Q = (const bf16*)a.q + (long)p.img * a.q_img + at.t * a.q_ld + (p.g * a.rep + at.h) * a.q_head;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          v[j] = make_uint4(0, 0, 0, 0);
+          if (lq < n && 16 * j + 8 * lh < d) v[j] = *(const uint4*)(Q + 16 * j + 8 * lh);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        v[j].x ^= flip;
+        v[j].y ^= flip;
+        v[j].z ^= flip;
+        v[j].w ^= flip;
+        qf[g][j] = __builtin_bit_cast(bf16x8, v[j]);
+      }
     }
-  }
+  };
+  bf16x8 qf[QG][NJ];
+  load_q(r0, qf);
   if constexpr (SF)  // ones in channel d of every key of both buffers
     for (int i = tid; i < 2 * KT; i += NT) {
       bf16x8 v = {};
@@ -360,26 +396,24 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || D16 > 96 ? 1 : 2) void cross_bf
     }
   f32x16 o[QG][ND];
   float m_run[QG], l_run[QG];
+  auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int g = 0; g < QG; ++g) {
+    for (int g = 0; g < QG; ++g) {
 #pragma unroll
-    for (int t = 0; t < ND; ++t)
+      for (int t = 0; t < ND; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[g][t][r] = 0.f;
-    m_run[g] = -INFINITY;
-    l_run[g] = 0.f;
-  }
+        for (int r = 0; r < 16; ++r) o[g][t][r] = 0.f;
+      m_run[g] = -INFINITY;
+      l_run[g] = 0.f;
+    }
+  };
+  clear();
 
-  // A thread's pieces of a tile: key and channel, and their offsets (past a
-  // resource's end, as those of channels from d on, they read as zero).
-  int pk[CPT], ko[CPT], vo[CPT];
-#pragma unroll
-  for (int i = 0; i < CPT; ++i) {
-    const int idx = tid + NT * i, c = CH % NT == 0 || idx < CH ? idx % (D16 / 8) * 8 : d;
-    pk[i] = min(idx / (D16 / 8), KT - 1);
-    ko[i] = c < d ? (pk[i] * (int)a.k_ld + c) * 2 : OOB;
-    vo[i] = c < d ? (pk[i] * (int)a.v_ld + c) * 2 : OOB;
-  }
+  // A thread's pieces of a tile: keys pk + RPP i, channels pc on.  (Offsets past a
+  // resource's end, as those of channels from d on and of keys that take no part, read as zero.)
+  const int pk = tid / LPR, pc = tid % LPR * 8;
+  const bool mine = pk < RPP && pc < D16;  // (fewer than NT threads where LPR is wide or the tile short)
+  const int ko = pc < d ? (pk * (int)a.k_ld + pc) * 2 : OOB, vo = pc < d ? (pk * (int)a.v_ld + pc) * 2 : OOB;
   const bf16* K = (const bf16*)a.k + tx.k0 + p.g * a.k_head;
   const bf16* V = (const bf16*)a.v + tx.v0 + p.g * a.v_head;
   bf16x8 rk[CPT], rv[CPT];
@@ -387,21 +421,21 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || D16 > 96 ? 1 : 2) void cross_bf
     const int n = min(KT, k_end - k0);
     const __amdgpu_buffer_rsrc_t kr = make_rsrc(K + (long)k0 * a.k_ld, ((n - 1) * (long)a.k_ld + d) * 2);
     const __amdgpu_buffer_rsrc_t vr = make_rsrc(V + (long)k0 * a.v_ld, ((n - 1) * (long)a.v_ld + d) * 2);
+    const uint64_t b = bits >> (pk & 63);
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
-      const bool on = (bits >> pk[i]) & 1;
-      rk[i] = buf_load16(kr, on ? ko[i] : OOB);
-      rv[i] = buf_load16(vr, on ? vo[i] : OOB);
+      const bool on = (b >> (RPP * i & 63)) & 1;
+      rk[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(kr, on ? ko : OOB, i * RPP * (int)a.k_ld * 2, 0));
+      rv[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(vr, on ? vo : OOB, i * RPP * (int)a.v_ld * 2, 0));
     }
   };
   auto stage = [&](int b) __attribute__((always_inline)) {
+    if (mine)
 #pragma unroll
-    for (int i = 0; i < CPT; ++i) {
-      if (CH % NT != 0 && tid + NT * i >= CH) break;
-      const int c = (tid + NT * i) % (D16 / 8) * 8;
-      *(bf16x8*)&Ks[b][pk[i] * LDK + c] = rk[i];
-      if (!SF || c < d) *(bf16x8*)&Vs[b][pk[i] * LDV + c] = rv[i];
-    }
+      for (int i = 0; i < CPT; ++i) {
+        *(bf16x8*)&Ks[b][(pk + RPP * i) * LDK + pc] = rk[i];
+        if (!SF || pc < d) *(bf16x8*)&Vs[b][(pk + RPP * i) * LDV + pc] = rv[i];
+      }
   };
   // which of the 64 keys from k0 on take part: lane's own, as loaded; then a bit per key
   auto own_key = [&](int k0) -> bool {
@@ -476,11 +510,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || D16 > 96 ? 1 : 2) void cross_bf
       for (int t = 0; t < ND; ++t) {
         const bf16* at = &Vb[(16 * u + 4 * lh + ((lane & 15) >> 2)) * LDV + t * 32 + (lane & 16) + 4 * (lane & 3)];
         const bf16x4 lo = read_transposed(at), hi = read_transposed(at + 8 * LDV);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          vf[t][e] = lo[e];
-          vf[t][4 + e] = hi[e];
-        }
+        vf[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
 #pragma unroll
       for (int g = 0; g < QG; ++g) {
@@ -496,88 +526,131 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || D16 > 96 ? 1 : 2) void cross_bf
       }
     }
   };
-
-  if (k_begin < k_end) {
-    uint64_t bits = __ballot(own_key(k_begin));
-    fetch(k_begin, bits);
-    bool nk = own_key(k_begin + KT);
-    stage(0);
-    __syncthreads();
-    for (int k0 = k_begin, b = 0; k0 < k_end; k0 += KT, b ^= 1) {
-      uint64_t next = 0;
-      const bool more = k0 + KT < k_end;
-      if (more) {
-        next = __ballot(nk);
-        fetch(k0 + KT, next);
-        nk = own_key(k0 + 2 * KT);
-      }
-      if (bits >> 32)
-        tile(std::integral_constant<int, 2>{}, b, bits);
-      else if (bits)
-        tile(std::integral_constant<int, 1>{}, b, bits);
-      if (more) stage(b ^ 1);
-      __syncthreads();
-      bits = next;
-    }
-  }
+  auto tile_of = [&](int b, uint64_t bits) __attribute__((always_inline)) {
+    if (bits >> 32)
+      tile(std::integral_constant<int, 2>{}, b, bits);
+    else if (bits)
+      tile(std::integral_constant<int, 1>{}, b, bits);
+  };
 
   // O^T: lane holds channels 32 t + 8 (r / 4) + 4 lh + r % 4 of its row.
+  auto finish = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int g = 0; g < QG; ++g) {
-    float l = l_run[g];
-    if constexpr (SF) {
-      l = 0.f;
-#pragma unroll
-      for (int t = 0; t < ND; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (32 * t + 8 * (r >> 2) + 4 * lh + (r & 3) == d) l = o[g][t][r];
-    }
-    const float2 h = half_swap(l);
-    l = h.x + h.y;
-    const int r = r0 + 32 * g + lq;
-    if (splits > 1) {
-      if (r < rows) {
-        const Scratch sc = scratch_at(a, p.img, p.g, r, p.split, splits);
+    for (int g = 0; g < QG; ++g) {
+      float l = l_run[g];
+      if constexpr (SF) {
+        l = 0.f;
 #pragma unroll
         for (int t = 0; t < ND; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int c = 32 * t + 8 * i + 4 * lh;
-            if (c < d) *(float4*)(sc.o + c) = make_float4(o[g][t][4 * i], o[g][t][4 * i + 1], o[g][t][4 * i + 2], o[g][t][4 * i + 3]);
+          for (int r = 0; r < 16; ++r)
+            if (32 * t + 8 * (r >> 2) + 4 * lh + (r & 3) == d) l = o[g][t][r];
+      }
+      const float2 h = half_swap(l);
+      l = h.x + h.y;
+      const int r = r0 + 32 * g + lq;
+      if (!SHORT && splits > 1) {
+        if (r < rows) {
+          const Scratch sc = scratch_at(a, p.img, p.g, r, p.split, splits);
+#pragma unroll
+          for (int t = 0; t < ND; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int c = 32 * t + 8 * i + 4 * lh;
+              if (c < d) *(float4*)(sc.o + c) = make_float4(o[g][t][4 * i], o[g][t][4 * i + 1], o[g][t][4 * i + 2], o[g][t][4 * i + 3]);
+            }
+          if (lh == 0) {
+            sc.ml[0] = m_run[g];
+            sc.ml[1] = l;
           }
-        if (lh == 0) {
-          sc.ml[0] = m_run[g];
-          sc.ml[1] = l;
+        }
+        continue;
+      }
+      // Rows are laid out in LDS (K's tiles are done with, unless SHORT) and leave 16 bytes a lane.
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      constexpr int LDO = SHORT ? D16 : LDK;
+      bf16* R = (SHORT ? Os : &Ks[0][0]) + wave * 32 * LDO;
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c = 32 * t + 8 * i + 4 * lh;
+          if (c < d) {
+            bf16x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = (bf16)(o[g][t][4 * i + e] * inv);
+            *(bf16x4*)(R + lq * LDO + c) = w;
+          }
+        }
+      asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
+      const int rg = r0 + 32 * g, c = lane % LPR * 8, row0 = lane / LPR;
+      bf16* O = (bf16*)a.o + (long)p.img * a.o_img + p.g * a.rep * a.o_head + c;
+      if (c < d) {
+        if (a.rep == 1) {
+          O += (long)rg * a.o_ld;
+#pragma unroll
+          for (int i = 0; i < 32; i += 64 / LPR)
+            if (rg + row0 + i < rows) *(bf16x8*)(O + (row0 + i) * (int)a.o_ld) = *(const bf16x8*)(R + (row0 + i) * LDO + c);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; i += 64 / LPR)
+            if (rg + row0 + i < rows) {
+              const RowAt at = row_at(a, rg + row0 + i);
+              *(bf16x8*)(O + at.t * a.o_ld + at.h * a.o_head) = *(const bf16x8*)(R + (row0 + i) * LDO + c);
+            }
         }
       }
-      continue;
+      asm volatile("" ::: "memory");
     }
-    // Rows are laid out in LDS (K's tiles are done with) and leave 16 bytes a lane.
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    bf16* R = &Ks[0][0] + wave * 32 * LDK;
+  };
+
+  if constexpr (SHORT) {
+    const uint64_t b0 = __ballot(own_key(0)), b1 = __ballot(own_key(KT));
+    if (k_end > 0) fetch(0, b0);
+    stage(0);
+    if (k_end > KT) {
+      fetch(KT, b1);
+      stage(1);
+    }
+    __syncthreads();
+    for (int it = 0; it < passes; ++it) {
+      bf16x8 qn[QG][NJ];
+      const int rn = r0 + NW * 32;
+      if (it + 1 < passes && rn < rows) load_q(rn, qn);
+      if (r0 < rows) {
+        tile_of(0, b0);
+        if (k_end > KT) tile_of(1, b1);
+        finish();
+      }
+      if (it + 1 < passes) {
+        clear();
 #pragma unroll
-    for (int t = 0; t < ND; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = 32 * t + 8 * i + 4 * lh;
-        if (c < d) {
-          bf16x4 w;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = (bf16)(o[g][t][4 * i + e] * inv);
-          *(bf16x4*)(R + lq * LDK + c) = w;
+        for (int j = 0; j < NJ; ++j) qf[0][j] = qn[0][j];
+        r0 = rn;
+      }
+    }
+  } else {
+    if (k_begin < k_end) {
+      uint64_t bits = __ballot(own_key(k_begin));
+      fetch(k_begin, bits);
+      bool nk = own_key(k_begin + KT);
+      stage(0);
+      __syncthreads();
+      for (int k0 = k_begin, b = 0; k0 < k_end; k0 += KT, b ^= 1) {
+        uint64_t next = 0;
+        const bool more = k0 + KT < k_end;
+        if (more) {
+          next = __ballot(nk);
+          fetch(k0 + KT, next);
+          nk = own_key(k0 + 2 * KT);
         }
-      }
-    asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
-    const int d8 = d >> 3;
-    for (int i = lane; i < 32 * d8; i += 64) {
-      const int row = i / d8, c = (i - row * d8) * 8, rr = r0 + 32 * g + row;
-      if (rr < rows) {
-        const int t = rr / a.rep, hd = p.g * a.rep + rr - t * a.rep;
-        *(bf16x8*)((bf16*)a.o + (long)p.img * a.o_img + t * a.o_ld + hd * a.o_head + c) = *(const bf16x8*)(R + row * LDK + c);
+        tile_of(b, bits);
+        if (more) stage(b ^ 1);
+        __syncthreads();
+        bits = next;
       }
     }
-    asm volatile("" ::: "memory");
+    finish();
   }
 }
 
@@ -611,7 +684,8 @@ __global__ __launch_bounds__(64 * NW, D32 <= 64 ? 2 : 1) void cross_f32_kernel(C
   if (splits > 1 && k_begin >= tx.len) return;  // (the join knows the text's length)
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lq = lane & 31, lh = lane >> 5;
   const int rows = a.rep * a.n_q, r = p.tile * (32 * NW) + wave * 32 + lq, d = a.d;
-  const int t_q = r / a.rep, h_q = p.g * a.rep + r - t_q * a.rep;
+  const RowAt at = row_at(a, r);
+  const int t_q = at.t, h_q = p.g * a.rep + at.h;
   const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
   const float qs = a.scale * LOG2E;
 
@@ -768,17 +842,28 @@ template <int D16, bool SF, int NW, int QG>
 static void launch_bf16(const CrossArgs& a, const Plan& p, hipStream_t s) {
   const long rows = (long)a.rep * a.n_q;
   const int tiles = (int)((rows + 32 * NW * QG - 1) / (32 * NW * QG));
-  cross_bf16_kernel<D16, SF, NW, QG><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits);
+  cross_bf16_kernel<D16, SF, NW, QG, false><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits, 1);
 }
 
 template <int D16, bool SF>
 static void launch_sum(const CrossArgs& a, const Plan& p, hipStream_t s) {
+  const long rows = (long)a.rep * a.n_q;
   if (p.kind == 1) {
     launch_bf16<D16, SF, 1, 1>(a, p, s);
     return;
   }
+  if constexpr (D16 <= 160)  // (wider heads' tiles leave no LDS for the output rows)
+    if (a.max_len <= 2 * KT) {
+      constexpr int NW = 4;
+      // up to 8 groups of rows per wave, as long as some 1000 blocks remain
+      const long groups = (rows + 32 * NW - 1) / (32 * NW), all = groups * a.kv_heads * a.n;
+      const int passes = (int)(all / 1024 < 1 ? 1 : all / 1024 > 8 ? 8 : all / 1024);
+      const int tiles = (int)((groups + passes - 1) / passes);
+      cross_bf16_kernel<D16, SF, NW, 1, true><<<(unsigned)place_blocks(a.kv_heads, tiles, 1, a.n), 64 * NW, 0, s>>>(a, 0, tiles, 1, passes);
+      return;
+    }
   if constexpr (D16 <= 64)
-    if ((long)a.rep * a.n_q > 128) {
+    if (rows > 128) {
       launch_bf16<D16, SF, 4, 2>(a, p, s);
       return;
     }
@@ -812,11 +897,17 @@ long cross_attention_scratch_floats(DType dt, int n, int heads, int kv_heads, in
   return p.splits > 1 ? (long)rows * p.splits * (d + 2) : 0;
 }
 
-hipError_t launch_cross_attention(DType dt, const CrossArgs& a, hipStream_t s) {
+hipError_t launch_cross_attention(DType dt, CrossArgs a, hipStream_t s) {
   const long rows = (long)a.rep * a.n_q;
   if (a.n <= 0 || rows <= 0) return hipSuccess;
   const Plan p = plan_of(a.rep, a.n_q, a.max_len);
   if (p.splits > 1 && !a.scratch) return hipErrorInvalidValue;
+  if (a.rep > 1) {  // r = q rep + s, r < 2^31: with l = ceil(log2 rep), mul = ceil(2^(31 + l) / rep), q = r mul >> (31 + l)
+    int l = 0;
+    while ((1u << l) < (unsigned)a.rep) ++l;
+    a.rep_mul = (unsigned)(((1ull << (31 + l)) + a.rep - 1) / a.rep);
+    a.rep_shift = l - 1;
+  }
   if (p.kind == 0) {
     if (dt == BF16)
       launch_few_rows<bf16>(a, p, s);

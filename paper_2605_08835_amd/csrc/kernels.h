@@ -222,10 +222,11 @@ struct CrossArgs {
   const uint8_t* mask;  // or null
   void* o; long o_ld, o_head, o_img;
   int n, heads, kv_heads, rep, d, n_q;
+  unsigned rep_mul, rep_shift;  // r / rep = umulhi(r, rep_mul) >> rep_shift, r < 2^31 (rep > 1): set by the launcher
   float scale;
   float* scratch;
 };
-hipError_t launch_cross_attention(DType dt, const CrossArgs& a, hipStream_t s);
+hipError_t launch_cross_attention(DType dt, CrossArgs a, hipStream_t s);
 long cross_attention_scratch_floats(DType dt, int n, int heads, int kv_heads, int d, int n_q, int max_len);
 
 }  // namespace sd

@@ -377,8 +377,8 @@ sd_status synerdiff_op_cross_attention(int32_t dtype, const void* q, int64_t q_l
   if (bad_dtype(dtype)) return op_fail(SD_ERR_INVALID_ARG, "bad dtype");
   if (!cross_shape_ok(dtype, n, heads, kv_heads, d, n_q, max_len))
     return op_fail(d > 256 ? SD_ERR_UNSUPPORTED : SD_ERR_INVALID_ARG, "bad shape (d a multiple of 8 up to 256, heads of kv_heads)");
-  if (heads > 1 << 16 || max_len > 1 << 30 || k_ld > 1 << 23 || v_ld > 1 << 23)
-    return op_fail(SD_ERR_UNSUPPORTED, "more than 2^16 heads, 2^30 keys or 2^23 elements from key to key");
+  if (heads > 1 << 16 || max_len > 1 << 30 || q_ld > 1 << 23 || k_ld > 1 << 23 || v_ld > 1 << 23 || o_ld > 1 << 23)
+    return op_fail(SD_ERR_UNSUPPORTED, "more than 2^16 heads, 2^30 keys or 2^23 elements from token to token");
   if (n_ctx < 0 || kv_tokens < 0 || kv_tokens > 0x7FFFFFFF) return op_fail(SD_ERR_INVALID_ARG, "bad context count or length");
   if (!kv_index && n_ctx < n) return op_fail(SD_ERR_INVALID_ARG, "fewer contexts than rows");
   if (!(scale == scale) || scale - scale != 0.f) return op_fail(SD_ERR_INVALID_ARG, "scale must be finite");
