@@ -92,7 +92,7 @@ static Plan plan_of(int rep, int n_q, int max_len) {
   const long rows = (long)rep * n_q;
   Plan p;
   p.kind = rows <= FEW ? 0 : rows <= 64 ? 1 : 2;
-  p.keys = p.kind == 0 ? 512 : p.kind == 1 ? 256 : rows <= 256 ? 2048 : 0;
+  p.keys = p.kind <= 1 ? 512 : rows <= 256 ? 2048 : 0;
   p.splits = p.keys && max_len > p.keys ? (max_len + p.keys - 1) / p.keys : 1;
   return p;
 }
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
   constexpr int LPR = D16 <= 32 ? 4 : D16 <= 64 ? 8 : D16 <= 128 ? 16 : 32, RPP = NT / LPR < KT ? NT / LPR : KT, CPT = KT / RPP;
   __shared__ __attribute__((aligned(16))) bf16 Ks[2][KT * LDK];
   __shared__ __attribute__((aligned(16))) bf16 Vs[2][KT * LDV + 32];  // (the last rows are read past their end where D16 % 32)
-  __shared__ __attribute__((aligned(16))) bf16 Os[SHORT ? NW * 32 * D16 : 8];
+  __shared__ __attribute__((aligned(16))) bf16 Os[SHORT ? NW * 32 * LDK : 8];
   const Place p = place_of(a.kv_heads, tiles, splits, a.n);
   if (!p.on) return;
   const Text tx = text_of(a, p.img);
@@ -394,7 +394,7 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
       v[0] = (bf16)1.0f;
       *(bf16x8*)&Vs[i / KT][(i % KT) * LDV + d] = v;
     }
-  f32x16 o[QG][ND];
+  f32x16 o[QG][ND];  // (set by the first tile that holds a key)
   float m_run[QG], l_run[QG];
   auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -407,7 +407,6 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
       l_run[g] = 0.f;
     }
   };
-  clear();
 
   // A thread's pieces of a tile: keys pk + RPP i, channels pc on.  (Offsets past a
   // resource's end, as those of channels from d on and of keys that take no part, read as zero.)
@@ -443,35 +442,33 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
     return k < k_end && (!mask || mask[k]);
   };
 
-  // NKT: 32-key halves of the tile that hold keys at all.
-  auto tile = [&](auto nkt, int b, uint64_t bits) __attribute__((always_inline)) {
+  bf16x8 ones = {};  // B operand of the masks: ones for k = 0
+  if (lh == 0) ones[0] = (bf16)1.0f;
+
+  // NKT: 32-key halves of the tile that hold keys at all.  FIRST: nothing has
+  // been summed yet.
+  auto tile = [&](auto nkt, auto first, int b, uint64_t bits) __attribute__((always_inline)) {
     constexpr int NKT = decltype(nkt)::value;
+    constexpr bool FIRST = decltype(first)::value;
     const bf16 *Kb = Ks[b], *Vb = Vs[b];
     f32x16 s[QG][NKT];
 #pragma unroll
-    for (int kt = 0; kt < NKT; ++kt)
+    for (int kt = 0; kt < NKT; ++kt) {
+      // Keys that take no part start from -inf: one product of a column of 0
+      // or -inf per key with a row of ones (a select per score cost three
+      // vector instructions each, and the vector ALU bounds this kernel).
+      const f32x16 zero = {};
+      bf16x8 off = {};
+      if (lh == 0) off[0] = __builtin_bit_cast(bf16, (unsigned short)(bits >> (32 * kt + lq) & 1 ? 0 : 0xFF80));
+      const f32x16 start = mfma32(off, ones, zero);
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         const bf16x8 kf = *(const bf16x8*)&Kb[(kt * 32 + lq) * LDK + 16 * j + 8 * lh];
 #pragma unroll
-        for (int g = 0; g < QG; ++g) {
-          const f32x16 zero = {};
-          s[g][kt] = mfma32(kf, qf[g][j], j ? s[g][kt] : zero);
-        }
-      }
-    // register r of half kt: key 32 kt + 8 (r / 4) + 4 lh + r % 4
-    if (bits != (NKT == 2 ? ~0ull : 0xFFFFFFFFull)) {
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        const uint32_t bm = (uint32_t)(bits >> (32 * kt)) >> (4 * lh);
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!(bm >> (8 * (r >> 2) + (r & 3)) & 1)) {
-#pragma unroll
-            for (int g = 0; g < QG; ++g) s[g][kt][r] = -INFINITY;
-          }
+        for (int g = 0; g < QG; ++g) s[g][kt] = mfma32(kf, qf[g][j], j ? s[g][kt] : start);
       }
     }
+    // register r of half kt: key 32 kt + 8 (r / 4) + 4 lh + r % 4
     float mt[QG];
     bool any = false;
 #pragma unroll
@@ -483,9 +480,12 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
         for (int r = 0; r < 16; ++r) v = fmaxf(v, s[g][kt][r]);
       const float2 h = half_swap(v);
       mt[g] = fmaxf(h.x, h.y) * sl2;
-      any = any || mt[g] > m_run[g] + TAU;
+      if constexpr (FIRST)
+        m_run[g] = mt[g];
+      else
+        any = any || mt[g] > m_run[g] + TAU;
     }
-    if (__any(any)) {
+    if (!FIRST && __any(any)) {
 #pragma unroll
       for (int g = 0; g < QG; ++g) {
         // (where a row's maximum stays, its sums are multiplied by one)
@@ -520,21 +520,27 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
           pf[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[g][u >> 1][8 * (u & 1) + i], sl2, -m_run[g]));
         if constexpr (!SF)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) l_run[g] += (float)pf[i];
+          for (int i = 0; i < 8; ++i) l_run[g] = FIRST && u == 0 && i == 0 ? (float)pf[i] : l_run[g] + (float)pf[i];
 #pragma unroll
-        for (int t = 0; t < ND; ++t) o[g][t] = mfma32(vf[t], pf, o[g][t]);
+        for (int t = 0; t < ND; ++t) {
+          const f32x16 zero = {};
+          o[g][t] = mfma32(vf[t], pf, FIRST && u == 0 ? zero : o[g][t]);
+        }
       }
     }
   };
-  auto tile_of = [&](int b, uint64_t bits) __attribute__((always_inline)) {
+  bool any_key = false;  // (uniform)
+  auto tile_of = [&](auto first, int b, uint64_t bits) __attribute__((always_inline)) {
     if (bits >> 32)
-      tile(std::integral_constant<int, 2>{}, b, bits);
+      tile(std::integral_constant<int, 2>{}, first, b, bits);
     else if (bits)
-      tile(std::integral_constant<int, 1>{}, b, bits);
+      tile(std::integral_constant<int, 1>{}, first, b, bits);
+    any_key = any_key || bits;
   };
 
   // O^T: lane holds channels 32 t + 8 (r / 4) + 4 lh + r % 4 of its row.
   auto finish = [&]() __attribute__((always_inline)) {
+    if (!any_key) clear();
 #pragma unroll
     for (int g = 0; g < QG; ++g) {
       float l = l_run[g];
@@ -568,8 +574,7 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
       }
       // Rows are laid out in LDS (K's tiles are done with, unless SHORT) and leave 16 bytes a lane.
       const float inv = l == 0.f ? 0.f : 1.0f / l;
-      constexpr int LDO = SHORT ? D16 : LDK;
-      bf16* R = (SHORT ? Os : &Ks[0][0]) + wave * 32 * LDO;
+      bf16* R = (SHORT ? Os : &Ks[0][0]) + wave * 32 * LDK;
 #pragma unroll
       for (int t = 0; t < ND; ++t)
 #pragma unroll
@@ -579,7 +584,7 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
             bf16x4 w;
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] = (bf16)(o[g][t][4 * i + e] * inv);
-            *(bf16x4*)(R + lq * LDO + c) = w;
+            *(bf16x4*)(R + lq * LDK + c) = w;
           }
         }
       asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
@@ -590,13 +595,13 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
           O += (long)rg * a.o_ld;
 #pragma unroll
           for (int i = 0; i < 32; i += 64 / LPR)
-            if (rg + row0 + i < rows) *(bf16x8*)(O + (row0 + i) * (int)a.o_ld) = *(const bf16x8*)(R + (row0 + i) * LDO + c);
+            if (rg + row0 + i < rows) *(bf16x8*)(O + (row0 + i) * (int)a.o_ld) = *(const bf16x8*)(R + (row0 + i) * LDK + c);
         } else {
 #pragma unroll
           for (int i = 0; i < 32; i += 64 / LPR)
             if (rg + row0 + i < rows) {
               const RowAt at = row_at(a, rg + row0 + i);
-              *(bf16x8*)(O + at.t * a.o_ld + at.h * a.o_head) = *(const bf16x8*)(R + (row0 + i) * LDO + c);
+              *(bf16x8*)(O + at.t * a.o_ld + at.h * a.o_head) = *(const bf16x8*)(R + (row0 + i) * LDK + c);
             }
         }
       }
@@ -618,12 +623,12 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
       const int rn = r0 + NW * 32;
       if (it + 1 < passes && rn < rows) load_q(rn, qn);
       if (r0 < rows) {
-        tile_of(0, b0);
-        if (k_end > KT) tile_of(1, b1);
+        const int bf = b0 ? 0 : 1;  // (the first tile that holds a key)
+        tile_of(std::true_type{}, bf, b0 ? b0 : b1);
+        if (b0) tile_of(std::false_type{}, 1, b1);
         finish();
       }
       if (it + 1 < passes) {
-        clear();
 #pragma unroll
         for (int j = 0; j < NJ; ++j) qf[0][j] = qn[0][j];
         r0 = rn;
@@ -644,13 +649,213 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
           fetch(k0 + KT, next);
           nk = own_key(k0 + 2 * KT);
         }
-        tile_of(b, bits);
+        if (any_key)
+          tile_of(std::false_type{}, b, bits);
+        else
+          tile_of(std::true_type{}, b, bits);
         if (more) stage(b ^ 1);
         __syncthreads();
         bits = next;
       }
     }
     finish();
+  }
+}
+
+// ------------------------------------------------------------------ few rows, bf16
+// A block takes 32 rows and a range of keys; its waves share the keys out, 32 at
+// a time, each with a piece of LDS, an online softmax and an O^T of its own,
+// and are joined at the end.  No barrier until then: what bounds it is the
+// bytes of K and V, so waves only have to keep loads in flight.  (The tile is
+// mostly empty for one query; its products still take less time than the loads.)
+template <int D16, bool SF, int NW>
+__global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(CrossArgs a, int keys, int tiles, int splits) {
+  constexpr int NJ = D16 / 16, ND = (D16 + 31) / 32, LDK = D16 + 8, LDV = v_row(D16), KW = 32;
+  constexpr int LPR = D16 <= 32 ? 4 : D16 <= 64 ? 8 : D16 <= 128 ? 16 : 32, RPP = 64 / LPR, CPT = KW / RPP;
+  constexpr int WAVE = KW * LDK + KW * LDV + 32, LDO = D16 + 4;  // (bf16 of a wave's LDS; floats of a row of its result)
+  static_assert(WAVE * 2 >= 32 * LDO * 4 || D16 > 160, "a wave's result takes the place of its tiles");
+  constexpr int AREA = WAVE * 2 > 32 * LDO * 4 ? WAVE * 2 : 32 * LDO * 4;
+  __shared__ __attribute__((aligned(16))) uint8_t smem[NW * AREA];
+  __shared__ float sm[NW][32], sl[NW][32];
+  const Place p = place_of(a.kv_heads, tiles, splits, a.n);
+  if (!p.on) return;
+  const Text tx = text_of(a, p.img);
+  const int k_begin = p.split * keys, k_end = splits > 1 ? min(tx.len, k_begin + keys) : tx.len;
+  if (splits > 1 && k_begin >= tx.len) return;  // (the join knows the text's length)
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, lh = lane >> 5;
+  const int rows = a.rep * a.n_q, d = a.d, r0 = p.tile * 32;
+  bf16 *Ks = (bf16*)(smem + wave * AREA), *Vs = Ks + KW * LDK;
+  const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
+  const float sl2 = a.scale == 0.f ? LOG2E : fabsf(a.scale) * LOG2E;
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+
+  const int pk = lane / LPR, pc = lane % LPR * 8;
+  const int ko = pc < d ? (pk * (int)a.k_ld + pc) * 2 : OOB, vo = pc < d ? (pk * (int)a.v_ld + pc) * 2 : OOB;
+  const bf16* K = (const bf16*)a.k + tx.k0 + p.g * a.k_head;
+  const bf16* V = (const bf16*)a.v + tx.v0 + p.g * a.v_head;
+  bf16x8 rk[CPT], rv[CPT];
+  auto fetch = [&](int k0, uint32_t bits) __attribute__((always_inline)) {
+    const int n = min(KW, k_end - k0);
+    const __amdgpu_buffer_rsrc_t kr = make_rsrc(K + (long)k0 * a.k_ld, ((n - 1) * (long)a.k_ld + d) * 2);
+    const __amdgpu_buffer_rsrc_t vr = make_rsrc(V + (long)k0 * a.v_ld, ((n - 1) * (long)a.v_ld + d) * 2);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      const bool on = bits >> pk >> (RPP * i) & 1;
+      rk[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(kr, on ? ko : OOB, i * RPP * (int)a.k_ld * 2, 0));
+      rv[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(vr, on ? vo : OOB, i * RPP * (int)a.v_ld * 2, 0));
+    }
+  };
+  auto own_key = [&](int k0) -> bool {
+    const int k = k0 + lq;
+    return k < k_end && (!mask || mask[k]);
+  };
+  int k0 = k_begin + wave * KW;
+  uint32_t bits = (uint32_t)__ballot(own_key(k0));
+  if (k0 < k_end) fetch(k0, bits);
+
+  bf16x8 qf[NJ];
+  {
+    const RowAt at = row_at(a, r0 + lq);
+    const bf16* Q = (const bf16*)a.q + (long)p.img * a.q_img + at.t * a.q_ld + (p.g * a.rep + at.h) * a.q_head;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int c = 16 * j + 8 * lh;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (r0 + lq < rows && c < d && a.scale != 0.f) v = *(const uint4*)(Q + c);
+      v.x ^= flip;
+      v.y ^= flip;
+      v.z ^= flip;
+      v.w ^= flip;
+      qf[j] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+  if constexpr (SF)  // ones in channel d of every key
+    if (lane < KW) {
+      bf16x8 v = {};
+      v[0] = (bf16)1.0f;
+      *(bf16x8*)&Vs[lane * LDV + d] = v;
+    }
+  bf16x8 ones = {};
+  if (lh == 0) ones[0] = (bf16)1.0f;
+  f32x16 o[ND];
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  for (; k0 < k_end; k0 += NW * KW) {
+#pragma unroll
+    for (int i = 0; i < CPT; ++i)
+      if (pc < D16) {
+        *(bf16x8*)&Ks[(pk + RPP * i) * LDK + pc] = rk[i];
+        if (!SF || pc < d) *(bf16x8*)&Vs[(pk + RPP * i) * LDV + pc] = rv[i];
+      }
+    asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
+    const uint32_t now = bits;
+    const int kn = k0 + NW * KW;
+    if (kn < k_end) {
+      bits = (uint32_t)__ballot(own_key(kn));
+      fetch(kn, bits);
+    }
+    if (!now) continue;
+    const f32x16 zero = {};
+    bf16x8 off = {};  // (keys that take no part start from -inf)
+    if (lh == 0) off[0] = __builtin_bit_cast(bf16, (unsigned short)(now >> lq & 1 ? 0 : 0xFF80));
+    f32x16 s = mfma32(off, ones, zero);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) s = mfma32(*(const bf16x8*)&Ks[lq * LDK + 16 * j + 8 * lh], qf[j], s);
+    float v = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) v = fmaxf(v, s[r]);
+    const float2 h = half_swap(v);
+    const float mt = fmaxf(h.x, h.y) * sl2;
+    const bool need = mt > m_run + TAU;
+    if (__any(need)) {
+      const float al = need ? __builtin_amdgcn_exp2f(m_run - mt) : 1.0f;
+      m_run = need ? mt : m_run;
+      l_run *= al;
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] *= al;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      bf16x8 pf;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pf[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[8 * u + i], sl2, -m_run));
+      if constexpr (!SF)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) l_run += (float)pf[i];
+#pragma unroll
+      for (int t = 0; t < ND; ++t) {
+        const bf16* at = &Vs[(16 * u + 4 * lh + ((lane & 15) >> 2)) * LDV + t * 32 + (lane & 16) + 4 * (lane & 3)];
+        const bf16x4 lo = read_transposed(at), hi = read_transposed(at + 8 * LDV);
+        o[t] = mfma32(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), pf, o[t]);
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+
+  // the wave's row sums, maxima and O to LDS
+  float l = l_run;
+  if constexpr (SF) {
+    l = 0.f;
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (32 * t + 8 * (r >> 2) + 4 * lh + (r & 3) == d) l = o[t][r];
+  }
+  const float2 h = half_swap(l);
+  const int here = min(32, rows - r0);
+  if (lh == 0) {
+    sm[wave][lq] = m_run;
+    sl[wave][lq] = h.x + h.y;
+  }
+  float* R = (float*)(smem + wave * AREA);
+  if (lq < here)
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 32 * t + 8 * i + 4 * lh;
+        if (c < d) *(float4*)(R + lq * LDO + c) = make_float4(o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]);
+      }
+  __syncthreads();
+  // four channels a thread
+  const int d4 = d >> 2;
+  for (int i = tid; i < here * d4; i += 64 * NW) {
+    const int row = i / d4, c = (i - row * d4) * 4;
+    float mt = sm[0][row];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) mt = fmaxf(mt, sm[w][row]);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    float lt = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = sm[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][row] - mt);
+      const f32x4 x = *(const f32x4*)((const float*)(smem + w * AREA) + row * LDO + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(f, x[e], v[e]);
+      lt = fmaf(f, sl[w][row], lt);
+    }
+    if (splits > 1) {
+      const Scratch sc = scratch_at(a, p.img, p.g, r0 + row, p.split, splits);
+      *(f32x4*)(sc.o + c) = v;
+      if (c == 0) {
+        sc.ml[0] = mt;
+        sc.ml[1] = lt;
+      }
+    } else {
+      const RowAt at = row_at(a, r0 + row);
+      const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+      bf16x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = (bf16)(v[e] * inv);
+      *(bf16x4*)((bf16*)a.o + (long)p.img * a.o_img + at.t * a.o_ld + (p.g * a.rep + at.h) * a.o_head + c) = w;
+    }
   }
 }
 
@@ -848,11 +1053,13 @@ static void launch_bf16(const CrossArgs& a, const Plan& p, hipStream_t s) {
 template <int D16, bool SF>
 static void launch_sum(const CrossArgs& a, const Plan& p, hipStream_t s) {
   const long rows = (long)a.rep * a.n_q;
-  if (p.kind == 1) {
-    launch_bf16<D16, SF, 1, 1>(a, p, s);
+  if (p.kind <= 1) {
+    constexpr int NW = D16 <= 64 ? 8 : 4;
+    const int tiles = (int)((rows + 31) / 32);
+    cross_keys_kernel<D16, SF, NW><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits);
     return;
   }
-  if constexpr (D16 <= 160)  // (wider heads' tiles leave no LDS for the output rows)
+  if constexpr (D16 <= 128)  // (wider heads' tiles leave no LDS for the output rows)
     if (a.max_len <= 2 * KT) {
       constexpr int NW = 4;
       // up to 8 groups of rows per wave, as long as some 1000 blocks remain
@@ -860,11 +1067,6 @@ static void launch_sum(const CrossArgs& a, const Plan& p, hipStream_t s) {
       const int passes = (int)(all / 1024 < 1 ? 1 : all / 1024 > 8 ? 8 : all / 1024);
       const int tiles = (int)((groups + passes - 1) / passes);
       cross_bf16_kernel<D16, SF, NW, 1, true><<<(unsigned)place_blocks(a.kv_heads, tiles, 1, a.n), 64 * NW, 0, s>>>(a, 0, tiles, 1, passes);
-      return;
-    }
-  if constexpr (D16 <= 64)
-    if (rows > 128) {
-      launch_bf16<D16, SF, 4, 2>(a, p, s);
       return;
     }
   launch_bf16<D16, SF, 4, 1>(a, p, s);
@@ -908,11 +1110,8 @@ hipError_t launch_cross_attention(DType dt, CrossArgs a, hipStream_t s) {
     a.rep_mul = (unsigned)(((1ull << (31 + l)) + a.rep - 1) / a.rep);
     a.rep_shift = l - 1;
   }
-  if (p.kind == 0) {
-    if (dt == BF16)
-      launch_few_rows<bf16>(a, p, s);
-    else
-      launch_few_rows<float>(a, p, s);
+  if (p.kind == 0 && dt != BF16) {
+    launch_few_rows<float>(a, p, s);
   } else if (dt == BF16) {
     if (a.d <= 32) launch_width<32>(a, p, s);
     else if (a.d <= 48) launch_width<48>(a, p, s);
