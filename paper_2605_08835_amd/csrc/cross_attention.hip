@@ -91,8 +91,8 @@ constexpr int FEW = 8;
 static Plan plan_of(int rep, int n_q, int max_len) {
   const long rows = (long)rep * n_q;
   Plan p;
-  p.kind = rows <= FEW ? 0 : rows <= 64 ? 1 : 2;
-  p.keys = p.kind <= 1 ? 512 : rows <= 256 ? 2048 : 0;
+  p.kind = rows <= FEW ? 0 : rows <= 128 ? 1 : 2;
+  p.keys = p.kind <= 1 ? 1024 : rows <= 512 ? 512 : 0;
   p.splits = p.keys && max_len > p.keys ? (max_len + p.keys - 1) / p.keys : 1;
   return p;
 }
@@ -544,13 +544,13 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
 #pragma unroll
     for (int g = 0; g < QG; ++g) {
       float l = l_run[g];
-      if constexpr (SF) {
-        l = 0.f;
+      if constexpr (SF) {  // (d is a multiple of 8: register 0 of a quad of half 0)
 #pragma unroll
         for (int t = 0; t < ND; ++t)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (32 * t + 8 * (r >> 2) + 4 * lh + (r & 3) == d) l = o[g][t][r];
+          for (int i = 0; i < 4; ++i)
+            if (32 * t + 8 * i == d) l = o[g][t][4 * i];
+        l = lh == 0 ? l : 0.f;
       }
       const float2 h = half_swap(l);
       l = h.x + h.y;
@@ -619,13 +619,18 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
     }
     __syncthreads();
     for (int it = 0; it < passes; ++it) {
-      bf16x8 qn[QG][NJ];
+      bf16x8 qn[QG][NJ] = {};
       const int rn = r0 + NW * 32;
       if (it + 1 < passes && rn < rows) load_q(rn, qn);
       if (r0 < rows) {
         const int bf = b0 ? 0 : 1;  // (the first tile that holds a key)
         tile_of(std::true_type{}, bf, b0 ? b0 : b1);
         if (b0) tile_of(std::false_type{}, 1, b1);
+        // The next rows' queries have landed before this group's stores are
+        // issued: waiting for them later would wait for the stores as well
+        // (one counter, and the compiler cannot count stores under branches).
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(qn[0][j]));
         finish();
       }
       if (it + 1 < passes) {
@@ -800,13 +805,13 @@ __global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(
 
   // the wave's row sums, maxima and O to LDS
   float l = l_run;
-  if constexpr (SF) {
-    l = 0.f;
+  if constexpr (SF) {  // (d is a multiple of 8: register 0 of a quad of half 0)
 #pragma unroll
     for (int t = 0; t < ND; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (32 * t + 8 * (r >> 2) + 4 * lh + (r & 3) == d) l = o[t][r];
+      for (int i = 0; i < 4; ++i)
+        if (32 * t + 8 * i == d) l = o[t][4 * i];
+    l = lh == 0 ? l : 0.f;
   }
   const float2 h = half_swap(l);
   const int here = min(32, rows - r0);
@@ -1054,7 +1059,7 @@ template <int D16, bool SF>
 static void launch_sum(const CrossArgs& a, const Plan& p, hipStream_t s) {
   const long rows = (long)a.rep * a.n_q;
   if (p.kind <= 1) {
-    constexpr int NW = D16 <= 64 ? 8 : 4;
+    constexpr int NW = 4;
     const int tiles = (int)((rows + 31) / 32);
     cross_keys_kernel<D16, SF, NW><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits);
     return;
