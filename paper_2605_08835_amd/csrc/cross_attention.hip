@@ -63,24 +63,50 @@ __device__ __forceinline__ Text text_of(const CrossArgs& a, int img) {
 }
 
 // Block -> (K/V head, row tile, split, image).  Consecutive blocks go to the 8
-// XCDs in turn; the K/V heads of one row tile stay on one XCD, next to each
-// other in time, since their rows share cache lines of q, o, K and V.
+// XCDs in turn, each with an L2 of its own.
+//  * together > 0: the row tiles of one K/V head read the same keys, so the tiles
+//    of `together` neighbouring heads stay on one XCD, next to each other in time (over
+//    all 8, K and V came from memory 8 times).
+//  * together = 0, where keys are read once or are few: all K/V heads of one
+//    tile stay on one XCD, since their rows share cache lines of q, o, K and V
+//    (48 x 4096 rows, 8 heads of 40, up to 77 keys: 97 us against 121 over all XCDs).
 struct Place {
   int g, tile, split, img;
   bool on;
 };
-__device__ __forceinline__ Place place_of(int kv_heads, int tiles, int splits, int n) {
+__device__ __forceinline__ Place place_of(int kv_heads, int tiles, int splits, int n, int together) {
   const unsigned id = blockIdx.x, xcd = id & 7, i = id >> 3;
   Place p;
-  p.g = i % kv_heads;
-  const unsigned t = i / kv_heads * 8 + xcd;
-  p.on = t < (unsigned)tiles * splits * n;
-  p.tile = t % tiles;
-  p.split = t / tiles % splits;
-  p.img = t / tiles / splits;
+  if (together) {
+    const unsigned per = (unsigned)tiles * splits * together, groups = kv_heads / together;
+    const unsigned u = i / per * 8 + xcd, t = i % per;
+    p.on = u < groups * n;
+    p.g = u % groups * together + t % together;
+    p.img = u / groups;
+    p.tile = t / together % tiles;
+    p.split = t / together / tiles;
+  } else {
+    const unsigned t = i / kv_heads * 8 + xcd;
+    p.g = i % kv_heads;
+    p.on = t < (unsigned)tiles * splits * n;
+    p.tile = t % tiles;
+    p.split = t / tiles % splits;
+    p.img = t / tiles / splits;
+  }
   return p;
 }
-static long place_blocks(long kv_heads, long tiles, long splits, long n) { return (tiles * splits * n + 7) / 8 * 8 * kv_heads; }
+static unsigned place_blocks(long kv_heads, long tiles, long splits, long n, long together) {
+  if (!together) return (unsigned)((tiles * splits * n + 7) / 8 * 8 * kv_heads);
+  return (unsigned)((kv_heads / together * n + 7) / 8 * 8 * tiles * splits * together);
+}
+// Heads whose rows fill whole lines of 128 bytes, where that many divide the
+// heads and leave every XCD two of them (16 x 4096 rows, 8 heads of 40, up to 300
+// keys: 67 us against 77 one by one); else one.
+static int place_together(const CrossArgs& a, int el) {
+  int h = 1;
+  while (h * a.d * el % 128) h *= 2;
+  return a.kv_heads % h == 0 && (long)a.n * (a.kv_heads / h) >= 16 ? h : 1;
+}
 
 // How a call is split: `keys` per range (0: not split).
 struct Plan {
@@ -135,7 +161,7 @@ __device__ __forceinline__ float2 half_swap(float v) {  // (v of lanes l and l ^
 template <typename T, int RB, int LPK>
 __global__ __launch_bounds__(512) void cross_few_kernel(CrossArgs a, int keys, int splits) {
   constexpr int U = RB <= 2 ? 4 : 2, NG = 64 / LPK, NW = 8, STEP = NW * NG * U;
-  const Place p = place_of(a.kv_heads, 1, splits, a.n);
+  const Place p = place_of(a.kv_heads, 1, splits, a.n, 0);
   if (!p.on) return;
   const Text tx = text_of(a, p.img);
   const int k_begin = p.split * keys, k_end = splits > 1 ? min(tx.len, k_begin + keys) : tx.len;
@@ -316,6 +342,20 @@ __device__ __forceinline__ bf16x4 read_transposed(const bf16* p) {
 #endif
 }
 
+// l + the eight rounded probabilities, two to an instruction (taking them apart
+// again cost three each, a third of a 64-key tile's vector instructions).
+__device__ __forceinline__ float sum_probs(bf16x8 p, float l) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 one = {(bf16)1.0f, (bf16)1.0f};
+  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 0, 1), one, l, false);
+  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 2, 3), one, l, false);
+  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 4, 5), one, l, false);
+  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 6, 7), one, l, false);
+#endif
+  return l;
+}
+
 __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 #if defined(__HIP_DEVICE_COMPILE__)
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -333,8 +373,8 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 // staged once, and the waves pass `passes` groups of rows each over them without
 // meeting again.  (Its arithmetic on a row is the same.)
 template <int D16, bool SF, int NW, int QG, bool SHORT>
-__global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1) : NW == 1 || D16 > 96 ? 1 : 2) void cross_bf16_kernel(
-    CrossArgs a, int keys, int tiles, int splits, int passes) {
+__global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1) : D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1) void cross_bf16_kernel(
+    CrossArgs a, int keys, int tiles, int splits, int passes, int together) {
   static_assert(!SHORT || QG == 1, "one group at a time");
   constexpr int NJ = D16 / 16, ND = (D16 + 31) / 32, NT = 64 * NW, LDK = D16 + 8, LDV = v_row(D16);
   // A tile is moved by passes of NT / LPR keys, LPR lanes (a power of two) a key
@@ -342,7 +382,7 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
   __shared__ __attribute__((aligned(16))) bf16 Ks[2][KT * LDK];
   __shared__ __attribute__((aligned(16))) bf16 Vs[2][KT * LDV + 32];  // (the last rows are read past their end where D16 % 32)
   __shared__ __attribute__((aligned(16))) bf16 Os[SHORT ? NW * 32 * LDK : 8];
-  const Place p = place_of(a.kv_heads, tiles, splits, a.n);
+  const Place p = place_of(a.kv_heads, tiles, splits, a.n, SHORT ? 0 : together);
   if (!p.on) return;
   const Text tx = text_of(a, p.img);
   const int k_begin = p.split * keys, k_end = splits > 1 ? min(tx.len, k_begin + keys) : tx.len;
@@ -518,9 +558,7 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           pf[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[g][u >> 1][8 * (u & 1) + i], sl2, -m_run[g]));
-        if constexpr (!SF)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) l_run[g] = FIRST && u == 0 && i == 0 ? (float)pf[i] : l_run[g] + (float)pf[i];
+        if constexpr (!SF) l_run[g] = sum_probs(pf, FIRST && u == 0 ? 0.f : l_run[g]);
 #pragma unroll
         for (int t = 0; t < ND; ++t) {
           const f32x16 zero = {};
@@ -674,7 +712,8 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
 // bytes of K and V, so waves only have to keep loads in flight.  (The tile is
 // mostly empty for one query; its products still take less time than the loads.)
 template <int D16, bool SF, int NW>
-__global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(CrossArgs a, int keys, int tiles, int splits) {
+__global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(CrossArgs a, int keys, int tiles, int splits,
+                                                                                  int together) {
   constexpr int NJ = D16 / 16, ND = (D16 + 31) / 32, LDK = D16 + 8, LDV = v_row(D16), KW = 32;
   constexpr int LPR = D16 <= 32 ? 4 : D16 <= 64 ? 8 : D16 <= 128 ? 16 : 32, RPP = 64 / LPR, CPT = KW / RPP;
   constexpr int WAVE = KW * LDK + KW * LDV + 32, LDO = D16 + 4;  // (bf16 of a wave's LDS; floats of a row of its result)
@@ -682,7 +721,7 @@ __global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(
   constexpr int AREA = WAVE * 2 > 32 * LDO * 4 ? WAVE * 2 : 32 * LDO * 4;
   __shared__ __attribute__((aligned(16))) uint8_t smem[NW * AREA];
   __shared__ float sm[NW][32], sl[NW][32];
-  const Place p = place_of(a.kv_heads, tiles, splits, a.n);
+  const Place p = place_of(a.kv_heads, tiles, splits, a.n, together);
   if (!p.on) return;
   const Text tx = text_of(a, p.img);
   const int k_begin = p.split * keys, k_end = splits > 1 ? min(tx.len, k_begin + keys) : tx.len;
@@ -790,9 +829,7 @@ __global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(
       bf16x8 pf;
 #pragma unroll
       for (int i = 0; i < 8; ++i) pf[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[8 * u + i], sl2, -m_run));
-      if constexpr (!SF)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) l_run += (float)pf[i];
+      if constexpr (!SF) l_run = sum_probs(pf, l_run);
 #pragma unroll
       for (int t = 0; t < ND; ++t) {
         const bf16* at = &Vs[(16 * u + 4 * lh + ((lane & 15) >> 2)) * LDV + t * 32 + (lane & 16) + 4 * (lane & 3)];
@@ -882,12 +919,13 @@ __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) {
 }  // namespace
 
 template <int D32, int NW>
-__global__ __launch_bounds__(64 * NW, D32 <= 64 ? 2 : 1) void cross_f32_kernel(CrossArgs a, int keys, int tiles, int splits) {
+__global__ __launch_bounds__(64 * NW, D32 <= 64 ? 2 : 1) void cross_f32_kernel(CrossArgs a, int keys, int tiles, int splits,
+                                                                               int together) {
   constexpr int NI = D32 / 8, ND = D32 / 32, NT = 64 * NW, LDK = D32 + 4, LDV = D32 + 8;  // (rows apart by banks)
   constexpr int CPT = FT * (D32 / 4) / NT;
   __shared__ __attribute__((aligned(16))) float Ks[2][FT * LDK];
   __shared__ __attribute__((aligned(16))) float Vs[2][FT * LDV];
-  const Place p = place_of(a.kv_heads, tiles, splits, a.n);
+  const Place p = place_of(a.kv_heads, tiles, splits, a.n, together);
   if (!p.on) return;
   const Text tx = text_of(a, p.img);
   const int k_begin = p.split * keys, k_end = splits > 1 ? min(tx.len, k_begin + keys) : tx.len;
@@ -1028,7 +1066,7 @@ __global__ __launch_bounds__(64 * NW, D32 <= 64 ? 2 : 1) void cross_f32_kernel(C
 // ------------------------------------------------------------------ launch
 template <typename T, int RB>
 static void launch_few(const CrossArgs& a, const Plan& p, hipStream_t s) {
-  const unsigned grid = (unsigned)place_blocks(a.kv_heads, 1, p.splits, a.n);
+  const unsigned grid = place_blocks(a.kv_heads, 1, p.splits, a.n, 0);
   if (a.d <= 32)
     cross_few_kernel<T, RB, 4><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
   else if (a.d <= 64)
@@ -1052,7 +1090,9 @@ template <int D16, bool SF, int NW, int QG>
 static void launch_bf16(const CrossArgs& a, const Plan& p, hipStream_t s) {
   const long rows = (long)a.rep * a.n_q;
   const int tiles = (int)((rows + 32 * NW * QG - 1) / (32 * NW * QG));
-  cross_bf16_kernel<D16, SF, NW, QG, false><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits, 1);
+  const int together = place_together(a, 2);
+  cross_bf16_kernel<D16, SF, NW, QG, false><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 64 * NW, 0, s>>>(
+      a, p.keys, tiles, p.splits, 1, together);
 }
 
 template <int D16, bool SF>
@@ -1061,7 +1101,8 @@ static void launch_sum(const CrossArgs& a, const Plan& p, hipStream_t s) {
   if (p.kind <= 1) {
     constexpr int NW = 4;
     const int tiles = (int)((rows + 31) / 32);
-    cross_keys_kernel<D16, SF, NW><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits);
+    const int together = tiles > 1 ? place_together(a, 2) : 0;
+    cross_keys_kernel<D16, SF, NW><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits, together);
     return;
   }
   if constexpr (D16 <= 128)  // (wider heads' tiles leave no LDS for the output rows)
@@ -1071,7 +1112,7 @@ static void launch_sum(const CrossArgs& a, const Plan& p, hipStream_t s) {
       const long groups = (rows + 32 * NW - 1) / (32 * NW), all = groups * a.kv_heads * a.n;
       const int passes = (int)(all / 1024 < 1 ? 1 : all / 1024 > 8 ? 8 : all / 1024);
       const int tiles = (int)((groups + passes - 1) / passes);
-      cross_bf16_kernel<D16, SF, NW, 1, true><<<(unsigned)place_blocks(a.kv_heads, tiles, 1, a.n), 64 * NW, 0, s>>>(a, 0, tiles, 1, passes);
+      cross_bf16_kernel<D16, SF, NW, 1, true><<<place_blocks(a.kv_heads, tiles, 1, a.n, 0), 64 * NW, 0, s>>>(a, 0, tiles, 1, passes, 0);
       return;
     }
   launch_bf16<D16, SF, 4, 1>(a, p, s);
@@ -1088,12 +1129,13 @@ static void launch_width(const CrossArgs& a, const Plan& p, hipStream_t s) {
 template <int D32>
 static void launch_f32(const CrossArgs& a, const Plan& p, hipStream_t s) {
   const long rows = (long)a.rep * a.n_q;
+  const int together = place_together(a, 4);
   if (p.kind == 1) {
     const int tiles = (int)((rows + 31) / 32);
-    cross_f32_kernel<D32, 1><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 64, 0, s>>>(a, p.keys, tiles, p.splits);
+    cross_f32_kernel<D32, 1><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 64, 0, s>>>(a, p.keys, tiles, p.splits, together);
   } else {
     const int tiles = (int)((rows + 127) / 128);
-    cross_f32_kernel<D32, 4><<<(unsigned)place_blocks(a.kv_heads, tiles, p.splits, a.n), 256, 0, s>>>(a, p.keys, tiles, p.splits);
+    cross_f32_kernel<D32, 4><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 256, 0, s>>>(a, p.keys, tiles, p.splits, together);
   }
 }
 
