@@ -706,6 +706,51 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
 }
 
 // ------------------------------------------------------------------ few rows, bf16
+// The results of a block's waves (row by row in LDS, `area` floats apart), whose
+// maxima and sums are sm and sl, joined in order: to the output, or as one split's
+// result to scratch.  Four channels a thread.
+template <typename T, int NW>
+__device__ __forceinline__ void join_waves(const CrossArgs& a, const Place& p, int splits, int r0, int here, const float* res,
+                                           int area, int ldo, const float (&sm)[NW][32], const float (&sl)[NW][32]) {
+  const int d4 = a.d >> 2;
+  for (int i = threadIdx.x; i < here * d4; i += 64 * NW) {
+    const int row = i / d4, c = (i - row * d4) * 4;
+    float mt = sm[0][row];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) mt = fmaxf(mt, sm[w][row]);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    float lt = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = sm[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][row] - mt);
+      const f32x4 x = *(const f32x4*)(res + w * area + row * ldo + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(f, x[e], v[e]);
+      lt = fmaf(f, sl[w][row], lt);
+    }
+    if (splits > 1) {
+      const Scratch sc = scratch_at(a, p.img, p.g, r0 + row, p.split, splits);
+      *(f32x4*)(sc.o + c) = v;
+      if (c == 0) {
+        sc.ml[0] = mt;
+        sc.ml[1] = lt;
+      }
+    } else {
+      const RowAt at = row_at(a, r0 + row);
+      const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+      T* out = (T*)a.o + (long)p.img * a.o_img + at.t * a.o_ld + (p.g * a.rep + at.h) * a.o_head + c;
+      if constexpr (std::is_same<T, float>::value) {
+        *(f32x4*)out = v * inv;
+      } else {
+        bf16x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (bf16)(v[e] * inv);
+        *(bf16x4*)out = w;
+      }
+    }
+  }
+}
+
 // A block takes 32 rows and a range of keys; its waves share the keys out, 32 at
 // a time, each with a piece of LDS, an online softmax and an O^T of its own,
 // and are joined at the end.  No barrier until then: what bounds it is the
@@ -866,39 +911,7 @@ __global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(
         if (c < d) *(float4*)(R + lq * LDO + c) = make_float4(o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]);
       }
   __syncthreads();
-  // four channels a thread
-  const int d4 = d >> 2;
-  for (int i = tid; i < here * d4; i += 64 * NW) {
-    const int row = i / d4, c = (i - row * d4) * 4;
-    float mt = sm[0][row];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) mt = fmaxf(mt, sm[w][row]);
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    float lt = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float f = sm[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][row] - mt);
-      const f32x4 x = *(const f32x4*)((const float*)(smem + w * AREA) + row * LDO + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = fmaf(f, x[e], v[e]);
-      lt = fmaf(f, sl[w][row], lt);
-    }
-    if (splits > 1) {
-      const Scratch sc = scratch_at(a, p.img, p.g, r0 + row, p.split, splits);
-      *(f32x4*)(sc.o + c) = v;
-      if (c == 0) {
-        sc.ml[0] = mt;
-        sc.ml[1] = lt;
-      }
-    } else {
-      const RowAt at = row_at(a, r0 + row);
-      const float inv = lt == 0.f ? 0.f : 1.0f / lt;
-      bf16x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = (bf16)(v[e] * inv);
-      *(bf16x4*)((bf16*)a.o + (long)p.img * a.o_img + at.t * a.o_ld + (p.g * a.rep + at.h) * a.o_head + c) = w;
-    }
-  }
+  join_waves<bf16, NW>(a, p, splits, r0, here, (const float*)smem, AREA / 4, LDO, sm, sl);
 }
 
 // ------------------------------------------------------------------ many rows, fp32
@@ -1063,6 +1076,147 @@ __global__ __launch_bounds__(64 * NW, D32 <= 64 ? 2 : 1) void cross_f32_kernel(C
     }
 }
 
+// Few rows, fp32 (9 to 128; up to 8 take the lanes above): as cross_keys_kernel,
+// on fp32 MFMAs.  PRE: the next keys are loaded while these are multiplied (wider
+// heads have no registers left for them, and 16 times the products of a bf16 tile to hide them with).
+template <int D32, int NW>
+__global__ __launch_bounds__(64 * NW) void cross_keys_f32_kernel(CrossArgs a, int keys, int tiles, int splits, int together) {
+  constexpr int NI = D32 / 8, ND = D32 / 32, LDK = D32 + 4, LDV = D32 + 8, LDO = D32 + 4, AREA = FT * (LDK + LDV);
+  constexpr int CPT = FT * (D32 / 4) / 64;
+  constexpr bool PRE = D32 <= 128;
+  __shared__ __attribute__((aligned(16))) float smem[NW * AREA];
+  __shared__ float sm[NW][32], sl[NW][32];
+  const Place p = place_of(a.kv_heads, tiles, splits, a.n, together);
+  if (!p.on) return;
+  const Text tx = text_of(a, p.img);
+  const int k_begin = p.split * keys, k_end = splits > 1 ? min(tx.len, k_begin + keys) : tx.len;
+  if (splits > 1 && k_begin >= tx.len) return;  // (the join knows the text's length)
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, lh = lane >> 5;
+  const int rows = a.rep * a.n_q, d = a.d, r0 = p.tile * 32;
+  float *Ks = smem + wave * AREA, *Vs = Ks + FT * LDK;
+  const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
+  const float qs = a.scale * LOG2E;
+  const float* K = (const float*)a.k + tx.k0 + p.g * a.k_head;
+  const float* V = (const float*)a.v + tx.v0 + p.g * a.v_head;
+
+  uint4 rk[CPT], rv[CPT];
+  auto load = [&](const float* X, long ld, int k0, uint32_t bits, uint4 (&r)[CPT]) __attribute__((always_inline)) {
+    const int n = min(FT, k_end - k0);
+    const __amdgpu_buffer_rsrc_t xr = make_rsrc(X + (long)k0 * ld, ((n - 1) * ld + d) * 4);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      const int idx = lane + 64 * i, key = idx / (D32 / 4), c = idx % (D32 / 4) * 4;
+      const bool on = (bits >> key & 1) && c < d;
+      r[i] = __builtin_bit_cast(uint4, buf_load16(xr, on ? (key * (int)ld + c) * 4 : OOB));
+    }
+  };
+  auto put = [&](float* X, int ld, const uint4 (&r)[CPT]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      const int idx = lane + 64 * i, key = idx / (D32 / 4), c = idx % (D32 / 4) * 4;
+      *(uint4*)&X[key * ld + c] = r[i];
+    }
+  };
+  auto own_key = [&](int k0) -> bool {
+    const int k = k0 + lq;
+    return k < k_end && (!mask || mask[k]);
+  };
+  int k0 = k_begin + wave * FT;
+  uint32_t bits = (uint32_t)__ballot(own_key(k0));
+  if (PRE && k0 < k_end) {
+    load(K, a.k_ld, k0, bits, rk);
+    load(V, a.v_ld, k0, bits, rv);
+  }
+  f32x4 qf[NI];
+  {
+    const RowAt at = row_at(a, r0 + lq);
+    const float* Q = (const float*)a.q + (long)p.img * a.q_img + at.t * a.q_ld + (p.g * a.rep + at.h) * a.q_head;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int c = 8 * i + 4 * lh;
+      qf[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (r0 + lq < rows && c < d) qf[i] = *(const f32x4*)(Q + c) * qs;
+    }
+  }
+  f32x16 o[ND];
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+  float m_run = -INFINITY, l = 0.f;
+  for (; k0 < k_end; k0 += NW * FT) {
+    if constexpr (!PRE) load(K, a.k_ld, k0, bits, rk);
+    put(Ks, LDK, rk);
+    if constexpr (!PRE) load(V, a.v_ld, k0, bits, rv);
+    put(Vs, LDV, rv);
+    asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
+    const uint32_t now = bits;
+    const int kn = k0 + NW * FT;
+    if (kn < k_end) {
+      bits = (uint32_t)__ballot(own_key(kn));
+      if constexpr (PRE) {
+        load(K, a.k_ld, kn, bits, rk);
+        load(V, a.v_ld, kn, bits, rv);
+      }
+    }
+    if (!now) continue;
+    f32x16 s = {};
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      if (8 * i >= d) break;
+      const f32x4 kf = *(const f32x4*)&Ks[lq * LDK + 8 * i + 4 * lh];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = mfma_f32(kf[e], qf[i][e], s);
+    }
+    if (now != ~0u) {
+      const uint32_t bm = now >> (4 * lh);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(bm >> (8 * (i >> 2) + (i & 3)) & 1)) s[i] = -INFINITY;
+    }
+    float v = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) v = fmaxf(v, s[i]);
+    const float2 hv = half_swap(v);
+    const float mt = fmaxf(hv.x, hv.y);
+    const bool need = mt > m_run + TAU;
+    if (__any(need)) {
+      const float al = need ? __builtin_amdgcn_exp2f(m_run - mt) : 1.0f;
+      m_run = need ? mt : m_run;
+      l *= al;
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] *= al;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float pr = __builtin_amdgcn_exp2f(s[i] - m_run);
+      l += pr;
+      const float* vr = &Vs[(8 * (i >> 2) + 4 * lh + (i & 3)) * LDV + lq];
+#pragma unroll
+      for (int t = 0; t < ND; ++t) o[t] = mfma_f32(vr[32 * t], pr, o[t]);
+    }
+    asm volatile("" ::: "memory");
+  }
+  const float2 hl = half_swap(l);
+  const int here = min(32, rows - r0);
+  if (lh == 0) {
+    sm[wave][lq] = m_run;
+    sl[wave][lq] = hl.x + hl.y;
+  }
+  if (lq < here)
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 32 * t + 8 * i + 4 * lh;
+        if (c < d) *(float4*)(Ks + lq * LDO + c) = make_float4(o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]);
+      }
+  __syncthreads();
+  join_waves<float, NW>(a, p, splits, r0, here, smem, AREA, LDO, sm, sl);
+}
+
 // ------------------------------------------------------------------ launch
 template <typename T, int RB>
 static void launch_few(const CrossArgs& a, const Plan& p, hipStream_t s) {
@@ -1131,8 +1285,9 @@ static void launch_f32(const CrossArgs& a, const Plan& p, hipStream_t s) {
   const long rows = (long)a.rep * a.n_q;
   const int together = place_together(a, 4);
   if (p.kind == 1) {
+    constexpr int NW = D32 <= 128 ? 4 : 2;  // (as many as the LDS holds)
     const int tiles = (int)((rows + 31) / 32);
-    cross_f32_kernel<D32, 1><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 64, 0, s>>>(a, p.keys, tiles, p.splits, together);
+    cross_keys_f32_kernel<D32, NW><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits, together);
   } else {
     const int tiles = (int)((rows + 127) / 128);
     cross_f32_kernel<D32, 4><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 256, 0, s>>>(a, p.keys, tiles, p.splits, together);
