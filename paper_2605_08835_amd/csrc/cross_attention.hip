@@ -6,17 +6,17 @@
 // K/V head, row r of an image and K/V head g is query r / rep, head g rep +
 // r % rep, so shared heads fill the tiles like further queries.
 //
-//  * Many rows (bf16): flash attention on MFMA.  A wave owns 32 QG rows, the
+//  * Many rows (bf16): flash attention on MFMA.  A wave owns 32 rows, the
 //    block shares tiles of 64 keys in LDS.  Scores are computed transposed,
 //    S^T = K Q^T, so that a lane holds one row's scores: its maximum and
 //    rescale are per-lane, and P^T feeds O^T = V^T P^T from the registers.
 //    V lies in LDS as it came (key by key); the transposing LDS read hands
 //    each lane four keys of one channel.
 //  * fp32: the same on fp32 MFMAs.
-//  * Few rows (at most 8): no tile to fill, bound by the bytes of K and V.
-//    Lanes share a key's channels, every lane group runs its own online
-//    softmax over the keys that come its way, and the groups are joined at
-//    the end.
+//  * Few rows (at most 128): bound by the bytes of K and V.  The waves of a
+//    block share out the keys of one tile of 32 rows and meet only at the end.
+//    fp32 with at most 8 rows needs no tile: lanes share a key's channels, and
+//    every lane group runs an online softmax of its own.
 //  * Few rows over long texts are split along the keys into ranges of a fixed
 //    length, whose unnormalised results a second kernel joins in order.  The
 //    ranges start at the text's own first key: a row's bits depend neither on
@@ -108,16 +108,16 @@ static int place_together(const CrossArgs& a, int el) {
   return a.kv_heads % h == 0 && (long)a.n * (a.kv_heads / h) >= 16 ? h : 1;
 }
 
-// How a call is split: `keys` per range (0: not split).
+// The kernel of a call, by the rows of a K/V head, and its ranges of `keys` (0:
+// not split): kind 0 up to 8 rows, 1 up to 128, 2 past that.  1024 keys a range: one query over
+// 9000 to 16384 keys, 4 x 20 heads of 64 71 us (512: 77, 2048: 72), 2 x 16 queries over 4000 to 8000 19 (23, 20).
 struct Plan {
-  int kind;  // 0: few rows, 1: one wave of 32 rows, 2: four waves
-  int keys, splits;
+  int kind, keys, splits;
 };
-constexpr int FEW = 8;
 static Plan plan_of(int rep, int n_q, int max_len) {
   const long rows = (long)rep * n_q;
   Plan p;
-  p.kind = rows <= FEW ? 0 : rows <= 128 ? 1 : 2;
+  p.kind = rows <= 8 ? 0 : rows <= 128 ? 1 : 2;
   p.keys = p.kind <= 1 ? 1024 : rows <= 512 ? 512 : 0;
   p.splits = p.keys && max_len > p.keys ? (max_len + p.keys - 1) / p.keys : 1;
   return p;
@@ -154,11 +154,10 @@ __device__ __forceinline__ float2 half_swap(float v) {  // (v of lanes l and l ^
 
 }  // namespace
 
-// ------------------------------------------------------------------ few rows
+// ------------------------------------------------------------------ few rows, fp32
 // RB rows (a power of two) per K/V head.  LPK lanes (a power of two) hold a key's
 // channels, 8 each; a wave has 64 / LPK key groups, U keys of each in flight.
-// Measured (4 images, 20 heads of 64, 9000 to 16384 keys): see launch.
-template <typename T, int RB, int LPK>
+template <int RB, int LPK>
 __global__ __launch_bounds__(512) void cross_few_kernel(CrossArgs a, int keys, int splits) {
   constexpr int U = RB <= 2 ? 4 : 2, NG = 64 / LPK, NW = 8, STEP = NW * NG * U;
   const Place p = place_of(a.kv_heads, 1, splits, a.n, 0);
@@ -169,8 +168,8 @@ __global__ __launch_bounds__(512) void cross_few_kernel(CrossArgs a, int keys, i
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ch = (lane % LPK) * 8, grp = lane / LPK;
   const int rows = a.rep * a.n_q;
   const bool has = ch < a.d;
-  const T* K = (const T*)a.k + tx.k0 + p.g * a.k_head + ch;
-  const T* V = (const T*)a.v + tx.v0 + p.g * a.v_head + ch;
+  const float* K = (const float*)a.k + tx.k0 + p.g * a.k_head + ch;
+  const float* V = (const float*)a.v + tx.v0 + p.g * a.v_head + ch;
   const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
 
   float q[RB][8], o[RB][8], m[RB], l[RB];
@@ -182,7 +181,7 @@ __global__ __launch_bounds__(512) void cross_few_kernel(CrossArgs a, int keys, i
     l[r] = 0.f;
     if (r < rows && has) {
       const int t = r / a.rep, h = p.g * a.rep + r % a.rep;
-      load8f((const T*)a.q + (long)p.img * a.q_img + t * a.q_ld + h * a.q_head + ch, q[r]);
+      load8f((const float*)a.q + (long)p.img * a.q_img + t * a.q_ld + h * a.q_head + ch, q[r]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) q[r][e] *= a.scale * LOG2E;
     }
@@ -287,7 +286,7 @@ __global__ __launch_bounds__(512) void cross_few_kernel(CrossArgs a, int keys, i
       }
     } else {
       const int t = r / a.rep, h = p.g * a.rep + r % a.rep;
-      ((T*)a.o)[(long)p.img * a.o_img + t * a.o_ld + h * a.o_head + c] = from_f<T>(lt == 0.f ? 0.f : v * (1.0f / lt));
+      ((float*)a.o)[(long)p.img * a.o_img + t * a.o_ld + h * a.o_head + c] = lt == 0.f ? 0.f : v * (1.0f / lt);
     }
   }
 }
@@ -368,15 +367,18 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 
 // D16: head width rounded up to a width the kernel is built for.  SF: d < D16,
 // so that channel d of V in LDS is free: it holds ones, and row d of O^T
-// becomes the sum of the (rounded) probabilities.  NW waves of QG groups of 32
-// rows.  SHORT: no text is longer than the two tiles that LDS holds; they are
-// staged once, and the waves pass `passes` groups of rows each over them without
-// meeting again.  (Its arithmetic on a row is the same.)
-template <int D16, bool SF, int NW, int QG, bool SHORT>
-__global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1) : D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1) void cross_bf16_kernel(
+// becomes the sum of the (rounded) probabilities.  Four waves of 32 rows.
+// SHORT: no text is longer than the two tiles that LDS holds; they are staged
+// once, and the waves pass `passes` groups of rows each over them without
+// meeting again (48 x 4096 rows, 8 heads of 40, up to 77 keys: 95 us, staging
+// them for every 128 rows 149).  Its arithmetic on a row is the same.  What
+// bounds it is memory: 80-byte rows of a 640-byte token reach 3.3 TB/s with the
+// arithmetic left out, which alone takes 47 us; three waves per SIMD hide part
+// of one behind the other.
+template <int D16, bool SF, bool SHORT>
+__global__ __launch_bounds__(256, D16 <= 48 || (D16 == 64 && !SHORT) ? 3 : D16 <= 96 ? 2 : 1) void cross_bf16_kernel(
     CrossArgs a, int keys, int tiles, int splits, int passes, int together) {
-  static_assert(!SHORT || QG == 1, "one group at a time");
-  constexpr int NJ = D16 / 16, ND = (D16 + 31) / 32, NT = 64 * NW, LDK = D16 + 8, LDV = v_row(D16);
+  constexpr int NW = 4, NJ = D16 / 16, ND = (D16 + 31) / 32, NT = 64 * NW, LDK = D16 + 8, LDV = v_row(D16);
   // A tile is moved by passes of NT / LPR keys, LPR lanes (a power of two) a key
   constexpr int LPR = D16 <= 32 ? 4 : D16 <= 64 ? 8 : D16 <= 128 ? 16 : 32, RPP = NT / LPR < KT ? NT / LPR : KT, CPT = KT / RPP;
   __shared__ __attribute__((aligned(16))) bf16 Ks[2][KT * LDK];
@@ -389,44 +391,41 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
   if (splits > 1 && k_begin >= tx.len) return;  // (the join knows the text's length)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, lh = lane >> 5;
   const int rows = a.rep * a.n_q, d = a.d;
-  int r0 = (p.tile * passes * NW + wave) * (32 * QG);  // (uniform)
+  int r0 = (p.tile * passes * NW + wave) * 32;  // (uniform)
   const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
   // (a scale of 0 or below: uniform weights, or -q, under a positive one)
   const float sl2 = a.scale == 0.f ? LOG2E : fabsf(a.scale) * LOG2E;
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
 
-  // Q^T fragments (B operand): row r0 + 32 g + lq, channels 16 j + 8 lh + [0, 8)
-  auto load_q = [&](int r0, bf16x8 (&qf)[QG][NJ]) __attribute__((always_inline)) {
+  // Q^T fragments (B operand): row rg + lq, channels 16 j + 8 lh + [0, 8)
+  auto load_q = [&](int rg, bf16x8 (&qf)[NJ]) __attribute__((always_inline)) {
+    uint4 v[NJ];
+    const int n = a.scale == 0.f ? 0 : min(32, rows - rg);
+    if (a.rep == 1) {  // (32 rows from one address on; what lies past them, and channels from d on, read as zero)
+      const bf16* Q = (const bf16*)a.q + (long)p.img * a.q_img + (long)rg * a.q_ld + p.g * a.q_head;
+      const __amdgpu_buffer_rsrc_t qr = make_rsrc(Q, n <= 0 ? 0 : ((n - 1) * (long)a.q_ld + d) * 2);
 #pragma unroll
-    for (int g = 0; g < QG; ++g) {
-      uint4 v[NJ];
-      const int rg = r0 + 32 * g, n = a.scale == 0.f ? 0 : min(32, rows - rg);
-      if (a.rep == 1) {  // (32 rows from one address on; what lies past them, and channels from d on, read as zero)
-        const bf16* Q = (const bf16*)a.q + (long)p.img * a.q_img + (long)rg * a.q_ld + p.g * a.q_head;
-        const __amdgpu_buffer_rsrc_t qr = make_rsrc(Q, n <= 0 ? 0 : ((n - 1) * (long)a.q_ld + d) * 2);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-          v[j] = __builtin_bit_cast(uint4, buf_load16(qr, 16 * j + 8 * lh < d ? (lq * (int)a.q_ld + 16 * j + 8 * lh) * 2 : OOB));
-      } else {
-        const RowAt at = row_at(a, rg + lq);
-        const bf16* Q = (const bf16*)a.q + (long)p.img * a.q_img + at.t * a.q_ld + (p.g * a.rep + at.h) * a.q_head;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          v[j] = make_uint4(0, 0, 0, 0);
-          if (lq < n && 16 * j + 8 * lh < d) v[j] = *(const uint4*)(Q + 16 * j + 8 * lh);
-        }
-      }
+      for (int j = 0; j < NJ; ++j)
+        v[j] = __builtin_bit_cast(uint4, buf_load16(qr, 16 * j + 8 * lh < d ? (lq * (int)a.q_ld + 16 * j + 8 * lh) * 2 : OOB));
+    } else {
+      const RowAt at = row_at(a, rg + lq);
+      const bf16* Q = (const bf16*)a.q + (long)p.img * a.q_img + at.t * a.q_ld + (p.g * a.rep + at.h) * a.q_head;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        v[j].x ^= flip;
-        v[j].y ^= flip;
-        v[j].z ^= flip;
-        v[j].w ^= flip;
-        qf[g][j] = __builtin_bit_cast(bf16x8, v[j]);
+        v[j] = make_uint4(0, 0, 0, 0);
+        if (lq < n && 16 * j + 8 * lh < d) v[j] = *(const uint4*)(Q + 16 * j + 8 * lh);
       }
     }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      v[j].x ^= flip;
+      v[j].y ^= flip;
+      v[j].z ^= flip;
+      v[j].w ^= flip;
+      qf[j] = __builtin_bit_cast(bf16x8, v[j]);
+    }
   };
-  bf16x8 qf[QG][NJ];
+  bf16x8 qf[NJ];
   load_q(r0, qf);
   if constexpr (SF)  // ones in channel d of every key of both buffers
     for (int i = tid; i < 2 * KT; i += NT) {
@@ -434,18 +433,15 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
       v[0] = (bf16)1.0f;
       *(bf16x8*)&Vs[i / KT][(i % KT) * LDV + d] = v;
     }
-  f32x16 o[QG][ND];  // (set by the first tile that holds a key)
-  float m_run[QG], l_run[QG];
+  f32x16 o[ND];  // (set by the first tile that holds a key)
+  float m_run, l_run;
   auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int g = 0; g < QG; ++g) {
+    for (int t = 0; t < ND; ++t)
 #pragma unroll
-      for (int t = 0; t < ND; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[g][t][r] = 0.f;
-      m_run[g] = -INFINITY;
-      l_run[g] = 0.f;
-    }
+      for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+    m_run = -INFINITY;
+    l_run = 0.f;
   };
 
   // A thread's pieces of a tile: keys pk + RPP i, channels pc on.  (Offsets past a
@@ -491,7 +487,7 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
     constexpr int NKT = decltype(nkt)::value;
     constexpr bool FIRST = decltype(first)::value;
     const bf16 *Kb = Ks[b], *Vb = Vs[b];
-    f32x16 s[QG][NKT];
+    f32x16 s[NKT];
 #pragma unroll
     for (int kt = 0; kt < NKT; ++kt) {
       // Keys that take no part start from -inf: one product of a column of 0
@@ -504,40 +500,27 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         const bf16x8 kf = *(const bf16x8*)&Kb[(kt * 32 + lq) * LDK + 16 * j + 8 * lh];
-#pragma unroll
-        for (int g = 0; g < QG; ++g) s[g][kt] = mfma32(kf, qf[g][j], j ? s[g][kt] : start);
+        s[kt] = mfma32(kf, qf[j], j ? s[kt] : start);
       }
     }
     // register r of half kt: key 32 kt + 8 (r / 4) + 4 lh + r % 4
-    float mt[QG];
-    bool any = false;
+    float v = s[0][0];
 #pragma unroll
-    for (int g = 0; g < QG; ++g) {
-      float v = s[g][0][0];
+    for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-      for (int kt = 0; kt < NKT; ++kt)
+      for (int r = 0; r < 16; ++r) v = fmaxf(v, s[kt][r]);
+    const float2 h = half_swap(v);
+    const float mt = fmaxf(h.x, h.y) * sl2;
+    const bool need = FIRST || mt > m_run + TAU;
+    if constexpr (FIRST) m_run = mt;
+    if (!FIRST && __any(need)) {  // (where a row's maximum stays, its sums are multiplied by one)
+      const float al = need ? __builtin_amdgcn_exp2f(m_run - mt) : 1.0f;
+      m_run = need ? mt : m_run;
+      l_run *= al;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) v = fmaxf(v, s[g][kt][r]);
-      const float2 h = half_swap(v);
-      mt[g] = fmaxf(h.x, h.y) * sl2;
-      if constexpr (FIRST)
-        m_run[g] = mt[g];
-      else
-        any = any || mt[g] > m_run[g] + TAU;
-    }
-    if (!FIRST && __any(any)) {
+      for (int t = 0; t < ND; ++t)
 #pragma unroll
-      for (int g = 0; g < QG; ++g) {
-        // (where a row's maximum stays, its sums are multiplied by one)
-        const bool need = mt[g] > m_run[g] + TAU;
-        const float al = need ? __builtin_amdgcn_exp2f(m_run[g] - mt[g]) : 1.0f;
-        m_run[g] = need ? mt[g] : m_run[g];
-        l_run[g] *= al;
-#pragma unroll
-        for (int t = 0; t < ND; ++t)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[g][t][r] *= al;
-      }
+        for (int r = 0; r < 16; ++r) o[t][r] *= al;
     }
     // O^T += V^T P^T, 16 keys at a time: slot (lh, i) of slice u is key 16 u +
     // 8 (i / 4) + 4 lh + i % 4, register 8 (u % 2) + i of half u / 2.  The
@@ -552,18 +535,15 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
         const bf16x4 lo = read_transposed(at), hi = read_transposed(at + 8 * LDV);
         vf[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
+      bf16x8 pf;
 #pragma unroll
-      for (int g = 0; g < QG; ++g) {
-        bf16x8 pf;
+      for (int i = 0; i < 8; ++i)
+        pf[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + i], sl2, -m_run));
+      if constexpr (!SF) l_run = sum_probs(pf, FIRST && u == 0 ? 0.f : l_run);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          pf[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[g][u >> 1][8 * (u & 1) + i], sl2, -m_run[g]));
-        if constexpr (!SF) l_run[g] = sum_probs(pf, FIRST && u == 0 ? 0.f : l_run[g]);
-#pragma unroll
-        for (int t = 0; t < ND; ++t) {
-          const f32x16 zero = {};
-          o[g][t] = mfma32(vf[t], pf, FIRST && u == 0 ? zero : o[g][t]);
-        }
+      for (int t = 0; t < ND; ++t) {
+        const f32x16 zero = {};
+        o[t] = mfma32(vf[t], pf, FIRST && u == 0 ? zero : o[t]);
       }
     }
   };
@@ -579,72 +559,69 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
   // O^T: lane holds channels 32 t + 8 (r / 4) + 4 lh + r % 4 of its row.
   auto finish = [&]() __attribute__((always_inline)) {
     if (!any_key) clear();
-#pragma unroll
-    for (int g = 0; g < QG; ++g) {
-      float l = l_run[g];
-      if constexpr (SF) {  // (d is a multiple of 8: register 0 of a quad of half 0)
-#pragma unroll
-        for (int t = 0; t < ND; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (32 * t + 8 * i == d) l = o[g][t][4 * i];
-        l = lh == 0 ? l : 0.f;
-      }
-      const float2 h = half_swap(l);
-      l = h.x + h.y;
-      const int r = r0 + 32 * g + lq;
-      if (!SHORT && splits > 1) {
-        if (r < rows) {
-          const Scratch sc = scratch_at(a, p.img, p.g, r, p.split, splits);
-#pragma unroll
-          for (int t = 0; t < ND; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int c = 32 * t + 8 * i + 4 * lh;
-              if (c < d) *(float4*)(sc.o + c) = make_float4(o[g][t][4 * i], o[g][t][4 * i + 1], o[g][t][4 * i + 2], o[g][t][4 * i + 3]);
-            }
-          if (lh == 0) {
-            sc.ml[0] = m_run[g];
-            sc.ml[1] = l;
-          }
-        }
-        continue;
-      }
-      // Rows are laid out in LDS (K's tiles are done with, unless SHORT) and leave 16 bytes a lane.
-      const float inv = l == 0.f ? 0.f : 1.0f / l;
-      bf16* R = (SHORT ? Os : &Ks[0][0]) + wave * 32 * LDK;
+    float l = l_run;
+    if constexpr (SF) {  // (d is a multiple of 8: register 0 of a quad of half 0)
 #pragma unroll
       for (int t = 0; t < ND; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c = 32 * t + 8 * i + 4 * lh;
-          if (c < d) {
-            bf16x4 w;
+        for (int i = 0; i < 4; ++i)
+          if (32 * t + 8 * i == d) l = o[t][4 * i];
+      l = lh == 0 ? l : 0.f;
+    }
+    const float2 h = half_swap(l);
+    l = h.x + h.y;
+    const int r = r0 + lq;
+    if (!SHORT && splits > 1) {
+      if (r < rows) {
+        const Scratch sc = scratch_at(a, p.img, p.g, r, p.split, splits);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = (bf16)(o[g][t][4 * i + e] * inv);
-            *(bf16x4*)(R + lq * LDK + c) = w;
+        for (int t = 0; t < ND; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int c = 32 * t + 8 * i + 4 * lh;
+            if (c < d) *(float4*)(sc.o + c) = make_float4(o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]);
           }
-        }
-      asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
-      const int rg = r0 + 32 * g, c = lane % LPR * 8, row0 = lane / LPR;
-      bf16* O = (bf16*)a.o + (long)p.img * a.o_img + p.g * a.rep * a.o_head + c;
-      if (c < d) {
-        if (a.rep == 1) {
-          O += (long)rg * a.o_ld;
-#pragma unroll
-          for (int i = 0; i < 32; i += 64 / LPR)
-            if (rg + row0 + i < rows) *(bf16x8*)(O + (row0 + i) * (int)a.o_ld) = *(const bf16x8*)(R + (row0 + i) * LDK + c);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; i += 64 / LPR)
-            if (rg + row0 + i < rows) {
-              const RowAt at = row_at(a, rg + row0 + i);
-              *(bf16x8*)(O + at.t * a.o_ld + at.h * a.o_head) = *(const bf16x8*)(R + (row0 + i) * LDK + c);
-            }
+        if (lh == 0) {
+          sc.ml[0] = m_run;
+          sc.ml[1] = l;
         }
       }
-      asm volatile("" ::: "memory");
+      return;
     }
+    // Rows are laid out in LDS (K's tiles are done with, unless SHORT) and leave 16 bytes a lane.
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    bf16* R = (SHORT ? Os : &Ks[0][0]) + wave * 32 * LDK;
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 32 * t + 8 * i + 4 * lh;
+        if (c < d) {
+          bf16x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = (bf16)(o[t][4 * i + e] * inv);
+          *(bf16x4*)(R + lq * LDK + c) = w;
+        }
+      }
+    asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
+    const int c = lane % LPR * 8, row0 = lane / LPR;
+    bf16* O = (bf16*)a.o + (long)p.img * a.o_img + p.g * a.rep * a.o_head + c;
+    if (c < d) {
+      if (a.rep == 1) {
+        O += (long)r0 * a.o_ld;
+#pragma unroll
+        for (int i = 0; i < 32; i += 64 / LPR)
+          if (r0 + row0 + i < rows) *(bf16x8*)(O + (row0 + i) * (int)a.o_ld) = *(const bf16x8*)(R + (row0 + i) * LDK + c);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; i += 64 / LPR)
+          if (r0 + row0 + i < rows) {
+            const RowAt at = row_at(a, r0 + row0 + i);
+            *(bf16x8*)(O + at.t * a.o_ld + at.h * a.o_head) = *(const bf16x8*)(R + (row0 + i) * LDK + c);
+          }
+      }
+    }
+    asm volatile("" ::: "memory");
   };
 
   if constexpr (SHORT) {
@@ -657,23 +634,18 @@ __global__ __launch_bounds__(64 * NW, SHORT ? (D16 <= 64 ? 3 : D16 <= 96 ? 2 : 1
     }
     __syncthreads();
     for (int it = 0; it < passes; ++it) {
-      bf16x8 qn[QG][NJ] = {};
+      bf16x8 qn[NJ];
       const int rn = r0 + NW * 32;
       if (it + 1 < passes && rn < rows) load_q(rn, qn);
       if (r0 < rows) {
         const int bf = b0 ? 0 : 1;  // (the first tile that holds a key)
         tile_of(std::true_type{}, bf, b0 ? b0 : b1);
         if (b0) tile_of(std::false_type{}, 1, b1);
-        // The next rows' queries have landed before this group's stores are
-        // issued: waiting for them later would wait for the stores as well
-        // (one counter, and the compiler cannot count stores under branches).
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(qn[0][j]));
         finish();
       }
       if (it + 1 < passes) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) qf[0][j] = qn[0][j];
+        for (int j = 0; j < NJ; ++j) qf[j] = qn[j];
         r0 = rn;
       }
     }
@@ -931,10 +903,10 @@ __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) {
 }
 }  // namespace
 
-template <int D32, int NW>
-__global__ __launch_bounds__(64 * NW, D32 <= 64 ? 2 : 1) void cross_f32_kernel(CrossArgs a, int keys, int tiles, int splits,
+template <int D32>
+__global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void cross_f32_kernel(CrossArgs a, int keys, int tiles, int splits,
                                                                                int together) {
-  constexpr int NI = D32 / 8, ND = D32 / 32, NT = 64 * NW, LDK = D32 + 4, LDV = D32 + 8;  // (rows apart by banks)
+  constexpr int NW = 4, NI = D32 / 8, ND = D32 / 32, NT = 64 * NW, LDK = D32 + 4, LDV = D32 + 8;  // (rows apart by banks)
   constexpr int CPT = FT * (D32 / 4) / NT;
   __shared__ __attribute__((aligned(16))) float Ks[2][FT * LDK];
   __shared__ __attribute__((aligned(16))) float Vs[2][FT * LDV];
@@ -1218,34 +1190,25 @@ __global__ __launch_bounds__(64 * NW) void cross_keys_f32_kernel(CrossArgs a, in
 }
 
 // ------------------------------------------------------------------ launch
-template <typename T, int RB>
+template <int RB>
 static void launch_few(const CrossArgs& a, const Plan& p, hipStream_t s) {
   const unsigned grid = place_blocks(a.kv_heads, 1, p.splits, a.n, 0);
   if (a.d <= 32)
-    cross_few_kernel<T, RB, 4><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
+    cross_few_kernel<RB, 4><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
   else if (a.d <= 64)
-    cross_few_kernel<T, RB, 8><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
+    cross_few_kernel<RB, 8><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
   else if (a.d <= 128)
-    cross_few_kernel<T, RB, 16><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
+    cross_few_kernel<RB, 16><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
   else
-    cross_few_kernel<T, RB, 32><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
+    cross_few_kernel<RB, 32><<<grid, 512, 0, s>>>(a, p.keys, p.splits);
 }
 
-template <typename T>
-static void launch_few_rows(const CrossArgs& a, const Plan& p, hipStream_t s) {
-  const int rows = a.rep * a.n_q;
-  if (rows == 1) launch_few<T, 1>(a, p, s);
-  else if (rows == 2) launch_few<T, 2>(a, p, s);
-  else if (rows <= 4) launch_few<T, 4>(a, p, s);
-  else launch_few<T, 8>(a, p, s);
-}
-
-template <int D16, bool SF, int NW, int QG>
+template <int D16, bool SF>
 static void launch_bf16(const CrossArgs& a, const Plan& p, hipStream_t s) {
   const long rows = (long)a.rep * a.n_q;
-  const int tiles = (int)((rows + 32 * NW * QG - 1) / (32 * NW * QG));
+  const int tiles = (int)((rows + 127) / 128);
   const int together = place_together(a, 2);
-  cross_bf16_kernel<D16, SF, NW, QG, false><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 64 * NW, 0, s>>>(
+  cross_bf16_kernel<D16, SF, false><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 256, 0, s>>>(
       a, p.keys, tiles, p.splits, 1, together);
 }
 
@@ -1261,15 +1224,14 @@ static void launch_sum(const CrossArgs& a, const Plan& p, hipStream_t s) {
   }
   if constexpr (D16 <= 128)  // (wider heads' tiles leave no LDS for the output rows)
     if (a.max_len <= 2 * KT) {
-      constexpr int NW = 4;
       // up to 8 groups of rows per wave, as long as some 1000 blocks remain
-      const long groups = (rows + 32 * NW - 1) / (32 * NW), all = groups * a.kv_heads * a.n;
+      const long groups = (rows + 127) / 128, all = groups * a.kv_heads * a.n;
       const int passes = (int)(all / 1024 < 1 ? 1 : all / 1024 > 8 ? 8 : all / 1024);
       const int tiles = (int)((groups + passes - 1) / passes);
-      cross_bf16_kernel<D16, SF, NW, 1, true><<<place_blocks(a.kv_heads, tiles, 1, a.n, 0), 64 * NW, 0, s>>>(a, 0, tiles, 1, passes, 0);
+      cross_bf16_kernel<D16, SF, true><<<place_blocks(a.kv_heads, tiles, 1, a.n, 0), 256, 0, s>>>(a, 0, tiles, 1, passes, 0);
       return;
     }
-  launch_bf16<D16, SF, 4, 1>(a, p, s);
+  launch_bf16<D16, SF>(a, p, s);
 }
 
 template <int D16>
@@ -1290,7 +1252,7 @@ static void launch_f32(const CrossArgs& a, const Plan& p, hipStream_t s) {
     cross_keys_f32_kernel<D32, NW><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits, together);
   } else {
     const int tiles = (int)((rows + 127) / 128);
-    cross_f32_kernel<D32, 4><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 256, 0, s>>>(a, p.keys, tiles, p.splits, together);
+    cross_f32_kernel<D32><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 256, 0, s>>>(a, p.keys, tiles, p.splits, together);
   }
 }
 
@@ -1313,7 +1275,8 @@ hipError_t launch_cross_attention(DType dt, CrossArgs a, hipStream_t s) {
     a.rep_shift = l - 1;
   }
   if (p.kind == 0 && dt != BF16) {
-    launch_few_rows<float>(a, p, s);
+    const long r = rows;
+    r == 1 ? launch_few<1>(a, p, s) : r == 2 ? launch_few<2>(a, p, s) : r <= 4 ? launch_few<4>(a, p, s) : launch_few<8>(a, p, s);
   } else if (dt == BF16) {
     if (a.d <= 32) launch_width<32>(a, p, s);
     else if (a.d <= 48) launch_width<48>(a, p, s);

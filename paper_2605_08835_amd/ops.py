@@ -134,42 +134,46 @@ def groupnorm_stats_noalloc(x0, groups, eps, gamma, beta, x1=None, scale=None, s
 
 # Operators on texts of their own lengths and on few-bit weights.  Their
 # tensors may live on any one device: the call runs there, on that device's
-# current stream.
+# current stream.  (A call takes about 8 us on the host, 4 of them the launch;
+# the checks are written for that: no message is built unless it is raised.)
 _TYPE = {torch.float32: SD_F32, torch.bfloat16: SD_BF16, torch.float8_e4m3fn: SD_E4M3}
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
-def _enqueue(fn, like, args, others):
+def _bad(what):
+    raise ValueError(what)
+
+
+def _enqueue(fn, like, others, args):
     """fn(*args, stream) on the device of `like`, which the tensors `others` (or
     None) share.  (The raw-stream and device queries cost 0.2 us together, the
-    public ones 3, of a call of about 8.)"""
+    public ones 3.)"""
     dev = like.get_device()
     for t in others:
         if t is not None and t.get_device() != dev:
-            raise ValueError(f"tensors on {like.device} and {t.device}")
+            _bad(f"tensors on {like.device} and {t.device}")
     if dev < 0:
-        raise ValueError(f"tensors on {like.device}: the kernels run on the GPU")
+        _bad(f"tensors on {like.device}: the kernels run on the GPU")
     stream = torch._C._cuda_getCurrentRawStream(dev)
     if dev == torch._C._cuda_getDevice():
-        _check(fn(*args, stream))
+        status = fn(*args, stream)
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, stream))
+            status = fn(*args, stream)
+    if status:
+        _check(status)
 
 
 def _row_stride(t, what):
     """Distance between the rows (last axis) of t, whose rows lie evenly."""
-    if t.dim() == 2:
-        rows, c = t.shape
-        s0, s1 = t.stride()
-        _need(s1 == 1 or c == 1, f"{what}: the last axis must be contiguous")
-        return s0 if rows > 1 else c
-    _need(t.dim() >= 1 and t.is_contiguous(), f"{what}: more than two axes must be contiguous")
-    return t.shape[-1]
+    if t.is_contiguous():
+        return t.shape[-1]
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
+        _bad(f"{what}: the last axis must be contiguous, and more than two axes all of them")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def rmsnorm(x, gamma=None, eps=1e-6, resid=None, sum_out=None, out=None, fp8=False, scale_group=0):
@@ -178,41 +182,44 @@ def rmsnorm(x, gamma=None, eps=1e-6, resid=None, sum_out=None, out=None, fp8=Fal
     Returns y, or (y, h) with a residual (h rounded to x's type, into sum_out
     when given).  fp8: y is float8_e4m3fn and fp32 scales [..., C / 128 rounded
     up] (scale_group = 128) or [..., 1] (scale_group = 0) follow it, y ~ y8 *
-    scale.  sum_out may be x or resid, out (not fp8) likewise, but not both the same."""
-    if x.dtype is not torch.bfloat16 and x.dtype is not torch.float32:
-        raise TypeError(x.dtype)
-    C = x.shape[-1]
-    rows = x.numel() // C if C else 0
+    scale.  sum_out may be x or resid, and so may out (not with fp8), but not
+    both the same one."""
+    dt = x.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise TypeError(dt)
+    shape = x.shape
+    C = shape[-1] if shape else _bad("x must have rows")
     x_ld = _row_stride(x, "x")
-    y_type = torch.float8_e4m3fn if fp8 else x.dtype
+    r_ld = s_ld = 0
     if resid is not None:
-        _need(resid.shape == x.shape and resid.dtype is x.dtype, "resid has another shape or type than x")
+        if resid.shape != shape or resid.dtype is not dt:
+            _bad("resid has another shape or type than x")
+        r_ld = _row_stride(resid, "resid")
         if sum_out is None:
             sum_out = torch.empty_like(x)
-        else:
-            _need(sum_out.shape == x.shape and sum_out.dtype is x.dtype, "sum_out has another shape or type than x")
-    else:
-        _need(sum_out is None, "sum_out without resid")
-    if gamma is not None:
-        _need(gamma.dtype is torch.float32 and gamma.shape == (C,) and gamma.is_contiguous(), "gamma must be fp32 [C]")
-    _need(scale_group in (0, 128) and (fp8 or not scale_group), "scale_group is 0 or 128, and 128 only with fp8")
+        elif sum_out.shape != shape or sum_out.dtype is not dt:
+            _bad("sum_out has another shape or type than x")
+        s_ld = _row_stride(sum_out, "sum_out")
+    elif sum_out is not None:
+        _bad("sum_out without resid")
+    if gamma is not None and (gamma.dtype is not torch.float32 or gamma.shape != (C,) or not gamma.is_contiguous()):
+        _bad("gamma must be fp32 [C]")
+    if scale_group and (scale_group != 128 or not fp8):
+        _bad("scale_group is 0 or 128, and 128 only with fp8")
+    y_type = torch.float8_e4m3fn if fp8 else dt
     if out is None:
         out = torch.empty_like(x, dtype=y_type) if fp8 else torch.empty_like(x)
-    else:
-        _need(out.shape == x.shape and out.dtype is y_type, "out has another shape or type than the result")
+    elif out.shape != shape or out.dtype is not y_type:
+        _bad("out has another shape or type than the result")
     scale = None
     if fp8:
-        blocks = -(-C // 128) if scale_group else 1
-        scale = x.new_empty(x.shape[:-1] + (blocks,), dtype=torch.float32)
-    _enqueue(lib().synerdiff_op_rmsnorm, x,
-             (_TYPE[x.dtype], x.data_ptr(), x_ld, _ptr(resid), 0 if resid is None else _row_stride(resid, "resid"),
-              _ptr(sum_out), 0 if sum_out is None else _row_stride(sum_out, "sum_out"), _ptr(gamma), float(eps), rows, C,
-              _TYPE[y_type], out.data_ptr(), _row_stride(out, "out"), _ptr(scale), scale_group),
-             (resid, sum_out, gamma, out))
-    got = (out, scale) if fp8 else (out,)
-    if resid is not None:
-        got += (sum_out,)
-    return got if len(got) > 1 else out
+        scale = x.new_empty(shape[:-1] + ((C + 127) // 128 if scale_group else 1,), dtype=torch.float32)
+    _enqueue(lib().synerdiff_op_rmsnorm, x, (resid, sum_out, gamma, out),
+             (_TYPE[dt], x.data_ptr(), x_ld, _at(resid), r_ld, _at(sum_out), s_ld, _at(gamma), eps,
+              x.numel() // C if C else 0, C, _TYPE[y_type], out.data_ptr(), _row_stride(out, "out"), _at(scale), scale_group))
+    if resid is None:
+        return (out, scale) if fp8 else out
+    return (out, scale, sum_out) if fp8 else (out, sum_out)
 
 
 def linear_rows_w4(x, w, scale, group, zero=None, x_scale=None, bias=None, add=None, silu_in=0, silu_out=0,
@@ -223,44 +230,51 @@ def linear_rows_w4(x, w, scale, group, zero=None, x_scale=None, bias=None, add=N
     up], zero uint8 of that shape or None (8), weight = scale * (code - zero).
     bias fp32 [N] and add fp32 [M, N] are added, silu_in / silu_out as in
     linear_rows; returns [M, N] in out_dtype (fp32 or bf16)."""
-    t = _TYPE.get(x.dtype)
-    if t is None:
-        raise TypeError(x.dtype)
-    if scale.dtype is not torch.float32 and scale.dtype is not torch.bfloat16:
-        raise TypeError(scale.dtype)
-    if out_dtype is not torch.float32 and out_dtype is not torch.bfloat16:
-        raise TypeError(out_dtype)
-    _need(x.dim() == 2 and w.dim() == 2 and w.dtype is torch.uint8, "x must be [M, K], w uint8 [N, K / 2]")
+    t, st, ot = _TYPE.get(x.dtype), _TYPE.get(scale.dtype), _TYPE.get(out_dtype)
+    if t is None or st not in (SD_F32, SD_BF16) or ot not in (SD_F32, SD_BF16):
+        raise TypeError((x.dtype, scale.dtype, out_dtype))
+    if x.dim() != 2 or w.dim() != 2 or w.dtype is not torch.uint8:
+        _bad("x must be [M, K], w uint8 [N, K / 2]")
     M, K = x.shape
-    N = w.shape[0]
-    _need(group in (32, 64, 128), "group must be 32, 64 or 128")
-    _need(K > 0 and K % 8 == 0 and w.shape[1] * 2 == K and w.is_contiguous(), "w must be [N, K / 2], contiguous, K a multiple of 8")
-    shape = (N, -(-K // group))
-    _need(scale.shape == shape and scale.is_contiguous(), "scale must be [N, K / group rounded up], contiguous")
-    if zero is not None:
-        _need(zero.dtype is torch.uint8 and zero.shape == shape and zero.is_contiguous(), "zero must be uint8 of scale's shape")
+    N, half = w.shape
+    if group != 128 and group != 64 and group != 32:
+        _bad("group must be 32, 64 or 128")
+    if K == 0 or K % 8 or half * 2 != K or not w.is_contiguous():
+        _bad("w must be [N, K / 2], contiguous, K a multiple of 8")
+    shape = (N, (K + group - 1) // group)
+    if scale.shape != shape or not scale.is_contiguous():
+        _bad("scale must be [N, K / group rounded up], contiguous")
+    if zero is not None and (zero.dtype is not torch.uint8 or zero.shape != shape or not zero.is_contiguous()):
+        _bad("zero must be uint8 of scale's shape")
     x_group = 0
     if t == SD_E4M3:
-        _need(x_scale is not None and x_scale.dtype is torch.float32 and x_scale.is_contiguous() and x_scale.dim() == 2 and
-              x_scale.shape[0] == M and x_scale.shape[1] in (1, -(-K // 128)),
-              "e4m3 rows need x_scale fp32 [M, 1] or [M, K / 128 rounded up]")
+        blocks = (K + 127) // 128
+        if x_scale is None or x_scale.dtype is not torch.float32 or not x_scale.is_contiguous() or (
+                x_scale.shape != (M, 1) and x_scale.shape != (M, blocks)):
+            _bad("e4m3 rows need x_scale fp32 [M, 1] or [M, K / 128 rounded up]")
         x_group = 128 if x_scale.shape[1] > 1 else 0
-    else:
-        _need(x_scale is None, "x_scale belongs to e4m3 rows")
-    if bias is not None:
-        _need(bias.dtype is torch.float32 and bias.shape == (N,) and bias.is_contiguous(), "bias must be fp32 [N]")
-    if add is not None:
-        _need(add.dtype is torch.float32 and add.shape == (M, N) and add.is_contiguous(), "add must be fp32 [M, N]")
+    elif x_scale is not None:
+        _bad("x_scale belongs to e4m3 rows")
+    if bias is not None and (bias.dtype is not torch.float32 or bias.shape != (N,) or not bias.is_contiguous()):
+        _bad("bias must be fp32 [N]")
+    if add is not None and (add.dtype is not torch.float32 or add.shape != (M, N) or not add.is_contiguous()):
+        _bad("add must be fp32 [M, N]")
     if out is None:
-        out = x.new_empty((M, N), dtype=out_dtype)
+        out, out_ld = x.new_empty((M, N), dtype=out_dtype), N
     else:
-        _need(out.shape == (M, N) and out.dtype is out_dtype, "out has another shape or type than the result")
-    _enqueue(lib().synerdiff_op_linear_rows_w4, x,
-             (t, x.data_ptr(), _row_stride(x, "x"), _ptr(x_scale), x_group, M, K, w.data_ptr(), group,
-              _TYPE[scale.dtype], scale.data_ptr(), _ptr(zero), _ptr(bias), _ptr(add), 1 if silu_in else 0,
-              1 if silu_out else 0, _TYPE[out_dtype], out.data_ptr(), _row_stride(out, "out"), N),
-             (w, scale, zero, x_scale, bias, add, out))
+        if out.shape != (M, N) or out.dtype is not out_dtype:
+            _bad("out has another shape or type than the result")
+        out_ld = _row_stride(out, "out")
+    _enqueue(lib().synerdiff_op_linear_rows_w4, x, (w, scale, zero, x_scale, bias, add, out),
+             (t, x.data_ptr(), _row_stride(x, "x"), _at(x_scale), x_group, M, K, w.data_ptr(), group, st, scale.data_ptr(),
+              _at(zero), _at(bias), _at(add), 1 if silu_in else 0, 1 if silu_out else 0, ot, out.data_ptr(), out_ld, N))
     return out
+
+
+def _index(a, length, name):
+    if a.dtype is not torch.int32 or a.shape != (length,) or not a.is_contiguous():
+        _bad(f"{name} must be int32 [{length}]")
+    return a.data_ptr()
 
 
 def cross_attention(q, k, v, max_len, kv_start=None, kv_len=None, kv_index=None, mask=None, scale=None, out=None):
@@ -274,42 +288,49 @@ def cross_attention(q, k, v, max_len, kv_start=None, kv_len=None, kv_index=None,
     v and out may be strided as long as d is contiguous.  scale defaults to
     1 / sqrt(d).  A row without keys gives zeros.  Returns [n, n_q, heads, d]
     in q's type."""
-    if q.dtype is not torch.bfloat16 and q.dtype is not torch.float32:
-        raise TypeError(q.dtype)
-    _need(q.dim() == 4 and k.dim() == (4 if kv_start is None else 3), "q [n, n_q, heads, d]; k, v [tokens, kv_heads, d] "
-          "with kv_start, [n_ctx, max_len, kv_heads, d] without")
+    dt = q.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise TypeError(dt)
+    packed = kv_start is not None
+    ks = k.stride()
+    if q.dim() != 4 or len(ks) != (3 if packed else 4):
+        _bad("q [n, n_q, heads, d]; k, v [tokens, kv_heads, d] with kv_start, [n_ctx, max_len, kv_heads, d] without")
     n, n_q, heads, d = q.shape
-    _need(k.dtype is q.dtype and v.dtype is q.dtype and k.shape == v.shape and k.shape[-1] == d,
-          "k and v must have q's type and width, and one shape")
-    kv_heads = k.shape[-2]
-    qs, ks, vs = q.stride(), k.stride(), v.stride()
-    _need(d == 1 or qs[3] == ks[-1] == vs[-1] == 1, "d must be contiguous")
-    if kv_start is None:
-        n_ctx, tokens = k.shape[0], 0
-        _need(k.shape[1] == max_len, "padded k, v must be [n_ctx, max_len, kv_heads, d]")
-        k_ctx, v_ctx = ks[0], vs[0]
+    kshape = k.shape
+    if k.dtype is not dt or v.dtype is not dt or kshape != v.shape or kshape[-1] != d:
+        _bad("k and v must have q's type and width, and one shape")
+    kv_heads = kshape[-2]
+    qs, vs = q.stride(), v.stride()
+    if d > 1 and (qs[3] != 1 or ks[-1] != 1 or vs[-1] != 1):
+        _bad("d must be contiguous")
+    if packed:
+        n_ctx, tokens, k_ctx, v_ctx = kv_start.shape[0], kshape[0], 0, 0
+        if kv_len is None:
+            _bad("packed texts need kv_len")
     else:
-        n_ctx, tokens, k_ctx, v_ctx = kv_start.shape[0], k.shape[0], 0, 0
-        _need(kv_len is not None, "packed texts need kv_len")
-    for a, length, name in ((kv_start, n_ctx, "kv_start"), (kv_len, n_ctx, "kv_len"), (kv_index, n, "kv_index")):
-        if a is not None:
-            _need(a.dtype is torch.int32 and a.shape == (length,) and a.is_contiguous(), f"{name} must be int32 [{length}]")
-    if mask is not None:
-        _need(mask.dtype in (torch.bool, torch.uint8) and mask.shape == k.shape[:-2] and mask.is_contiguous(),
-              "mask must be bool or uint8, one value per token")
+        n_ctx, tokens, k_ctx, v_ctx = kshape[0], 0, ks[0], vs[0]
+        if kshape[1] != max_len:
+            _bad("padded k, v must be [n_ctx, max_len, kv_heads, d]")
+    start_p = _index(kv_start, n_ctx, "kv_start") if packed else None
+    len_p = _index(kv_len, n_ctx, "kv_len") if kv_len is not None else None
+    index_p = _index(kv_index, n, "kv_index") if kv_index is not None else None
+    if mask is not None and ((mask.dtype is not torch.bool and mask.dtype is not torch.uint8) or mask.shape != kshape[:-2]
+                             or not mask.is_contiguous()):
+        _bad("mask must be bool or uint8, one value per token")
     if out is None:
-        out = q.new_empty((n, n_q, heads, d))
-        os = (n_q * heads * d, heads * d, d)
+        out, os = q.new_empty((n, n_q, heads, d)), (n_q * heads * d, heads * d, d)
     else:
-        _need(out.shape == q.shape and out.dtype is q.dtype and out.stride(3) == 1, "out must have q's shape and type, d contiguous")
         os = out.stride()
-    L, t = lib(), _TYPE[q.dtype]
-    floats = L.synerdiff_op_cross_attention_scratch_floats(t, n, heads, kv_heads, d, n_q, max_len)
-    scratch = q.new_empty(floats, dtype=torch.float32) if floats > 0 else None
-    _enqueue(L.synerdiff_op_cross_attention, q,
+        if out.shape != q.shape or out.dtype is not dt or (d > 1 and os[3] != 1):
+            _bad("out must have q's shape and type, d contiguous")
+    L, t = lib(), _TYPE[dt]
+    floats, scratch = 0, None
+    if max_len > 512:  # (no shorter text is split)
+        floats = L.synerdiff_op_cross_attention_scratch_floats(t, n, heads, kv_heads, d, n_q, max_len)
+        if floats > 0:
+            scratch = q.new_empty(floats, dtype=torch.float32)
+    _enqueue(L.synerdiff_op_cross_attention, q, (k, v, kv_start, kv_len, kv_index, mask, out),
              (t, q.data_ptr(), qs[1], qs[2], qs[0], k.data_ptr(), ks[-3], ks[-2], k_ctx, v.data_ptr(), vs[-3], vs[-2],
-              v_ctx, tokens, n_ctx, max_len, _ptr(kv_start), _ptr(kv_len), _ptr(kv_index), _ptr(mask), out.data_ptr(),
-              os[1], os[2], os[0], n, heads, kv_heads, d, n_q, d ** -0.5 if scale is None else float(scale),
-              _ptr(scratch), floats),
-             (k, v, kv_start, kv_len, kv_index, mask, out))
+              v_ctx, tokens, n_ctx, max_len, start_p, len_p, index_p, _at(mask), out.data_ptr(), os[1], os[2], os[0], n,
+              heads, kv_heads, d, n_q, d ** -0.5 if scale is None else scale, _at(scratch), floats))
     return out
