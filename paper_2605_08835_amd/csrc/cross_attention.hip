@@ -843,15 +843,21 @@ __global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      bf16x8 pf;
+      // (as bf16 plus the rest as bf16, 2^-17 of each: these products have time to spare)
+      bf16x8 pf, pr;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) pf[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[8 * u + i], sl2, -m_run));
-      if constexpr (!SF) l_run = sum_probs(pf, l_run);
+      for (int i = 0; i < 8; ++i) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * u + i], sl2, -m_run));
+        if constexpr (!SF) l_run += x;
+        pf[i] = (bf16)x;
+        pr[i] = (bf16)(x - (float)pf[i]);
+      }
 #pragma unroll
       for (int t = 0; t < ND; ++t) {
         const bf16* at = &Vs[(16 * u + 4 * lh + ((lane & 15) >> 2)) * LDV + t * 32 + (lane & 16) + 4 * (lane & 3)];
         const bf16x4 lo = read_transposed(at), hi = read_transposed(at + 8 * LDV);
-        o[t] = mfma32(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), pf, o[t]);
+        const bf16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        o[t] = mfma32(vf, pf, mfma32(vf, pr, o[t]));
       }
     }
     asm volatile("" ::: "memory");
