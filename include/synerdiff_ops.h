@@ -221,7 +221,7 @@ sd_status synerdiff_op_rmsnorm(int32_t dtype, const void* d_x, int64_t x_ld, con
  * fp32 [M, N], may be NULL; add may equal an fp32 out of out_ld = N; out
  * overlaps nothing else.  Products and sums are fp32-accurate for every
  * x_type.  A row of x with an infinity or NaN gives no finite value.
- * K a multiple of 8, x_ld <= 2^24, M <= 2^20; x and its rows 16-byte aligned (e4m3: 8).  The rows of a
+ * K a multiple of 8, x_ld and N <= 2^24, M <= 2^19; x and its rows 16-byte aligned (e4m3: 8).  The rows of a
  * result do not depend on M.  M = 0 or N = 0 does nothing. */
 sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* d_x, int64_t x_ld, const float* d_x_scale,
                                       int32_t x_group, int32_t M, int32_t K, const uint8_t* d_w, int32_t group,
@@ -243,10 +243,11 @@ sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* d_x, int64_t x
  * outside [0, kv_tokens) is empty, one that ends past it is cut there.  Padded contexts (d_kv_start NULL): k + c * k_ctx + j *
  * k_ld + g * k_head + e, and mask byte c * max_len + j.  v likewise.  A
  * kv_len past max_len counts as max_len, a negative one as 0.  Strides in
- * elements, not negative (0 for a shared head).
+ * elements, not negative (0 for a shared head; that of an axis of one element
+ * is not looked at).
  * Constraints: d a multiple of 8, <= 256; heads a multiple of kv_heads, <=
- * 2^16; max_len <= 2^30; q_ld, k_ld, v_ld, o_ld <= 2^23; n * n_q * heads (times the
- * splits) <= 2 * 10^9; q, k, v, o and all their strides at multiples of 16
+ * 2^16; max_len <= 2^30; q_ld, k_ld, v_ld, o_ld <= 2^23; a grid of less than 2^32
+ * threads (a block of 512 per 32 rows of a K/V head and split); q, k, v, o and all their strides at multiples of 16
  * bytes.  o overlaps nothing.  Few queries over long texts are split along the keys: d_scratch
  * (fp32, 16-byte aligned) has to hold synerdiff_op_cross_attention_scratch_floats(...) floats
  * then (SD_ERR_WORKSPACE if smaller; 0 = none needed), and belongs to this call

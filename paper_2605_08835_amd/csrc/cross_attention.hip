@@ -460,8 +460,8 @@ __global__ __launch_bounds__(256, D16 <= 48 || (D16 == 64 && !SHORT) ? 3 : D16 <
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
       const bool on = (b >> (RPP * i & 63)) & 1;
-      rk[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(kr, on ? ko : OOB, i * RPP * (int)a.k_ld * 2, 0));
-      rv[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(vr, on ? vo : OOB, i * RPP * (int)a.v_ld * 2, 0));
+      rk[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(kr, on ? ko + i * RPP * (int)a.k_ld * 2 : OOB, 0, 0));
+      rv[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(vr, on ? vo + i * RPP * (int)a.v_ld * 2 : OOB, 0, 0));
     }
   };
   auto stage = [&](int b) __attribute__((always_inline)) {
@@ -762,8 +762,8 @@ __global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
       const bool on = bits >> pk >> (RPP * i) & 1;
-      rk[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(kr, on ? ko : OOB, i * RPP * (int)a.k_ld * 2, 0));
-      rv[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(vr, on ? vo : OOB, i * RPP * (int)a.v_ld * 2, 0));
+      rk[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(kr, on ? ko + i * RPP * (int)a.k_ld * 2 : OOB, 0, 0));
+      rv[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(vr, on ? vo + i * RPP * (int)a.v_ld * 2 : OOB, 0, 0));
     }
   };
   auto own_key = [&](int k0) -> bool {
@@ -1264,8 +1264,10 @@ static void launch_f32(const CrossArgs& a, const Plan& p, hipStream_t s) {
 
 long cross_attention_scratch_floats(DType dt, int n, int heads, int kv_heads, int d, int n_q, int max_len) {
   const Plan p = plan_of(heads / kv_heads, n_q, max_len);
-  const double rows = (double)heads * n_q * n;
-  if (rows * p.splits > 2.0e9 || (double)heads / kv_heads * n_q > 2.0e9) return -1;  // (grids and row indices are 32 bits)
+  // (a grid holds less than 2^32 threads: blocks of at most 512 per 32 rows of a K/V head and split, in eights, and joins of 64 a row)
+  const double rows = (double)heads * n_q * n, tiles = (double)heads / kv_heads * n_q / 32 + 1;
+  const double blocks = ((double)n * kv_heads + 8) * tiles * p.splits, shared = (tiles * p.splits * n + 8) * kv_heads;
+  if (blocks * 512 > 4.0e9 || shared * 512 > 4.0e9 || (p.splits > 1 && rows * 64 > 4.0e9)) return -1;
   return p.splits > 1 ? (long)rows * p.splits * (d + 2) : 0;
 }
 

@@ -361,6 +361,11 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
   // half h of chunk c
   auto load_x = [&](int c, int h, u32x4 (&x)[2][2]) __attribute__((always_inline)) {
     const int k = c * KC + h * HC;
+    if (k >= a.K) {  // (no offset past the rows, not even with lanes switched off)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) x[i][0] = x[i][1] = u32x4{0, 0, 0, 0};
+      return;
+    }
     const int at = k + 8 * (lane & 7) < a.K ? xoff : OOB;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {

@@ -331,7 +331,8 @@ sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* x, int64_t x_l
   if (x_type == SD_E4M3 ? x_group != 0 && x_group != 128 : x_scale || x_group)
     return op_fail(SD_ERR_INVALID_ARG, "x_group is 0 or 128, x scales only with e4m3 rows");
   if (x_type == SD_E4M3 && silu_in) return op_fail(SD_ERR_UNSUPPORTED, "silu_in on e4m3 rows");
-  if (M > 1 << 20 || K > 1 << 24) return op_fail(SD_ERR_UNSUPPORTED, "more than 2^20 rows or 2^24 columns");
+  if (M > 1 << 19 || K > 1 << 24 || N > 1 << 24)
+    return op_fail(SD_ERR_UNSUPPORTED, "more than 2^19 rows or 2^24 columns");
   if (M == 0 || N == 0) return SD_OK;
   if (!x || !w || !scale || !out || (x_type == SD_E4M3 && !x_scale)) return op_fail(SD_ERR_INVALID_ARG, "NULL argument");
   if (x_ld < K || out_ld < N) return op_fail(SD_ERR_INVALID_ARG, "a row stride is below its row");
@@ -377,16 +378,23 @@ sd_status synerdiff_op_cross_attention(int32_t dtype, const void* q, int64_t q_l
   if (bad_dtype(dtype)) return op_fail(SD_ERR_INVALID_ARG, "bad dtype");
   if (!cross_shape_ok(dtype, n, heads, kv_heads, d, n_q, max_len))
     return op_fail(d > 256 ? SD_ERR_UNSUPPORTED : SD_ERR_INVALID_ARG, "bad shape (d a multiple of 8 up to 256, heads of kv_heads)");
-  if (heads > 1 << 16 || max_len > 1 << 30 || q_ld > 1 << 23 || k_ld > 1 << 23 || v_ld > 1 << 23 || o_ld > 1 << 23)
-    return op_fail(SD_ERR_UNSUPPORTED, "more than 2^16 heads, 2^30 keys or 2^23 elements from token to token");
+  if (heads > 1 << 16 || max_len > 1 << 30) return op_fail(SD_ERR_UNSUPPORTED, "more than 2^16 heads or 2^30 keys");
   if (n_ctx < 0 || kv_tokens < 0 || kv_tokens > 0x7FFFFFFF) return op_fail(SD_ERR_INVALID_ARG, "bad context count or length");
   if (!kv_index && n_ctx < n) return op_fail(SD_ERR_INVALID_ARG, "fewer contexts than rows");
   if (!(scale == scale) || scale - scale != 0.f) return op_fail(SD_ERR_INVALID_ARG, "scale must be finite");
   if (n == 0 || n_q == 0) return SD_OK;
+  // (the stride of an axis of one element may hold anything)
+  if (n_q == 1) q_ld = o_ld = 0;
+  if (heads == 1) q_head = o_head = 0;
+  if (n == 1) q_img = o_img = 0;
+  if (kv_heads == 1) k_head = v_head = 0;
+  if (n_ctx == 1 || kv_start) k_ctx = v_ctx = 0;
+  if ((kv_start ? kv_tokens : max_len) == 1) k_ld = v_ld = 0;
+  if (q_ld > 1 << 23 || k_ld > 1 << 23 || v_ld > 1 << 23 || o_ld > 1 << 23)
+    return op_fail(SD_ERR_UNSUPPORTED, "more than 2^23 elements from token to token");
   const bool keys = n_ctx > 0 && max_len > 0 && (!kv_start || kv_tokens > 0);
   if (!q || !o || (keys && (!k || !v))) return op_fail(SD_ERR_INVALID_ARG, "NULL argument");
-  const int64_t strides[] = {q_ld, q_head, q_img, k_ld, k_head, kv_start ? 0 : k_ctx, v_ld, v_head,
-                             kv_start ? 0 : v_ctx, o_ld, o_head, o_img};
+  const int64_t strides[] = {q_ld, q_head, q_img, k_ld, k_head, k_ctx, v_ld, v_head, v_ctx, o_ld, o_head, o_img};
   const int64_t piece = dtype == SD_BF16 ? 8 : 4;
   for (int64_t s : strides)
     if (s < 0 || s % piece) return op_fail(SD_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");

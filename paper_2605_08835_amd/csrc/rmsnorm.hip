@@ -305,10 +305,21 @@ hipError_t launch_rmsnorm(DType dt, const RmsNormArgs& a, hipStream_t s) {
                          (uint64_t)((a.resid ? a.resid_ld : 0) * el) | (uint64_t)((a.sum ? a.sum_ld : 0) * el);
   const uint64_t yp = (uint64_t)a.y | (uint64_t)(a.y_ld * yel);
   const bool any = a.C % 8 != 0 || (piece & 15) || (yp & (a.y8 ? 7 : 15));
-  if (dt == BF16)
-    launch_width<bf16>(a, any, s);
-  else
-    launch_width<float>(a, any, s);
+  // (a grid holds less than 2^32 threads)
+  constexpr long MOST = 1 << 23;
+  for (long t = 0; t < a.tokens; t += MOST) {
+    RmsNormArgs b = a;
+    b.tokens = a.tokens - t < MOST ? a.tokens - t : MOST;
+    b.x = (const uint8_t*)a.x + t * a.x_ld * el;
+    if (a.resid) b.resid = (const uint8_t*)a.resid + t * a.resid_ld * el;
+    if (a.sum) b.sum = (uint8_t*)a.sum + t * a.sum_ld * el;
+    b.y = (uint8_t*)a.y + t * a.y_ld * yel;
+    if (a.scale) b.scale = a.scale + t * a.blocks;
+    if (dt == BF16)
+      launch_width<bf16>(b, any, s);
+    else
+      launch_width<float>(b, any, s);
+  }
   return hipGetLastError();
 }
 

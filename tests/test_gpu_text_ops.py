@@ -407,6 +407,10 @@ def test_cross_attention_layouts(ops, nq, hi, dt):
     assert torch.equal(out[:, :nq, 1:, 8:48], whole)
     out[:, :nq, 1:, 8:48] = 5
     assert (out == 5).all()
+    odd = q.new_empty(3 * nq * heads * d + 64).as_strided((1, nq, heads, d), (13, heads * d, d, 1))  # a stride that nothing steps by
+    odd.copy_(q[:1])
+    kw1 = dict(kw, kv_len=kw["kv_len"][:1], mask=kw["mask"][:1])
+    assert torch.equal(ops.cross_attention(odd, k[:1], v[:1], hi, **kw1), whole[:1])
     one = k[:, :, :1].expand(n, hi, kvh, d)  # a shared head: stride 0
     ref = ops.cross_attention(q, one.contiguous(), v, hi, **kw)
     assert torch.equal(ops.cross_attention(q, one, v, hi, **kw), ref)

@@ -60,7 +60,7 @@ W4 = dict(x_type=BF16, x=A[0], x_ld=64, x_scale=None, x_group=0, M=0, K=64, w=A[
     (dict(), 0, ""), (dict(M=4, N=0), 0, ""),
     (dict(x_type=3), -1, "dtype"), (dict(scale_type=2), -1, "dtype"), (dict(out_type=2), -1, "dtype"),
     (dict(K=0), -1, "shape"), (dict(K=60), -1, "shape"), (dict(M=-1), -1, "shape"), (dict(N=-1), -1, "shape"),
-    (dict(M=(1 << 20) + 1), -2, "2^20"), (dict(K=(1 << 24) + 8), -2, "2^24"),
+    (dict(M=(1 << 19) + 1), -2, "2^19"), (dict(K=(1 << 24) + 8), -2, "2^24"), (dict(N=(1 << 24) + 1), -2, "2^24"),
     (dict(M=4, x_ld=(1 << 24) + 8), -2, "2^24"),
     (dict(group=0), -1, "group"), (dict(group=48), -1, "group"), (dict(group=256), -1, "group"),
     (dict(x_scale=A[7]), -1, "x_group"), (dict(x_group=128), -1, "x_group"),
@@ -89,7 +89,8 @@ XA = dict(dtype=BF16, q=A[0], q_ld=128, q_head=64, q_img=1280, k=A[1], k_ld=128,
     (dict(), 0, ""), (dict(n=0, n_q=5), 0, ""),
     (dict(dtype=2), -1, "dtype"), (dict(heads=3), -1, "shape"), (dict(d=60), -1, "shape"), (dict(d=0), -1, "shape"),
     (dict(d=264), -2, "shape"), (dict(heads=1 << 17), -2, "2^16"), (dict(max_len=(1 << 30) + 1), -2, "2^30"),
-    (dict(k_ld=(1 << 23) + 8), -2, "2^23"), (dict(n_q=1 << 30), -2, "too many"), (dict(n=-1), -1, "shape"), (dict(n_q=-1), -1, "shape"), (dict(max_len=-1), -1, "shape"),
+    (dict(n_q=9, k_ld=(1 << 23) + 8), -2, "2^23"), (dict(n_q=1 << 30), -2, "too many"),
+    (dict(n=1 << 22, n_ctx=1 << 22, n_q=9), -2, "too many"), (dict(n=-1), -1, "shape"), (dict(n_q=-1), -1, "shape"), (dict(max_len=-1), -1, "shape"),
     (dict(kv_heads=0), -1, "shape"), (dict(n_ctx=-1), -1, "context"), (dict(kv_tokens=-1), -1, "context"),
     (dict(kv_tokens=1 << 31), -1, "context"), (dict(n_ctx=2), -1, "fewer contexts"),
     (dict(scale=float("nan")), -1, "scale"), (dict(scale=float("inf")), -1, "scale"),
