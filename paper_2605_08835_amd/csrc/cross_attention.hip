@@ -292,32 +292,63 @@ __global__ __launch_bounds__(512) void cross_few_kernel(CrossArgs a, int keys, i
 }
 
 // ------------------------------------------------------------------ join
-// One wave per row: the splits of its text in order.
-template <typename T>
-__global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a, int keys, int splits) {
-  const int lane = threadIdx.x & 63;
-  const long rows = (long)a.rep * a.n_q, e = blockIdx.x * 4L + (threadIdx.x >> 6);
-  if (e >= (long)a.n * a.kv_heads * rows) return;
+// One wave per row, one block per wave: the splits of its text in order.  Lane
+// u holds (m, l) of split u, lanes hold a channel of every 64; the loads of U
+// splits are in flight at once (80 rows of 64, 9 to 16 splits: 4.7 us, one split
+// after another 12.9).
+template <typename T, int NI>
+__global__ __launch_bounds__(64) void cross_join_kernel(CrossArgs a, int keys, int splits) {
+  constexpr int U = NI == 1 ? 16 : 8;
+  const int lane = threadIdx.x;
+  const unsigned rows = (unsigned)(a.rep * a.n_q), e = blockIdx.x;
   const int r = (int)(e % rows), g = (int)(e / rows % a.kv_heads), img = (int)(e / rows / a.kv_heads);
   const int ns = (text_of(a, img).len + keys - 1) / keys;
   const Scratch sc = scratch_at(a, img, g, r, 0, splits);
-  float mt = -INFINITY;
-  for (int s = lane; s < ns; s += 64) mt = fmaxf(mt, sc.ml[2 * s]);
+  float m = -INFINITY, l = 0.f;
+  if (lane < ns) m = sc.ml[2 * lane], l = sc.ml[2 * lane + 1];
+  float mt = m;
+  for (int s = lane + 64; s < ns; s += 64) mt = fmaxf(mt, sc.ml[2 * s]);
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) mt = fmaxf(mt, __shfl_xor(mt, x, 64));
-  float v[4] = {0.f, 0.f, 0.f, 0.f}, lt = 0.f;
-  for (int s = 0; s < ns; ++s) {
-    const float f = sc.ml[2 * s] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sc.ml[2 * s] - mt);
-    lt = fmaf(f, sc.ml[2 * s + 1], lt);
+  float v[NI], lt = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < a.d) v[i] = fmaf(f, sc.o[(long)s * a.d + lane + 64 * i], v[i]);
+  for (int i = 0; i < NI; ++i) v[i] = 0.f;
+  for (int s0 = 0; s0 < ns; s0 += 64) {
+    if (s0) {
+      m = -INFINITY, l = 0.f;
+      if (s0 + lane < ns) m = sc.ml[2 * (s0 + lane)], l = sc.ml[2 * (s0 + lane) + 1];
+    }
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mt);
+    for (int u0 = s0; u0 < min(s0 + 64, ns); u0 += U) {
+      float x[U][NI];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          x[u][i] = 0.f;
+          if (u0 + u < ns && lane + 64 * i < a.d) x[u][i] = sc.o[(long)(u0 + u) * a.d + lane + 64 * i];
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float fu = __shfl(f, u0 - s0 + u, 64);
+        lt = fmaf(fu, __shfl(l, u0 - s0 + u, 64), lt);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) v[i] = fmaf(fu, x[u][i], v[i]);
+      }
+    }
   }
   const float inv = lt == 0.f ? 0.f : 1.0f / lt;
   T* o = (T*)a.o + (long)img * a.o_img + (r / a.rep) * a.o_ld + (g * a.rep + r % a.rep) * a.o_head;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < NI; ++i)
     if (lane + 64 * i < a.d) o[lane + 64 * i] = from_f<T>(v[i] * inv);
+}
+template <typename T>
+static void launch_join(const CrossArgs& a, const Plan& p, hipStream_t s) {
+  const unsigned grid = (unsigned)((long)a.n * a.kv_heads * a.rep * a.n_q);
+  if (a.d <= 64) cross_join_kernel<T, 1><<<grid, 64, 0, s>>>(a, p.keys, p.splits);
+  else if (a.d <= 128) cross_join_kernel<T, 2><<<grid, 64, 0, s>>>(a, p.keys, p.splits);
+  else cross_join_kernel<T, 4><<<grid, 64, 0, s>>>(a, p.keys, p.splits);
 }
 
 // ------------------------------------------------------------------ many rows, bf16
@@ -375,6 +406,8 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 // bounds it is memory: 80-byte rows of a 640-byte token reach 3.3 TB/s with the
 // arithmetic left out, which alone takes 47 us; three waves per SIMD hide part
 // of one behind the other.
+// Otherwise the vector unit bounds it, the exponentials above all: 16 x 1024
+// rows, 20 heads of 64, padded texts of 200 to 512 keys 64 us, 400 TFLOP/s.
 template <int D16, bool SF, bool SHORT>
 __global__ __launch_bounds__(256, D16 <= 48 || (D16 == 64 && !SHORT) ? 3 : D16 <= 96 ? 2 : 1) void cross_bf16_kernel(
     CrossArgs a, int keys, int tiles, int splits, int passes, int together) {
@@ -726,7 +759,8 @@ __device__ __forceinline__ void join_waves(const CrossArgs& a, const Place& p, i
 // A block takes 32 rows and a range of keys; its waves share the keys out, 32 at
 // a time, each with a piece of LDS, an online softmax and an O^T of its own,
 // and are joined at the end.  No barrier until then: what bounds it is the
-// bytes of K and V, so waves only have to keep loads in flight.  (The tile is
+// bytes of K and V, so waves only have to keep loads in flight: 4.9 TB/s, one
+// query over 9000 to 16384 keys, 4 x 20 heads of 64 in 57 us.  (The tile is
 // mostly empty for one query; its products still take less time than the loads.)
 template <int D16, bool SF, int NW>
 __global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(CrossArgs a, int keys, int tiles, int splits,
@@ -897,7 +931,9 @@ __global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(
 // Channels are summed in the order that makes a lane's share of them four
 // consecutive ones (half lh takes 8 i + 4 lh + [0, 4)); a key's probability
 // meets its V row straight from the register it was computed in, since the two
-// k of an MFMA are the two lane halves' keys.  Bound by the fp32 matrix rate.
+// k of an MFMA are the two lane halves' keys.  Bound by the fp32 matrix rate
+// once the card is full; 6 x 1024 rows, 8 heads of 32 on 4, up to 231 keys (20 us,
+// 37 TFLOP/s) wait for the blocks of the longest text.
 namespace {
 constexpr int FT = 32;
 __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) {
@@ -1264,7 +1300,8 @@ static void launch_f32(const CrossArgs& a, const Plan& p, hipStream_t s) {
 
 long cross_attention_scratch_floats(DType dt, int n, int heads, int kv_heads, int d, int n_q, int max_len) {
   const Plan p = plan_of(heads / kv_heads, n_q, max_len);
-  // (a grid holds less than 2^32 threads: blocks of at most 512 per 32 rows of a K/V head and split, in eights, and joins of 64 a row)
+  // (a grid holds less than 2^32 threads: blocks of at most 512 per 32 rows of a
+  // K/V head and split, in eights, and joins of 64 a row)
   const double rows = (double)heads * n_q * n, tiles = (double)heads / kv_heads * n_q / 32 + 1;
   const double blocks = ((double)n * kv_heads + 8) * tiles * p.splits, shared = (tiles * p.splits * n + 8) * kv_heads;
   if (blocks * 512 > 4.0e9 || shared * 512 > 4.0e9 || (p.splits > 1 && rows * 64 > 4.0e9)) return -1;
@@ -1305,11 +1342,10 @@ hipError_t launch_cross_attention(DType dt, CrossArgs a, hipStream_t s) {
     else launch_f32<256>(a, p, s);
   }
   if (p.splits > 1) {
-    const unsigned grid = (unsigned)((a.n * a.kv_heads * rows + 3) / 4);
     if (dt == BF16)
-      cross_join_kernel<bf16><<<grid, 256, 0, s>>>(a, p.keys, p.splits);
+      launch_join<bf16>(a, p, s);
     else
-      cross_join_kernel<float><<<grid, 256, 0, s>>>(a, p.keys, p.splits);
+      launch_join<float>(a, p, s);
   }
   return hipGetLastError();
 }

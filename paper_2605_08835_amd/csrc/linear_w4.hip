@@ -9,8 +9,8 @@
 //    binade are one even ladder), so 8 codes become bf16 with two masks, a
 //    shift and four conversions, exactly.
 //  * The zero point stays outside the products: sum x over the group, the
-//    same for every weight row, comes from the staging pass or one more MFMA
-//    with ones.
+//    same for every weight row, comes from one more MFMA with ones (wide
+//    layers: from the pass that brings x into LDS).
 //  * A group's sums keep whole codes until its scale multiplies them in fp32:
 //    the weights are never rounded.
 //  * fp32 x is cut into three bf16 parts of 8 bits each (their sum is x
@@ -154,7 +154,8 @@ __device__ __forceinline__ void finish(const LinearW4Args& a, const float* red, 
 // rows.  Neighbouring lanes load neighbouring bytes of a row (a lane per row,
 // as the MFMA wants it, takes the L1 one cycle per lane: 8192 x 8192, 16 rows
 // 18.8 us); a wave's own piece of LDS turns them into operands, without a
-// barrier.
+// barrier: 14.0 us, 2.5 TB/s of codes.  Loading alone takes 7; the turn, the
+// scales and the waves' sums are the rest.
 template <bool E8, int MT, int T>
 __host__ __device__ constexpr int w4_wave_bytes() { return T * 16 * 80 + MT * 16 * 17 * (E8 ? 8 : 16); }
 template <int T>
@@ -494,8 +495,9 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
 
 // The same for wide layers: WN waves side by side (16 weight rows each) share
 // one pass of x through LDS, wave rows wk split K.  (20160 x 1280, fp32 under
-// SiLU: 1 row 11.3 us against 14.1 above, 32 rows 18.5 against 29; narrower
-// layers leave it too few waves along K: 8192 x 8192, 1 row 40 us against 20.)
+// SiLU: 1 row 11.2 us against 14.3 above, 32 rows 18.3 against 29.6; narrower
+// layers leave it too few waves: 8192 x 8192, 1 row 61 us against 20.)  Bound by
+// bringing x in, activated and cut, once per block, and its LDS reads.
 template <int MT, int G>
 __global__ __launch_bounds__(1024) void linear_w4_wide_kernel(LinearW4Args a) {
   constexpr int WN = 8, GC = KC / G, JG = G / 32, LD = KC + 8;  // LDS rows 272 bytes apart: no bank conflicts over 16 rows

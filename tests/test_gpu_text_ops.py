@@ -354,6 +354,15 @@ def test_cross_attention_long_texts(ops, nq, heads, kvh, d, lens, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("nq,d", [(1, 16), (2, 72), (1, 136)])
+def test_cross_attention_joins_many_ranges(ops, nq, d, dt):
+    """More ranges than a wave has lanes, beside texts of one and of exactly 64."""
+    q, k, v, hi, kw, texts = _attn_case(d, dt, 4, nq, 1, 1, d, [70001, 65536, 3, 66561], False, 0.0, spread=2.0)
+    got = ops.cross_attention(q, k, v, hi, **kw)
+    _check_attn(got, q, k, v, texts, dt, f"{(nq, d, dt)}")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("nq", [1, 3, 90])
 def test_cross_attention_empty_texts_shared_texts_and_bad_indices(ops, nq, dt):
     index = [2, 0, 2, 1, -1, 3, 7, 0, 1 << 30]
