@@ -73,6 +73,16 @@ __device__ __forceinline__ u32x4 codes_bf16(uint32_t w) {
 // The high halves of a (first) and b as one dword.
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
+// SiLU where asked: one branch around all 8 (value by value the compiler
+// computes it always and picks: fp32, 16 rows of 4096 x 4096 12.3 us against 9.5).
+__device__ __forceinline__ void silu_if(int on, float (&v)[8]) {
+  if (__builtin_amdgcn_readfirstlane(on)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = silu_f(v[e]);
+    asm volatile("" : "+v"(v[0]));  // (and keeps the branch)
+  }
+}
+
 // A wave's work in order: chunks wave, wave + nw, ... of the block's tiles of
 // weight rows (blockIdx.x, + gridDim.x, ...), one sequence, so that loads run
 // ahead across tiles.
@@ -154,7 +164,7 @@ __device__ __forceinline__ void finish(const LinearW4Args& a, const float* red, 
 // rows.  Neighbouring lanes load neighbouring bytes of a row (a lane per row,
 // as the MFMA wants it, takes the L1 one cycle per lane: 8192 x 8192, 16 rows
 // 18.8 us); a wave's own piece of LDS turns them into operands, without a
-// barrier: 14.0 us, 2.5 TB/s of codes.  Loading alone takes 7; the turn, the
+// barrier: 14.2 us, 2.5 TB/s of codes.  Loading alone takes 7; the turn, the
 // scales and the waves' sums are the rest.
 template <bool E8, int MT, int T>
 __host__ __device__ constexpr int w4_wave_bytes() { return T * 16 * 80 + MT * 16 * 17 * (E8 ? 8 : 16); }
@@ -381,14 +391,18 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
     for (int i = 0; i < 2; ++i) {
       if (8 * i >= rows) break;
       uint32_t part[3][8];
+      float xv[8];
+      if (a.x_type == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) xv[e] = __uint_as_float(x[i][e >> 2][e & 3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) xv[e] = __uint_as_float(e & 1 ? x[i][0][e >> 1] & 0xFFFF0000u : x[i][0][e >> 1] << 16);
+      }
+      silu_if(a.silu_in, xv);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float v;
-        if (a.x_type == 0)
-          v = __uint_as_float(x[i][e >> 2][e & 3]);
-        else
-          v = __uint_as_float(e & 1 ? x[i][0][e >> 1] & 0xFFFF0000u : x[i][0][e >> 1] << 16);
-        if (a.silu_in) v = silu_f(v);
+        float v = xv[e];
         // (an infinity or NaN leaves a NaN in the second part)
         part[0][e] = __float_as_uint(v);
         v -= __uint_as_float(part[0][e] & 0xFFFF0000u);
@@ -495,7 +509,7 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
 
 // The same for wide layers: WN waves side by side (16 weight rows each) share
 // one pass of x through LDS, wave rows wk split K.  (20160 x 1280, fp32 under
-// SiLU: 1 row 11.2 us against 14.3 above, 32 rows 18.3 against 29.6; narrower
+// SiLU: 1 row 11.0 us against 14.3 above, 32 rows 17.9 against 29.6; narrower
 // layers leave it too few waves: 8192 x 8192, 1 row 61 us against 20.)  Bound by
 // bringing x in, activated and cut, once per block, and its LDS reads.
 template <int MT, int G>
@@ -541,10 +555,10 @@ __global__ __launch_bounds__(1024) void linear_w4_wide_kernel(LinearW4Args a) {
       if (idx >= PIECES || m0 + row >= a.M) continue;  // (whole groups of 16 lanes)
       uint32_t part[3][8];
       float sum = 0.f;
+      silu_if(a.silu_in, xr[p]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float v = xr[p][e];
-        if (a.silu_in) v = silu_f(v);
         sum += v;
         // (an infinity or NaN leaves a NaN in the second part)
         part[0][e] = __float_as_uint(v);
@@ -641,15 +655,16 @@ static void launch_tile(const LinearW4Args& a, hipStream_t s) {
   linear_w4_kernel<E8, MT, T, G><<<grid, 64 * nw, nw * wave, s>>>(a);
 }
 
-// Two tiles of x rows past 16 rows, two of weight rows where there are plenty
-// (half the traffic of x), as far as 128 registers hold them: groups of 32
-// take one by one, e4m3 in groups of 64 one tile of x.
+// Two tiles of x rows past 16 rows, two of weight rows where a block would have
+// more than one anyway (6144 x 2048, 16 rows of bf16: 6.4 -> 5.1 us), as far as
+// 128 registers hold them: groups of 32 take one by one, e4m3 in groups of 64
+// one tile of x.
 template <bool E8, int G>
 static void launch_x(const LinearW4Args& a, hipStream_t s) {
   constexpr int MT = G == 128 || (G == 64 && !E8) ? 2 : 1, T = G == 32 ? 1 : 2;
   if (MT == 2 && a.M > 16)
     launch_tile<E8, MT, 1, G>(a, s);
-  else if (T == 2 && a.N >= 8192)
+  else if (T == 2 && a.N > 4096)
     launch_tile<E8, 1, T, G>(a, s);
   else
     launch_tile<E8, 1, 1, G>(a, s);
@@ -680,7 +695,9 @@ static void launch_wide(const LinearW4Args& a, hipStream_t s) {
 template <int G>
 static void launch_f32(const LinearW4Args& a, hipStream_t s) {
   if (a.N < 16384) {
-    if (G == 128 && a.N >= 8192)  // (two tiles of weight rows spill at smaller groups)
+    // two tiles of weight rows share a pass of x, where a block would have more
+    // than one anyway (6144 x 2048, 1 row: 7.9 -> 6.0 us); smaller groups spill
+    if (G == 128 && a.N > 4096)
       launch_f32_tile<G == 128 ? 2 : 1, G>(a, s);
     else
       launch_f32_tile<1, G>(a, s);

@@ -248,6 +248,21 @@ def test_linear_rows_w4_strides_and_row_independence(ops, xt):
     assert ops.linear_rows_w4(x[:0], w, scale, 32, zero=z, x_scale=None if xs is None else xs[:0]).shape == (0, N)
 
 
+@pytest.mark.parametrize("xt", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(17, 24, 4096), (33, 1160, 4100), (20, 1288, 8200), (49, 2184, 8195), (64, 4232, 4129)])
+def test_linear_rows_w4_rows_by_the_dozen(ops, M, K, N, xt):
+    """Layers of some thousand outputs: right, and the same bits whether the rows come alone or together."""
+    for group, zero in ((32, True), (64, False), (128, True)):
+        g = _gen(M + K + N + group)
+        x, xs, w, scale, z = _w4_case(g, M, K, N, group, zero, xt, "f32")
+        for si in (False, True):
+            got = ops.linear_rows_w4(x, w, scale, group, zero=z, silu_in=si)
+            for i, rows in ((0, 1), (M // 2, 5), (1, 16), (M - 17, 17)):
+                assert torch.equal(ops.linear_rows_w4(x[i:i + rows], w, scale, group, zero=z, silu_in=si), got[i:i + rows]), (i, rows)
+        ref, size = _w4_ref(x, xs, w, scale, z, group, silu_in=True)
+        _close(_np(got), ref, W4 * size + 8 * U32 * size, f"{(M, K, N, xt, group)}")
+
+
 def test_linear_rows_w4_large_small_and_non_finite_values(ops):
     g = _gen(8)
     x, xs, w, scale, z = _w4_case(g, 5, 256, 48, 64, False, "f32", "f32")
