@@ -196,65 +196,64 @@ __global__ __launch_bounds__(256) void rmsnorm_kernel(RmsNormArgs a) {
     }
     return;
   }
-  // e4m3: blocks of 128 channels are the BL = 128 / N lanes that share a
-  // piece index (TPR >= 32, a multiple of BL); a whole row's maximum is taken over all.
-  if constexpr (TPR >= 32) {
-    uint32_t top[R];
+  // e4m3: several blocks of 128 channels are each the BL = 128 / N lanes that
+  // share a piece index (TPR >= 32, a multiple of BL); one scale's maximum is taken over the row.
+  uint32_t top[R];
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      top[i] = 0x0D800000u;  // 2^-100
+  for (int i = 0; i < R; ++i) {
+    top[i] = 0x0D800000u;  // 2^-100
 #pragma unroll
-      for (int e = 0; e < N; ++e) top[i] = max(top[i], __float_as_uint(h[i][e]) & 0x7FFFFFFFu);
+    for (int e = 0; e < N; ++e) top[i] = max(top[i], __float_as_uint(h[i][e]) & 0x7FFFFFFFu);
+  }
+  const bool grouped = TPR >= 32 && a.blocks > 1;
+  if (grouped) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) top[i] = lanes_max<BL>(top[i]);
+  } else {
+#pragma unroll
+    for (int i = 1; i < R; ++i) top[0] = max(top[0], top[i]);
+    top[0] = lanes_max<(TPR < 64 ? TPR : 64)>(top[0]);
+    if constexpr (TPR == 256) {
+      if ((threadIdx.x & 63) == 0) partm[threadIdx.x >> 6] = top[0];
+      __syncthreads();
+      top[0] = max(max(partm[0], partm[1]), max(partm[2], partm[3]));
     }
-    if (a.blocks > 1 || a.group == 128) {
 #pragma unroll
-      for (int i = 0; i < R; ++i) top[i] = lanes_max<BL>(top[i]);
-    } else {
+    for (int i = 1; i < R; ++i) top[i] = top[0];
+  }
+  if (!on) return;
+  uint8_t* y = (uint8_t*)a.y + row * a.y_ld;
 #pragma unroll
-      for (int i = 1; i < R; ++i) top[0] = max(top[0], top[i]);
-      top[0] = lanes_max<(TPR < 64 ? TPR : 64)>(top[0]);
-      if constexpr (TPR == 256) {
-        if ((threadIdx.x & 63) == 0) partm[threadIdx.x >> 6] = top[0];
-        __syncthreads();
-        top[0] = max(max(partm[0], partm[1]), max(partm[2], partm[3]));
-      }
+  for (int i = 0; i < R; ++i) {
+    const int c = (i * TPR + lane) * N;
+    if (c >= C) continue;
+    const float s = __uint_as_float(top[i]) / 448.f;
+    if (grouped ? lane % BL == 0 : i == 0 && lane == 0) a.scale[row * a.blocks + (grouped ? c / 128 : 0)] = s;
+    const float inv = 1.0f / s;
+    uint32_t q[N / 4];
 #pragma unroll
-      for (int i = 1; i < R; ++i) top[i] = top[0];
+    for (int e = 0; e < N; e += 4) {
+      int p = __builtin_amdgcn_cvt_pk_fp8_f32(h[i][e] * inv, h[i][e + 1] * inv, 0, false);
+      q[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(h[i][e + 2] * inv, h[i][e + 3] * inv, p, true);
     }
-    if (!on) return;
-    uint8_t* y = (uint8_t*)a.y + row * a.y_ld;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int c = (i * TPR + lane) * N;
-      if (c >= C) continue;
-      const float s = __uint_as_float(top[i]) / 448.f;
-      if (a.group == 128 ? lane % BL == 0 : i == 0 && lane == 0) a.scale[row * a.blocks + (a.group == 128 ? c / 128 : 0)] = s;
-      const float inv = 1.0f / s;
-      uint32_t q[N / 4];
-#pragma unroll
-      for (int e = 0; e < N; e += 4) {
-        int p = __builtin_amdgcn_cvt_pk_fp8_f32(h[i][e] * inv, h[i][e + 1] * inv, 0, false);
-        q[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(h[i][e + 2] * inv, h[i][e + 3] * inv, p, true);
-      }
-      if (c + N <= C) {
-        if constexpr (ANY && N == 8) {
-          U8B u;
-          u.w[0] = q[0]; u.w[1] = q[1];
-          *(U8B*)(y + c) = u;
-        } else if constexpr (ANY) {
-          U4B u;
-          u.w = q[0];
-          *(U4B*)(y + c) = u;
-        } else if constexpr (N == 8) {
-          *(uint2*)(y + c) = make_uint2(q[0], q[1]);
-        } else {
-          *(uint32_t*)(y + c) = q[0];
-        }
+    if (c + N <= C) {
+      if constexpr (ANY && N == 8) {
+        U8B u;
+        u.w[0] = q[0]; u.w[1] = q[1];
+        *(U8B*)(y + c) = u;
       } else if constexpr (ANY) {
-#pragma unroll
-        for (int e = 0; e < N - 1; ++e)
-          if (c + e < C) y[c + e] = (uint8_t)(q[e / 4] >> (8 * (e % 4)));
+        U4B u;
+        u.w = q[0];
+        *(U4B*)(y + c) = u;
+      } else if constexpr (N == 8) {
+        *(uint2*)(y + c) = make_uint2(q[0], q[1]);
+      } else {
+        *(uint32_t*)(y + c) = q[0];
       }
+    } else if constexpr (ANY) {
+#pragma unroll
+      for (int e = 0; e < N - 1; ++e)
+        if (c + e < C) y[c + e] = (uint8_t)(q[e / 4] >> (8 * (e % 4)));
     }
   }
 }
@@ -271,12 +270,16 @@ static void launch_rows(const RmsNormArgs& a, bool any, hipStream_t s) {
 
 // The lanes per row follow the width alone (a row's bits are the same in
 // every batch): the fewest that hold it in up to 8 pieces, and a count of
-// pieces near the row's own.
+// pieces near the row's own; lanes without a piece still cost their row's time
+// (142689 x 16 bf16 to e4m3 with a residual: 4.6 us on 2 lanes, 25.2 on 32;
+// 80000 x 320 to e4m3 18.0 on 8, 23.1 on 32, but 50000 x 512 19.3 and 16.9).
 template <typename T>
 static void launch_width(const RmsNormArgs& a, bool any, hipStream_t s) {
   const int nv = (a.C + Vec<T>::N - 1) / Vec<T>::N;
-  if (nv <= 64 && !a.y8) {
-    if (nv <= 8) launch_rows<T, 8, 1>(a, any, s);
+  if (nv <= (!a.y8 ? 64 : a.blocks == 1 ? 40 : 0)) {
+    if (nv <= 2) launch_rows<T, 2, 1>(a, any, s);
+    else if (nv <= 4) launch_rows<T, 4, 1>(a, any, s);
+    else if (nv <= 8) launch_rows<T, 8, 1>(a, any, s);
     else if (nv <= 16) launch_rows<T, 8, 2>(a, any, s);
     else if (nv <= 24) launch_rows<T, 8, 3>(a, any, s);
     else if (nv <= 40) launch_rows<T, 8, 5>(a, any, s);

@@ -82,6 +82,20 @@ def test_rmsnorm(ops, rows, C, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [2, 4, 12, 16, 17, 24, 32, 40, 100])
+def test_rmsnorm_many_narrow_rows(ops, C, dt):
+    """Several rows a wave: sums and scales stay each row's own."""
+    g = _gen(C)
+    x = torch.randn(1037, C, generator=g, device="cuda") * torch.exp2(torch.randint(-6, 7, (1037, 1), generator=g, device="cuda").float())
+    x, r = x.to(_t(dt)), torch.randn(1037, C, generator=g, device="cuda").to(_t(dt))
+    gamma = torch.randn(C, generator=g, device="cuda")
+    for resid in (None, r):
+        for fp8, group in ((False, 0), (True, 0), (True, 128)):
+            got = ops.rmsnorm(x, gamma, 1e-6, resid=resid, fp8=fp8, scale_group=group)
+            _check_norm(got, x, gamma, 1e-6, resid, fp8, group, dt, f"{(C, dt, fp8, group)}")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("C", [64, 65, 320, 1000])
 def test_rmsnorm_strides_alignment_and_neighbours(ops, C, dt):
     """Rows inside wider buffers, aligned and not, one row apart or more; what
