@@ -101,11 +101,14 @@ static unsigned place_blocks(long kv_heads, long tiles, long splits, long n, lon
 }
 // Heads whose rows fill whole lines of 128 bytes, where that many divide the
 // heads and leave every XCD two of them (16 x 4096 rows, 8 heads of 40, up to 300
-// keys: 67 us against 77 one by one); else one.
+// keys: 67 us against 77 one by one); else one; none where that left over a
+// quarter of the XCDs' turns empty.
 static int place_together(const CrossArgs& a, int el) {
   int h = 1;
   while (h * a.d * el % 128) h *= 2;
-  return a.kv_heads % h == 0 && (long)a.n * (a.kv_heads / h) >= 16 ? h : 1;
+  if (a.kv_heads % h || (long)a.n * (a.kv_heads / h) < 16) h = 1;
+  const long groups = (long)a.n * (a.kv_heads / h), rounds = (groups + 7) / 8;
+  return groups * 4 >= rounds * 24 ? h : 0;
 }
 
 // The kernel of a call, by the rows of a K/V head, and its ranges of `keys` (0:
@@ -409,7 +412,7 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 // Otherwise the vector unit bounds it, the exponentials above all: 16 x 1024
 // rows, 20 heads of 64, padded texts of 200 to 512 keys 64 us, 400 TFLOP/s.
 template <int D16, bool SF, bool SHORT>
-__global__ __launch_bounds__(256, D16 <= 48 || (D16 == 64 && !SHORT) ? 3 : D16 <= 96 ? 2 : 1) void cross_bf16_kernel(
+__global__ __launch_bounds__(256, D16 <= 48 || (D16 == 64 && !SHORT) ? 3 : D16 <= 128 ? 2 : 1) void cross_bf16_kernel(
     CrossArgs a, int keys, int tiles, int splits, int passes, int together) {
   constexpr int NW = 4, NJ = D16 / 16, ND = (D16 + 31) / 32, NT = 64 * NW, LDK = D16 + 8, LDV = v_row(D16);
   // A tile is moved by passes of NT / LPR keys, LPR lanes (a power of two) a key
@@ -1264,7 +1267,9 @@ static void launch_sum(const CrossArgs& a, const Plan& p, hipStream_t s) {
     cross_keys_kernel<D16, SF, NW><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits, together);
     return;
   }
-  if constexpr (D16 <= 128)  // (wider heads' tiles leave no LDS for the output rows)
+  // (wider heads: LDS for the output rows leaves one block a CU; 16 x 1024 rows, 8
+  // heads of 120, up to 120 keys 37 us against 29)
+  if constexpr (D16 <= 96)
     if (a.max_len <= 2 * KT) {
       // up to 8 groups of rows per wave, as long as some 1000 blocks remain
       const long groups = (rows + 127) / 128, all = groups * a.kv_heads * a.n;
@@ -1291,7 +1296,11 @@ static void launch_f32(const CrossArgs& a, const Plan& p, hipStream_t s) {
   if (p.kind == 1) {
     constexpr int NW = D32 <= 128 ? 4 : 2;  // (as many as the LDS holds)
     const int tiles = (int)((rows + 31) / 32);
-    cross_keys_f32_kernel<D32, NW><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits, together);
+    const unsigned grid = place_blocks(a.kv_heads, tiles, p.splits, a.n, together);
+    if (a.max_len <= FT)  // (the first wave has them all: the same sums; 13 x 22 rows, 40 heads of 128 on 10: 28 -> 19 us)
+      cross_keys_f32_kernel<D32, 1><<<grid, 64, 0, s>>>(a, p.keys, tiles, p.splits, together);
+    else
+      cross_keys_f32_kernel<D32, NW><<<grid, 64 * NW, 0, s>>>(a, p.keys, tiles, p.splits, together);
   } else {
     const int tiles = (int)((rows + 127) / 128);
     cross_f32_kernel<D32><<<place_blocks(a.kv_heads, tiles, p.splits, a.n, together), 256, 0, s>>>(a, p.keys, tiles, p.splits, together);

@@ -383,6 +383,17 @@ def test_cross_attention_long_texts(ops, nq, heads, kvh, d, lens, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,nq,heads,kvh,d", [(13, 22, 8, 2, 128), (5, 40, 3, 3, 40), (3, 300, 8, 1, 256), (9, 200, 2, 1, 120), (7, 33, 2, 2, 200)])
+def test_cross_attention_short_texts(ops, n, nq, heads, kvh, d, dt):
+    """Texts of at most one tile, few and many groups of rows: right, and the same bits beside a longer text."""
+    lens = [1 + (7 * i) % 32 for i in range(n)]
+    q, k, v, hi, kw, texts = _attn_case(n + d, dt, n, nq, heads, kvh, d, lens, False, 0.1)
+    got = ops.cross_attention(q, k, v, hi, **kw)
+    _check_attn(got, q, k, v, texts, dt, f"{(n, nq, heads, kvh, d, dt)}")
+    assert torch.equal(ops.cross_attention(q, k, v, 90, **kw), got)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("nq,d", [(1, 16), (2, 72), (1, 136)])
 def test_cross_attention_joins_many_ranges(ops, nq, d, dt):
     """More ranges than a wave has lanes, beside texts of one and of exactly 64."""
