@@ -196,10 +196,10 @@ sd_status synerdiff_op_conv_out_cfg_ddim(int32_t dtype, const void* d_x, int32_t
  * d_scale fp32 [tokens, blocks] with scale_group = 128, or [tokens] with
  * scale_group = 0; a NaN in a row makes all its y and scales NaN.
  * sum may equal x or resid, and y (of y_type dtype) may equal x or resid,
- * with the same ld; otherwise outputs overlap nothing.  Any alignment and ld; buffers whose
- * rows all start at multiples of 16 bytes (y8: 8) and C a multiple of 8 move
- * in 16-byte pieces.  1 <= C <= 16384 (SD_ERR_UNSUPPORTED past it), eps >= 0.
- * tokens = 0 does nothing. */
+ * with the same ld; otherwise outputs overlap nothing.  Any alignment and ld;
+ * buffers whose rows all start at multiples of 16 bytes (y8: 8) and C a
+ * multiple of 8 move in 16-byte pieces.  1 <= C <= 16384 (SD_ERR_UNSUPPORTED
+ * past it), eps >= 0.  tokens = 0 does nothing. */
 sd_status synerdiff_op_rmsnorm(int32_t dtype, const void* d_x, int64_t x_ld, const void* d_resid, int64_t resid_ld,
                                void* d_sum, int64_t sum_ld, const float* d_gamma, float eps, int64_t tokens,
                                int32_t C, int32_t y_type, void* d_y, int64_t y_ld, float* d_scale,
@@ -215,14 +215,15 @@ sd_status synerdiff_op_rmsnorm(int32_t dtype, const void* d_x, int64_t x_ld, con
  * x [M, K] in x_type SD_F32, SD_BF16 or SD_E4M3, row m at m * x_ld
  * (elements); e4m3 rows stand for x8 * x_scale, fp32 [M] with x_group = 0 or
  * [M, ceil(K / 128)] with x_group = 128, as synerdiff_op_rmsnorm writes them
- * (x_scale NULL and x_group 0 for the other types).  act_* = SiLU where silu_* = 1,
- * else the identity (silu_in not with e4m3: SD_ERR_UNSUPPORTED).  out [M, N]
- * in out_type SD_F32 or SD_BF16, row m at m * out_ld; bias fp32 [N], add
+ * (x_scale NULL and x_group 0 for the other types).  act_* = SiLU where
+ * silu_* = 1, else the identity (silu_in not with e4m3: SD_ERR_UNSUPPORTED).
+ * out [M, N] in out_type SD_F32 or SD_BF16, row m at m * out_ld; bias fp32 [N], add
  * fp32 [M, N], may be NULL; add may equal an fp32 out of out_ld = N; out
  * overlaps nothing else.  Products and sums are fp32-accurate for every
  * x_type.  A row of x with an infinity or NaN gives no finite value.
- * K a multiple of 8, x_ld and N <= 2^24, M <= 2^19; x and its rows 16-byte aligned (e4m3: 8).  The rows of a
- * result do not depend on M.  M = 0 or N = 0 does nothing. */
+ * K a multiple of 8; K, N and x_ld <= 2^24, M <= 2^19 (SD_ERR_UNSUPPORTED past
+ * them); x and its rows 16-byte aligned (e4m3: 8).  The rows of a result do not
+ * depend on M.  M = 0 or N = 0 does nothing. */
 sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* d_x, int64_t x_ld, const float* d_x_scale,
                                       int32_t x_group, int32_t M, int32_t K, const uint8_t* d_w, int32_t group,
                                       int32_t scale_type, const void* d_scale, const uint8_t* d_zero,
@@ -232,7 +233,8 @@ sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* d_x, int64_t x
 /* Attention of each row's queries over a text of its own length:
  *   o[i, t, h] = sum_j p_j v[j, g] / sum_j p_j,  p_j = exp(scale * q[i, t, h] . k[j, g])
  * over the keys j of row i's context that take part, g = h / (heads /
- * kv_heads).  Row i reads context c = kv_index[i] (NULL: c = i, n_ctx >= n); key j < kv_len[c] (NULL: max_len for all) takes part if its mask byte is not
+ * kv_heads).  Row i reads context c = kv_index[i] (NULL: c = i, n_ctx >= n);
+ * key j < kv_len[c] (NULL: max_len for all) takes part if its mask byte is not
  * 0 (NULL: all do).  Keys that take no part are not read: they may hold
  * anything.  A row without a key, or whose kv_index lies outside [0, n_ctx),
  * gives zeros.
@@ -240,18 +242,20 @@ sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* d_x, int64_t x
  * q_head + e, o likewise.  Contexts one after another (d_kv_start not NULL):
  * key j of context c is row kv_start[c] + j of k: k + row * k_ld + g *
  * k_head + e, and mask byte `row` of [kv_tokens]; a context that starts
- * outside [0, kv_tokens) is empty, one that ends past it is cut there.  Padded contexts (d_kv_start NULL): k + c * k_ctx + j *
- * k_ld + g * k_head + e, and mask byte c * max_len + j.  v likewise.  A
+ * outside [0, kv_tokens) is empty, one that ends past it is cut there.  Padded
+ * contexts (d_kv_start NULL): k + c * k_ctx + j * k_ld + g * k_head + e, and
+ * mask byte c * max_len + j.  v likewise.  A
  * kv_len past max_len counts as max_len, a negative one as 0.  Strides in
  * elements, not negative (0 for a shared head; that of an axis of one element
  * is not looked at).
  * Constraints: d a multiple of 8, <= 256; heads a multiple of kv_heads, <=
- * 2^16; max_len <= 2^30; q_ld, k_ld, v_ld, o_ld <= 2^23; a grid of less than 2^32
- * threads (a block of 512 per 32 rows of a K/V head and split); q, k, v, o and all their strides at multiples of 16
- * bytes.  o overlaps nothing.  Few queries over long texts are split along the keys: d_scratch
- * (fp32, 16-byte aligned) has to hold synerdiff_op_cross_attention_scratch_floats(...) floats
- * then (SD_ERR_WORKSPACE if smaller; 0 = none needed), and belongs to this call
- * until it has run.  The bits of a row depend on its own inputs, n_q, heads,
+ * 2^16; max_len <= 2^30; q_ld, k_ld, v_ld, o_ld <= 2^23; a grid of less than
+ * 2^32 threads (a block of 512 per 32 rows of a K/V head and split); q, k, v, o
+ * and all their strides at multiples of 16 bytes.  o overlaps nothing.  Few
+ * queries over long texts are split along the keys: d_scratch (fp32, 16-byte
+ * aligned) has to hold synerdiff_op_cross_attention_scratch_floats(...) floats
+ * then (0: none needed, -1: the grid is too large; SD_ERR_WORKSPACE if smaller),
+ * and belongs to this call until it has run.  The bits of a row depend on its own inputs, n_q, heads,
  * kv_heads and d, not on the other rows or max_len.  n = 0 or n_q = 0 does nothing. */
 int64_t synerdiff_op_cross_attention_scratch_floats(int32_t dtype, int32_t n, int32_t heads, int32_t kv_heads,
                                                     int32_t d, int32_t n_q, int32_t max_len);

@@ -411,6 +411,8 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 // of one behind the other.
 // Otherwise the vector unit bounds it, the exponentials above all: 16 x 1024
 // rows, 20 heads of 64, padded texts of 200 to 512 keys 64 us, 400 TFLOP/s.
+// Two waves per SIMD up to 128 channels, though a few registers spill there (8 x
+// 2048 rows, 8 heads of 128, up to 512 keys: 61 us against 66).
 template <int D16, bool SF, bool SHORT>
 __global__ __launch_bounds__(256, D16 <= 48 || (D16 == 64 && !SHORT) ? 3 : D16 <= 128 ? 2 : 1) void cross_bf16_kernel(
     CrossArgs a, int keys, int tiles, int splits, int passes, int together) {

@@ -478,6 +478,17 @@ def test_cross_attention_rows_do_not_depend_on_their_batch(ops, nq, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 40, 96, 120, 160, 256])
+def test_cross_attention_bits_do_not_depend_on_the_longest_text(ops, d, dt):
+    for nq, heads, kvh in ((1, 3, 3), (2, 8, 2), (40, 2, 2), (200, 2, 1), (530, 1, 1)):
+        q, k, v, hi, kw, texts = _attn_case(d + nq, dt, 4, nq, heads, kvh, d, [30, 1, 60, 17], False, 0.2)
+        first = ops.cross_attention(q, k, v, hi, **kw)
+        _check_attn(first, q, k, v, texts, dt, f"{(nq, heads, kvh, d, dt)}")
+        for most in (100, 128, 129, 600, 1100, 5000):
+            assert torch.equal(ops.cross_attention(q, k, v, most, **kw), first), (nq, most)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("nq", [1, 40])
 def test_cross_attention_scores_far_apart(ops, nq, dt):
     """Scores of +-200 and more: the running maximum moves late and early;
