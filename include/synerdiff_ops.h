@@ -237,7 +237,8 @@ sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* d_x, int64_t x
  * key j < kv_len[c] (NULL: max_len for all) takes part if its mask byte is not
  * 0 (NULL: all do).  Keys that take no part are not read: they may hold
  * anything.  A row without a key, or whose kv_index lies outside [0, n_ctx),
- * gives zeros.
+ * gives zeros.  Keys that score -inf take no weight, and a row whose keys all
+ * do gives zeros.
  * Layouts: element (i, t, h, e) of q is at q + i * q_img + t * q_ld + h *
  * q_head + e, o likewise.  Contexts one after another (d_kv_start not NULL):
  * key j of context c is row kv_start[c] + j of k: k + row * k_ld + g *

@@ -146,6 +146,10 @@ __device__ __forceinline__ RowAt row_at(const CrossArgs& a, int r) {
   return {t, r - t * a.rep};
 }
 
+// What a row's exponents are taken against: its running maximum, or 0 as long as
+// every key so far scored -inf (then every p is 0; -inf minus -inf is NaN).
+__device__ __forceinline__ float exp_ref(float m) { return m == -INFINITY ? 0.f : m; }
+
 __device__ __forceinline__ float2 half_swap(float v) {  // (v of lanes l and l ^ 32)
 #if defined(__HIP_DEVICE_COMPILE__)
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -227,7 +231,7 @@ __global__ __launch_bounds__(512) void cross_few_kernel(CrossArgs a, int keys, i
       float mn = m[r];
 #pragma unroll
       for (int u = 0; u < U; ++u) mn = fmaxf(mn, s[r][u]);
-      const float ref = mn == -INFINITY ? 0.f : mn;  // (no key yet: every p is 0)
+      const float ref = exp_ref(mn);
       const float al = __builtin_amdgcn_exp2f(m[r] - ref);
       m[r] = mn;
       l[r] *= al;
@@ -560,6 +564,7 @@ __global__ __launch_bounds__(256, D16 <= 48 || (D16 == 64 && !SHORT) ? 3 : D16 <
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[t][r] *= al;
     }
+    const float ref = exp_ref(m_run);
     // O^T += V^T P^T, 16 keys at a time: slot (lh, i) of slice u is key 16 u +
     // 8 (i / 4) + 4 lh + i % 4, register 8 (u % 2) + i of half u / 2.  The
     // probabilities are rounded to bf16 (half a step, 2^-9 of each) and
@@ -576,7 +581,7 @@ __global__ __launch_bounds__(256, D16 <= 48 || (D16 == 64 && !SHORT) ? 3 : D16 <
       bf16x8 pf;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        pf[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + i], sl2, -m_run));
+        pf[i] = (bf16)__builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + i], sl2, -ref));
       if constexpr (!SF) l_run = sum_probs(pf, FIRST && u == 0 ? 0.f : l_run);
 #pragma unroll
       for (int t = 0; t < ND; ++t) {
@@ -880,13 +885,14 @@ __global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[t][r] *= al;
     }
+    const float ref = exp_ref(m_run);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       // (as bf16 plus the rest as bf16, 2^-17 of each: these products have time to spare)
       bf16x8 pf, pr;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * u + i], sl2, -m_run));
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * u + i], sl2, -ref));
         if constexpr (!SF) l_run += x;
         pf[i] = (bf16)x;
         pr[i] = (bf16)(x - (float)pf[i]);
@@ -1058,9 +1064,10 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void cross_f32_kernel(Cross
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[t][i] *= al;
         }
+        const float ref = exp_ref(m_run);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float pr = __builtin_amdgcn_exp2f(s[i] - m_run);
+          const float pr = __builtin_amdgcn_exp2f(s[i] - ref);
           l += pr;
           const float* vr = &Vs[b][(8 * (i >> 2) + 4 * lh + (i & 3)) * LDV + lq];
 #pragma unroll
@@ -1208,9 +1215,10 @@ __global__ __launch_bounds__(64 * NW) void cross_keys_f32_kernel(CrossArgs a, in
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] *= al;
     }
+    const float ref = exp_ref(m_run);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float pr = __builtin_amdgcn_exp2f(s[i] - m_run);
+      const float pr = __builtin_amdgcn_exp2f(s[i] - ref);
       l += pr;
       const float* vr = &Vs[(8 * (i >> 2) + 4 * lh + (i & 3)) * LDV + lq];
 #pragma unroll

@@ -286,8 +286,8 @@ def cross_attention(q, k, v, max_len, kv_start=None, kv_len=None, kv_index=None,
     [n]: the text of each row (None: row i reads text i).  No text is longer
     than max_len.  heads may be a multiple of kv_heads (shared in order); q, k,
     v and out may be strided as long as d is contiguous.  scale defaults to
-    1 / sqrt(d).  A row without keys gives zeros.  Returns [n, n_q, heads, d]
-    in q's type."""
+    1 / sqrt(d).  Keys that score -inf take no weight; a row without keys of
+    any weight gives zeros.  Returns [n, n_q, heads, d] in q's type."""
     dt = q.dtype
     if dt is not torch.bfloat16 and dt is not torch.float32:
         raise TypeError(dt)
