@@ -1,18 +1,19 @@
 // Linear layer over a few rows with 4-bit weights in groups along K:
-//   out[m, n] = f(bias[n] + add[m, n] + sum_g s[n, g] (sum_{k in g} x[m, k] q[n, k] - z[n, g] sum_{k in g} x[m, k])).
+//   out[m, n] = f(bias[n] + add[m, n] + sum_g s[n, g] sum_{k in g} x[m, k] (q[n, k] - z[n, g])).
 //
 // Bound by the bytes of the codes, so they are read once, in their own
 // layout, 16 bytes a lane, and the arithmetic on them is kept to a few
 // instructions per 8 codes:
 //  * The products run on bf16 MFMAs (16 rows of x by 16 weight rows, 32 k).
 //    A code as a byte is the e4m3 number q * 2^-9 (subnormals and the first
-//    binade are one even ladder), so 8 codes become bf16 with two masks, a
-//    shift and four conversions, exactly.
-//  * The zero point stays outside the products: sum x over the group, the
-//    same for every weight row, comes from one more MFMA with ones (wide
-//    layers: from the pass that brings x into LDS).
-//  * A group's sums keep whole codes until its scale multiplies them in fp32:
-//    the weights are never rounded.
+//    binade are one even ladder), so 8 codes become fp32 with two masks, a
+//    shift and four conversions; the zero point is taken off there, and the
+//    differences, whole numbers below 16, are bf16 exactly.  (Taken off the
+//    sums, as z sum x, it costs ten instructions less, 14.1 us in place of 14.7
+//    for 16 rows of 8192 x 8192, but then an outlier of x that meets a weight of
+//    zero swamps the rest of its group.)
+//  * A group's sums keep whole differences until its scale multiplies them in
+//    fp32: the weights are never rounded.
 //  * fp32 x is cut into three bf16 parts of 8 bits each (their sum is x
 //    exactly), so its products are exact as well; the small parts are summed
 //    first, where fp32 rounds least.
@@ -56,22 +57,23 @@ __device__ __forceinline__ void transpose_groups(u32x4& r) {
 #endif
 }
 
-// 8 codes -> bf16, in the order of k.
-__device__ __forceinline__ u32x4 codes_bf16(uint32_t w) {
+// The high halves of a (first) and b as one dword.
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// code - zero point z of 8 codes -> bf16, in the order of k.
+__device__ __forceinline__ u32x4 codes_bf16(uint32_t w, float z) {
   u32x4 r = {0, 0, 0, 0};
 #if defined(__HIP_DEVICE_COMPILE__)
   const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
-  const uint32_t lo = __builtin_amdgcn_perm(odd, even, 0x05010400u), hi = __builtin_amdgcn_perm(odd, even, 0x07030602u);
-  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.f, false));
-  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.f, true));
-  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.f, false));
-  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.f, true));
+  const auto put = [&](auto e, auto o, int i) __attribute__((always_inline)) {
+    r[i] = high_halves(__float_as_uint(e[0] - z), __float_as_uint(o[0] - z));
+    r[i + 1] = high_halves(__float_as_uint(e[1] - z), __float_as_uint(o[1] - z));
+  };
+  put(__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, false), 0);
+  put(__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, true), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, true), 2);
 #endif
   return r;
 }
-
-// The high halves of a (first) and b as one dword.
-__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
 // SiLU where asked: one branch around all 8 (value by value the compiler
 // computes it always and picks: fp32, 16 rows of 4096 x 4096 12.3 us against 9.5).
@@ -131,8 +133,8 @@ struct Weights {
       }
     }
   }
-  template <typename V>
-  __device__ __forceinline__ V at(V v, int g) const { return __shfl(v, col + 16 * g, 64); }
+  __device__ __forceinline__ static float zero_of(const LinearW4Args& a, int z) { return a.zero ? (float)(z & 15) : 8.0f; }
+  __device__ __forceinline__ float at(float v, int g) const { return __shfl(v, col + 16 * g, 64); }
 };
 
 // The sum of nw waves' tiles ([T][MT][4][64] accumulators, `apart` floats apart)
@@ -164,7 +166,7 @@ __device__ __forceinline__ void finish(const LinearW4Args& a, const float* red, 
 // rows.  Neighbouring lanes load neighbouring bytes of a row (a lane per row,
 // as the MFMA wants it, takes the L1 one cycle per lane: 8192 x 8192, 16 rows
 // 18.8 us); a wave's own piece of LDS turns them into operands, without a
-// barrier: 14.2 us, 2.5 TB/s of codes.  Loading alone takes 7; the turn, the
+// barrier: 14.7 us, 2.4 TB/s of codes.  Loading alone takes 7; the turn, the
 // scales and the waves' sums are the rest.
 template <bool E8, int MT, int T>
 __host__ __device__ constexpr int w4_wave_bytes() { return T * 16 * 80 + MT * 16 * 17 * (E8 ? 8 : 16); }
@@ -238,14 +240,13 @@ __global__ __launch_bounds__(1024) void linear_w4_kernel(LinearW4Args a) {
     for (int t = 0; t < T; ++t) *(u32x4*)(wl + t * 16 * WROW + wput) = w[t];
 #pragma unroll
     for (int i = 0; i < 4 * MT; ++i) *(XPiece*)(xl + i * 4 * XROW + xput) = xn[i];
-    float s[T], xs[MT];
-    int z[T];
+    float s[T], z[T], xs[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) xs[i] = xsn[i];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       s[t] = sn[t];
-      z[t] = zn[t];
+      z[t] = wt.zero_of(a, zn[t]);
     }
     asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
     u32x4 q[T];
@@ -267,9 +268,11 @@ __global__ __launch_bounds__(1024) void linear_w4_kernel(LinearW4Args a) {
     f32x4 part[T][MT];  // e4m3: the chunk's sums, until its scale of x multiplies them
 #pragma unroll
     for (int g = 0; g < GC; ++g) {
-      f32x4 d[T][MT], sx[MT];
+      f32x4 d[T][MT];
       const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-      const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+      float zg[T];
+#pragma unroll
+      for (int t = 0; t < T; ++t) zg[t] = wt.at(z[t], g);
 #pragma unroll
       for (int j = g * JG; j < (g + 1) * JG; ++j) {
         const bool first = j == g * JG;
@@ -283,32 +286,30 @@ __global__ __launch_bounds__(1024) void linear_w4_kernel(LinearW4Args a) {
             b[i][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xp[i][j].y, 1.f, false));
             b[i][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xp[i][j].y, 1.f, true));
 #else
-            b[i] = ones;
+            b[i] = u32x4{0, 0, 0, 0};
 #endif
           } else {
             b[i] = xp[i][j];
           }
-          sx[i] = mfma(b[i], ones, first ? zero : sx[i]);
         }
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-          const u32x4 qb = codes_bf16(q[t][j]);
+          const u32x4 qb = codes_bf16(q[t][j], zg[t]);
 #pragma unroll
           for (int i = 0; i < MT; ++i) d[t][i] = mfma(b[i], qb, first ? zero : d[t][i]);
         }
       }
 #pragma unroll
       for (int t = 0; t < T; ++t) {
-        const float sg = wt.at(s[t], g), zg = a.zero ? (float)(wt.at(z[t], g) & 15) : 8.0f;
+        const float sg = wt.at(s[t], g);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float v = fmaf(-zg, sx[i][e], d[t][i][e]);
             if constexpr (E8)
-              part[t][i][e] = g == 0 ? sg * v : fmaf(sg, v, part[t][i][e]);
+              part[t][i][e] = g == 0 ? sg * d[t][i][e] : fmaf(sg, d[t][i][e], part[t][i][e]);
             else
-              acc[t][i][e] = fmaf(sg, v, acc[t][i][e]);
+              acc[t][i][e] = fmaf(sg, d[t][i][e], acc[t][i][e]);
           }
       }
     }
@@ -433,18 +434,16 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
   while (it.tile < tiles) {
     Item it1 = it;
     it1.next(wave, nw, chunks, gridDim.x);
-    float s[T];
-    int z[T];
+    float s[T], z[T], zg[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       *(u32x4*)(wl + t * 16 * WROW + wput) = wn[t];
       s[t] = sn[t];
-      z[t] = zn[t];
+      z[t] = wt.zero_of(a, zn[t]);
     }
     u32x4 q[T];
-    f32x4 d[T], e[T], sx, sy;  // products and sums of x: of the first part, of the others
+    f32x4 d[T], e[T];  // products: of the first part, of the others
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       put_x(xn);
@@ -467,25 +466,24 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
         u32x4 x[3];
 #pragma unroll
         for (int u = 0; u < 3; ++u) x[u] = *(const u32x4*)(xl + u * PART + j * 64 + xget);
-        if (jc * 32 % G == 0) {
-          sx = sy = zero;
+        if (jc * 32 % G == 0)
 #pragma unroll
-          for (int t = 0; t < T; ++t) d[t] = e[t] = zero;
-        }
-        sy = mfma(x[1], ones, mfma(x[2], ones, sy));
-        sx = mfma(x[0], ones, sx);
+          for (int t = 0; t < T; ++t) {
+            d[t] = e[t] = zero;
+            zg[t] = wt.at(z[t], g);
+          }
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-          const u32x4 b = codes_bf16(q[t][jc]);
+          const u32x4 b = codes_bf16(q[t][jc], zg[t]);
           e[t] = mfma(x[1], b, mfma(x[2], b, e[t]));
           d[t] = mfma(x[0], b, d[t]);
         }
         if ((jc + 1) * 32 % G == 0)
 #pragma unroll
           for (int t = 0; t < T; ++t) {
-            const float sg = wt.at(s[t], g), zg = a.zero ? (float)(wt.at(z[t], g) & 15) : 8.0f;
+            const float sg = wt.at(s[t], g);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(sg, fmaf(-zg, sx[i] + sy[i], d[t][i] + e[t][i]), acc[t][i]);
+            for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(sg, d[t][i] + e[t][i], acc[t][i]);
           }
       }
       asm volatile("" ::: "memory");
@@ -520,8 +518,7 @@ __global__ __launch_bounds__(1024) void linear_w4_wide_kernel(LinearW4Args a) {
   extern __shared__ float lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nwk = blockDim.x / NT;
   const int wn = wave % WN, wk = wave / WN, tid = threadIdx.x % NT;
-  bf16* xs = (bf16*)lds + wk * XB;                               // [3][ROWS][LD]
-  float* xsum = lds + nwk * (XB / 2) + wk * ROWS * GC;           // [GC][ROWS]
+  bf16* xs = (bf16*)lds + wk * XB;  // [3][ROWS][LD]
   const int n0 = blockIdx.x * 16 * WN, m0 = blockIdx.y * ROWS;
   const int col = lane & 15, grp = lane >> 4;
   const bool tile_on = n0 + 16 * wn < a.N;
@@ -554,12 +551,10 @@ __global__ __launch_bounds__(1024) void linear_w4_wide_kernel(LinearW4Args a) {
       const int idx = tid + p * NT, row = idx / 16;
       if (idx >= PIECES || m0 + row >= a.M) continue;  // (whole groups of 16 lanes)
       uint32_t part[3][8];
-      float sum = 0.f;
       silu_if(a.silu_in, xr[p]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float v = xr[p][e];
-        sum += v;
         // (an infinity or NaN leaves a NaN in the second part)
         part[0][e] = __float_as_uint(v);
         v -= __uint_as_float(part[0][e] & 0xFFFF0000u);
@@ -574,9 +569,6 @@ __global__ __launch_bounds__(1024) void linear_w4_wide_kernel(LinearW4Args a) {
         for (int e = 0; e < 4; ++e) b[e] = high_halves(part[u][2 * e], part[u][2 * e + 1]);
         *(u32x4*)(xs + (u * ROWS + row) * LD + 8 * (idx % 16)) = b;
       }
-#pragma unroll
-      for (int o = 1; o < G / 8; o <<= 1) sum += __shfl_xor(sum, o, 64);
-      if (idx % (G / 8) == 0) xsum[(idx % 16) / (G / 8) * ROWS + row] = sum;
     }
   };
 
@@ -611,7 +603,7 @@ __global__ __launch_bounds__(1024) void linear_w4_wide_kernel(LinearW4Args a) {
     for (int g = 0; g < GC; ++g) {
       u32x4 q[JG];
 #pragma unroll
-      for (int j = 0; j < JG; ++j) q[j] = codes_bf16(w[g * JG + j]);
+      for (int j = 0; j < JG; ++j) q[j] = codes_bf16(w[g * JG + j], z[g]);
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         f32x4 d = {0.f, 0.f, 0.f, 0.f};
@@ -620,9 +612,8 @@ __global__ __launch_bounds__(1024) void linear_w4_wide_kernel(LinearW4Args a) {
 #pragma unroll
           for (int j = 0; j < JG; ++j)
             d = mfma(*(const u32x4*)(xs + (u * ROWS + 16 * i + col) * LD + 32 * (g * JG + j) + 8 * grp), q[j], d);
-        const f32x4 sx = *(const f32x4*)(xsum + g * ROWS + 16 * i + 4 * grp);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(s[g], fmaf(-z[g], sx[e], d[e]), acc[i][e]);
+        for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(s[g], d[e], acc[i][e]);
       }
     }
   }
@@ -685,8 +676,8 @@ static void launch_wide(const LinearW4Args& a, hipStream_t s) {
   constexpr int WN = 8, MOST = 2;
   const int chunks = (a.K + KC - 1) / KC, nwk = chunks < MOST ? chunks : MOST;
   const dim3 grid((unsigned)((a.N + 16 * WN - 1) / (16 * WN)), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
-  // operands of x and their sums; the waves' sums take their place
-  constexpr size_t row = 3 * 16 * MT * (KC + 8) * 2 + 16 * MT * (KC / G) * 4;
+  // operands of x; the waves' sums take their place
+  constexpr size_t row = 3 * 16 * MT * (KC + 8) * 2;
   static_assert(row >= WN * MT * 1024 && MOST * row <= 160 * 1024, "the sums fit, and all of it the LDS");
   linear_w4_wide_kernel<MT, G><<<grid, 64 * WN * nwk, nwk * row, s>>>(a);
 }

@@ -1,10 +1,14 @@
-"""Edge values of the text-side operators on the GPU, against the oracle's
-float64 definitions."""
+"""Edge values of the text-side operators on the GPU: scores of -inf, outliers
+that meet a weight of zero, values near the ends of a type's range, offsets
+past 32 bits.  Against the oracle's float64 definitions; U32 and U16 are half a
+step of fp32 and bf16 relative to the value."""
 import math
 
+import numpy as np
 import pytest
 
-from test_gpu_text_ops import _attn_case, _check_attn, ops  # noqa: F401
+from oracle import text as O
+from test_gpu_text_ops import U16, U32, _attn_case, _check_attn, _gen, _np, _t, ops  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -45,3 +49,66 @@ def test_cross_attention_minus_inf_scores(ops, nq, heads, kvh, d, length, dt):  
                 assert not got[:, hit].any(), what
             if overflow and nq > 1:
                 _check_attn(got[:, ~hit], qz[:, ~hit], kz, v, [range(L)], dt, what + " others")
+
+
+# ------------------------------------------------------------------ 4-bit weights: outliers and the ends of the range
+W4_FORMS = [(1, 320, 100), (16, 1288, 65), (33, 2184, 130), (5, 264, 4104), (40, 136, 8200), (3, 264, 16401), (20, 136, 16385)]
+
+
+def _w4(g, M, K, N, group, zero):
+    ng = -(-K // group)
+    w = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scale = (torch.rand(N, ng, generator=g, device="cuda") + 0.5) * 0.1
+    z = torch.randint(0, 16, (N, ng), generator=g, device="cuda", dtype=torch.uint8) if zero else None
+    return w, scale, z, torch.randn(M, K, generator=g, device="cuda")
+
+
+def _w4_bound(x, xs, w, scale, z, group, silu_in=False):
+    """The result in float64 and sum |x w|.  Products are exact and summed in
+    fp32, each step off by at most a unit in the last place (2 U32: the matrix
+    unit's inner sums are not assumed to round to nearest) of no more than that
+    sum: (3 K / 4 + 64) steps cover K products in three parts, four or more to
+    a step, and the chunks' and waves' sums."""
+    a = _np(x)
+    if xs is not None:
+        a = a * np.repeat(_np(xs), a.shape[1] if xs.shape[1] == 1 else 128, 1)[:, :a.shape[1]]
+    if silu_in:
+        a = a / (1 + np.exp(-a))
+    wt = O.w4_weights(w.cpu().numpy(), _np(scale), None if z is None else _np(z), group)
+    return a @ wt.T, np.abs(a) @ np.abs(wt).T
+
+
+def _w4_close(got, ref, size, K, what, extra=0.0):
+    got = _np(got)
+    assert np.isfinite(got).all(), what
+    err, tol = np.abs(got - ref), 2 * U32 * (0.75 * K + 64) * size + extra
+    assert (err <= tol).all(), f"{what}: {err.max():.3e}, {(err / np.maximum(tol, 1e-300)).max():.2f} of the tolerance"
+
+
+@pytest.mark.parametrize("xt", ["f32", "bf16", "e4m3row", "e4m3"])
+@pytest.mark.parametrize("M,K,N", W4_FORMS)
+def test_linear_rows_w4_outliers_on_zero_weights(ops, M, K, N, xt):  # noqa: F811
+    """Channels of x some 10^4 to 10^6 times the others whose weights are all
+    zero (code = zero point) leave the others' sum as exact as without them."""
+    for group in (32, 64, 128):
+        for zero in (False, True):
+            g = _gen(M + K + N + group + zero)
+            w, scale, z, x = _w4(g, M, K, N, group, zero)
+            big = torch.randint(0, K, (4,), generator=g, device="cuda").tolist()
+            for c in big:  # the byte's half that holds channel c takes the zero point
+                zc = torch.full((N,), 8, device="cuda", dtype=torch.uint8) if z is None else z[:, c // group]
+                b = w[:, c // 2]
+                w[:, c // 2] = (b & 0xF0) | zc if c % 2 == 0 else (b & 0x0F) | (zc << 4)
+            xs = None
+            if xt.startswith("e4m3"):  # the format holds 448 beside 2^-9: a factor of 2^17 at most
+                blocks = 1 if xt == "e4m3row" else -(-K // 128)
+                xs = torch.rand(M, blocks, generator=g, device="cuda") + 0.5
+                x = (x * 2.0 ** -6).to(torch.float8_e4m3fn)
+                x[:, big] = torch.tensor(448.0, device="cuda").to(torch.float8_e4m3fn)
+            else:
+                x[:, big] = torch.tensor([1e4, -1e5, 1e6, 3e6], device="cuda")
+                x = x.to(_t(xt))
+            ref, size = _w4_bound(x, xs, w, scale, z, group)
+            got = ops.linear_rows_w4(x, w, scale, group, zero=z, x_scale=xs)
+            # (the e4m3 row scales and their products: 4 more roundings)
+            _w4_close(got, ref, size, K, f"{(M, K, N, xt, group, zero)}", 8 * U32 * size)
