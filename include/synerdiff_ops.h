@@ -220,7 +220,9 @@ sd_status synerdiff_op_rmsnorm(int32_t dtype, const void* d_x, int64_t x_ld, con
  * out [M, N] in out_type SD_F32 or SD_BF16, row m at m * out_ld; bias fp32 [N], add
  * fp32 [M, N], may be NULL; add may equal an fp32 out of out_ld = N; out
  * overlaps nothing else.  Products x * (q - zero) are exact for every x_type
- * (bits of an fp32 x below 2^-133 apart) and summed in fp32.  A row of x with an infinity or NaN gives no finite value.
+ * (bits of an fp32 x below 2^-133 apart) and summed in fp32; a group's sum may
+ * pass fp32's range as long as scale times it does not.  |scale| below 2^116.
+ * A row of x with an infinity or NaN gives no finite value.
  * K a multiple of 8; K, N and x_ld <= 2^24, M <= 2^19 (SD_ERR_UNSUPPORTED past
  * them); x and its rows 16-byte aligned (e4m3: 8).  The rows of a result do not
  * depend on M.  M = 0 or N = 0 does nothing. */

@@ -12,8 +12,10 @@
 //    sums, as z sum x, it costs ten instructions less, 14.1 us in place of 14.7
 //    for 16 rows of 8192 x 8192, but then an outlier of x that meets a weight of
 //    zero swamps the rest of its group.)
-//  * A group's sums keep whole differences until its scale multiplies them in
-//    fp32: the weights are never rounded.
+//  * The differences are held 2^11 times too small, so that their products with
+//    a group's 128 finite x add up to a finite sum (128 * 15 < 2^11).  The
+//    group's scale, 2^11 times as large, multiplies that sum in fp32: the
+//    weights are never rounded.
 //  * fp32 x is cut into three bf16 parts of 8 bits each (their sum is x
 //    exactly), so its products are exact as well; the small parts are summed
 //    first, where fp32 rounds least.
@@ -60,7 +62,9 @@ __device__ __forceinline__ void transpose_groups(u32x4& r) {
 // The high halves of a (first) and b as one dword.
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// code - zero point z of 8 codes -> bf16, in the order of k.
+constexpr float DOWN = 1.0f / 2048;  // codes and zero points are held this much smaller
+
+// (code - zero point) * DOWN of 8 codes -> bf16, in the order of k; z: the zero point * DOWN.
 __device__ __forceinline__ u32x4 codes_bf16(uint32_t w, float z) {
   u32x4 r = {0, 0, 0, 0};
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -69,8 +73,8 @@ __device__ __forceinline__ u32x4 codes_bf16(uint32_t w, float z) {
     r[i] = high_halves(__float_as_uint(e[0] - z), __float_as_uint(o[0] - z));
     r[i + 1] = high_halves(__float_as_uint(e[1] - z), __float_as_uint(o[1] - z));
   };
-  put(__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, false), 0);
-  put(__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, true), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, true), 2);
+  put(__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f * DOWN, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f * DOWN, false), 0);
+  put(__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f * DOWN, true), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f * DOWN, true), 2);
 #endif
   return r;
 }
@@ -133,7 +137,9 @@ struct Weights {
       }
     }
   }
-  __device__ __forceinline__ static float zero_of(const LinearW4Args& a, int z) { return a.zero ? (float)(z & 15) : 8.0f; }
+  // what the products take of them: the scale / DOWN, the zero point * DOWN
+  __device__ __forceinline__ static float scale_up(float s) { return s * (1.0f / DOWN); }
+  __device__ __forceinline__ static float zero_down(const LinearW4Args& a, int z) { return (a.zero ? (float)(z & 15) : 8.0f) * DOWN; }
   __device__ __forceinline__ float at(float v, int g) const { return __shfl(v, col + 16 * g, 64); }
 };
 
@@ -245,8 +251,8 @@ __global__ __launch_bounds__(1024) void linear_w4_kernel(LinearW4Args a) {
     for (int i = 0; i < MT; ++i) xs[i] = xsn[i];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      s[t] = sn[t];
-      z[t] = wt.zero_of(a, zn[t]);
+      s[t] = wt.scale_up(sn[t]);
+      z[t] = wt.zero_down(a, zn[t]);
     }
     asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
     u32x4 q[T];
@@ -438,8 +444,8 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       *(u32x4*)(wl + t * 16 * WROW + wput) = wn[t];
-      s[t] = sn[t];
-      z[t] = wt.zero_of(a, zn[t]);
+      s[t] = wt.scale_up(sn[t]);
+      z[t] = wt.zero_down(a, zn[t]);
     }
     u32x4 q[T];
     f32x4 d[T], e[T];  // products: of the first part, of the others
@@ -590,8 +596,8 @@ __global__ __launch_bounds__(1024) void linear_w4_wide_kernel(LinearW4Args a) {
 #pragma unroll
     for (int g = 0; g < GC; ++g) {
       const long i = sat + min(c * GC + g, a.groups - 1);
-      s[g] = a.scale_f32 ? ((const float*)a.scale)[i] : (float)((const bf16*)a.scale)[i];
-      z[g] = a.zero ? (float)(a.zero[i] & 15) : 8.0f;
+      s[g] = (a.scale_f32 ? ((const float*)a.scale)[i] : (float)((const bf16*)a.scale)[i]) * (1.0f / DOWN);
+      z[g] = (a.zero ? (float)(a.zero[i] & 15) : 8.0f) * DOWN;
     }
     if (c + nwk < chunks) {
       fetch(c + nwk);

@@ -112,3 +112,22 @@ def test_linear_rows_w4_outliers_on_zero_weights(ops, M, K, N, xt):  # noqa: F81
             got = ops.linear_rows_w4(x, w, scale, group, zero=z, x_scale=xs)
             # (the e4m3 row scales and their products: 4 more roundings)
             _w4_close(got, ref, size, K, f"{(M, K, N, xt, group, zero)}", 8 * U32 * size)
+
+
+@pytest.mark.parametrize("xt", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", W4_FORMS)
+def test_linear_rows_w4_ends_of_the_range(ops, M, K, N, xt):  # noqa: F811
+    """x near the largest and the smallest numbers of its type, where the
+    result is neither.  (Parts of an fp32 x end at bf16's smallest number, 2^-133.)"""
+    for group, zero in ((32, True), (64, False), (128, True), (128, False)):
+        g = _gen(M + K + group + zero)
+        w, scale, z, x = _w4(g, M, K, N, group, zero)
+        sign = torch.where(x < 0, -1.0, 1.0)
+        top = (sign * torch.finfo(_t(xt)).max).to(_t(xt))
+        s = scale / (4 * K)  # sum |x w| < 3.4e38 * 15 * 0.15 / 4
+        ref, size = _w4_bound(top, None, w, s, z, group)
+        _w4_close(ops.linear_rows_w4(top, w, s, group, zero=z), ref, size, K, f"{(M, K, N, xt, group, zero)} large")
+        low = (x * 2.0 ** -118).to(_t(xt))
+        ref, size = _w4_bound(low, None, w, scale * 2.0 ** 110, z, group)
+        extra = 2.0 ** -133 * K * 15 * 0.15 * 2.0 ** 110 if xt == "f32" else 0.0
+        _w4_close(ops.linear_rows_w4(low, w, scale * 2.0 ** 110, group, zero=z), ref, size, K, f"{(M, K, N, xt, group, zero)} small", extra)
