@@ -240,7 +240,10 @@ sd_status synerdiff_op_linear_rows_w4(int32_t x_type, const void* d_x, int64_t x
  * 0 (NULL: all do).  Keys that take no part are not read: they may hold
  * anything.  A row without a key, or whose kv_index lies outside [0, n_ctx),
  * gives zeros.  Keys that score -inf take no weight, and a row whose keys all
- * do gives zeros.
+ * do gives zeros.  Scores, sums and results are fp32 until the result is
+ * rounded to dtype.  bf16 probabilities are rounded to bf16 (by up to 2^-8 of
+ * each) where a K/V head has more than 128 rows, heads / kv_heads * n_q; up to
+ * 128 keep 2^-17.
  * Layouts: element (i, t, h, e) of q is at q + i * q_img + t * q_ld + h *
  * q_head + e, o likewise.  Contexts one after another (d_kv_start not NULL):
  * key j of context c is row kv_start[c] + j of k: k + row * k_ld + g *
