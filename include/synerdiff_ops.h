@@ -188,7 +188,8 @@ sd_status synerdiff_op_conv_out_cfg_ddim(int32_t dtype, const void* d_x, int32_t
  *   h[t, c] = x[t, c] + resid[t, c]        (x alone when resid is NULL)
  *   y[t, c] = h[t, c] / sqrt(mean_c(h[t, c]^2) + eps) * gamma[c]
  * x, resid, sum in `dtype`; row t of each starts at t * its ld (elements, >=
- * C).  h is kept in fp32 for the norm; d_sum (may be NULL; NULL without
+ * C).  h is kept in fp32 for the norm, at any finite size (with eps below
+ * 2^-100 a row wants a value of 2^-60 or more: smaller squares vanish); d_sum (may be NULL; NULL without
  * resid) receives it rounded to dtype.  gamma fp32 [C] or NULL (all ones).
  * y_type = dtype: y is rounded to dtype.  y_type = SD_E4M3: per row, or per
  * block of 128 channels of a row (the last block may be narrower),

@@ -6,6 +6,8 @@
 // maxima come from the registers.  Bound by memory: 48 x 4096 rows of 320 bf16
 // with a residual 93 us, 12301 of 1280 to e4m3 20 us, both 5.4 TB/s; one row
 // 3 us, a launch and one round trip.
+#include <type_traits>
+
 #include "device_common.h"
 #include "kernels.h"
 
@@ -125,21 +127,38 @@ __global__ __launch_bounds__(256) void rmsnorm_kernel(RmsNormArgs a) {
     }
   }
 
-  float sq = 0.f;
-#pragma unroll
-  for (int i = 0; i < R; ++i)
-#pragma unroll
-    for (int e = 0; e < N; ++e) sq = fmaf(h[i][e], h[i][e], sq);
-#pragma unroll
-  for (int o = 1; o < (TPR < 64 ? TPR : 64); o <<= 1) sq += __shfl_xor(sq, o, 64);
-  __shared__ float part[4];
+  __shared__ float part[2][4];
   __shared__ uint32_t partm[4];
-  if constexpr (TPR == 256) {
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sq;
-    __syncthreads();
-    sq = (part[0] + part[1]) + (part[2] + part[3]);
+  // the row's sum of squares of f * h (the same in all its lanes)
+  auto squares = [&](auto scaled, float f) __attribute__((always_inline)) {
+    constexpr bool S = decltype(scaled)::value;
+    float sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float v = S ? h[i][e] * f : h[i][e];
+        sq = fmaf(v, v, sq);
+      }
+#pragma unroll
+    for (int o = 1; o < (TPR < 64 ? TPR : 64); o <<= 1) sq += __shfl_xor(sq, o, 64);
+    if constexpr (TPR == 256) {
+      if ((threadIdx.x & 63) == 0) part[S][threadIdx.x >> 6] = sq;
+      __syncthreads();
+      sq = (part[S][0] + part[S][1]) + (part[S][2] + part[S][3]);
+    }
+    return sq;
+  };
+  // A row whose squares pass fp32's range (values of 2^57 and more) is summed
+  // again 2^80 times smaller, eps with it; its norm is undone in two steps.
+  constexpr float DOWN = 0x1p-80f;
+  float sq = squares(std::false_type{}, 1.f), eps = a.eps;
+  const bool large = sq == INFINITY;  // (the same in all lanes of a row)
+  if (large) {
+    sq = squares(std::true_type{}, DOWN);
+    eps = eps * DOWN * DOWN;
   }
-  const float rstd = 1.0f / sqrtf(sq / (float)C + a.eps);
+  const float rstd = 1.0f / sqrtf(sq / (float)C + eps);
 
   if (a.sum && on) {
     T* sum = (T*)a.sum + row * a.sum_ld;
@@ -160,6 +179,9 @@ __global__ __launch_bounds__(256) void rmsnorm_kernel(RmsNormArgs a) {
     const int c = (i * TPR + lane) * N;
 #pragma unroll
     for (int e = 0; e < N; ++e) h[i][e] *= rstd;
+    if (large)
+#pragma unroll
+      for (int e = 0; e < N; ++e) h[i][e] *= DOWN;
     if (a.gamma) {
       if (c + N <= C) {
         float g[N];

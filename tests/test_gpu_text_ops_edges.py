@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 from oracle import text as O
-from test_gpu_text_ops import U16, U32, _attn_case, _check_attn, _gen, _np, _t, ops  # noqa: F401
+from test_gpu_text_ops import U16, U32, _attn_case, _check_attn, _check_norm, _gen, _np, _t, ops  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -131,3 +131,25 @@ def test_linear_rows_w4_ends_of_the_range(ops, M, K, N, xt):  # noqa: F811
         ref, size = _w4_bound(low, None, w, scale * 2.0 ** 110, z, group)
         extra = 2.0 ** -133 * K * 15 * 0.15 * 2.0 ** 110 if xt == "f32" else 0.0
         _w4_close(ops.linear_rows_w4(low, w, scale * 2.0 ** 110, group, zero=z), ref, size, K, f"{(M, K, N, xt, group, zero)} small", extra)
+
+
+# ------------------------------------------------------------------ rmsnorm: squares past fp32's range
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [1, 7, 16, 40, 129, 320, 1280, 2056, 5000, 8192, 16384])
+def test_rmsnorm_large_rows(ops, C, dt):  # noqa: F811
+    """Rows of 1e19 to 1e38, whole or in one value, beside ordinary ones; the residual alike."""
+    g = _gen(C)
+    rows = 37
+    x = torch.randn(rows, C, generator=g, device="cuda").clamp(-3, 3)
+    r = torch.randn(rows, C, generator=g, device="cuda").clamp(-3, 3)
+    x[::4] *= 1e38
+    x[1::8] *= 2e19
+    x[2::8, C // 2] = -2e30
+    r[::4] *= 1e10
+    r[3::8] *= 3e25
+    x, r, gamma = x.to(_t(dt)), r.to(_t(dt)), 1 + 0.1 * torch.randn(C, generator=g, device="cuda")
+    for eps in (1e-6, 0.0, 1e30):
+        for resid in (None, r):
+            for fp8, group in ((False, 0), (True, 0), (True, 128)):
+                got = ops.rmsnorm(x, gamma, eps, resid=resid, fp8=fp8, scale_group=group)
+                _check_norm(got, x, gamma, eps, resid, fp8, group, dt, f"{(C, dt, eps, resid is not None, fp8, group)}")
