@@ -251,12 +251,20 @@ __global__ __launch_bounds__(256) void rmsnorm_kernel(RmsNormArgs a) {
     if (c >= C) continue;
     const float s = __uint_as_float(top[i]) / 448.f;
     if (grouped ? lane % BL == 0 : i == 0 && lane == 0) a.scale[row * a.blocks + (grouped ? c / 128 : 0)] = s;
-    const float inv = 1.0f / s;
+    // y / s: the product with 1 / s is off by up to 1.5 units in the last place, which
+    // one step on what it leaves of y mends.  (s infinite: 0, and NaN for infinite y.)
+    const float inv = 1.0f / s, by = s == INFINITY ? 0.f : s;
+    float v[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float c0 = h[i][e] * inv;
+      v[e] = fmaf(fmaf(-c0, by, h[i][e]), inv, c0);
+    }
     uint32_t q[N / 4];
 #pragma unroll
     for (int e = 0; e < N; e += 4) {
-      int p = __builtin_amdgcn_cvt_pk_fp8_f32(h[i][e] * inv, h[i][e + 1] * inv, 0, false);
-      q[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(h[i][e + 2] * inv, h[i][e + 3] * inv, p, true);
+      int p = __builtin_amdgcn_cvt_pk_fp8_f32(v[e], v[e + 1], 0, false);
+      q[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[e + 2], v[e + 3], p, true);
     }
     if (c + N <= C) {
       if constexpr (ANY && N == 8) {

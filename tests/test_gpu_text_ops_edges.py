@@ -153,3 +153,33 @@ def test_rmsnorm_large_rows(ops, C, dt):  # noqa: F811
             for fp8, group in ((False, 0), (True, 0), (True, 128)):
                 got = ops.rmsnorm(x, gamma, eps, resid=resid, fp8=fp8, scale_group=group)
                 _check_norm(got, x, gamma, eps, resid, fp8, group, dt, f"{(C, dt, eps, resid is not None, fp8, group)}")
+
+
+@pytest.mark.parametrize("C", [16, 96, 160, 320, 2056, 5000])
+def test_rmsnorm_e4m3_codes_are_of_the_quotient(ops, C):  # noqa: F811
+    """y8 = e4m3(y / s) to the bit, with values near the middle between two
+    codes, where a product with a rounded 1 / s falls on the other side.  (These
+    widths are normed alike with and without an 8-bit output, so fp32's y is the y.)"""
+    g = _gen(C)
+    x = torch.ones(64, C, device="cuda") * (1 + torch.rand(64, 1, generator=g, device="cuda"))
+    for turn in range(6):
+        middle = 17.0 + 2 * torch.randint(0, 4, (C,), generator=g, device="cuda")
+        middle *= torch.exp2(torch.randint(-6, 5, (C,), generator=g, device="cuda").float())
+        middle[::16] = 448  # (every block's largest: s is about 1 times the factor below)
+        gamma = middle * (1 + torch.rand(1, generator=g, device="cuda"))
+        y = ops.rmsnorm(x, gamma, 1e-6)
+        for group in (0, 128) if C > 256 or C < 128 else (0,):
+            q, s = ops.rmsnorm(x, gamma, 1e-6, fp8=True, scale_group=group)
+            full = s.repeat_interleave(group or C, 1)[:, :C]
+            assert torch.equal(s[:, 0].cpu(), y[:, :group or C].abs().amax(1).cpu() / 448)
+            assert torch.equal(q.cpu().view(torch.uint8), (y.cpu() / full.cpu()).to(torch.float8_e4m3fn).view(torch.uint8)), (C, turn, group)
+
+
+def test_rmsnorm_e4m3_infinite_scale(ops):  # noqa: F811
+    """A row whose y is infinite: its scale is, the finite values' codes are 0."""
+    gamma = torch.ones(384, device="cuda")
+    gamma[100] = math.inf
+    for group, cols in ((0, 384), (128, 128)):
+        q, s = ops.rmsnorm(torch.ones(3, 384, device="cuda"), gamma, fp8=True, scale_group=group)
+        q, rest = q.float(), [i for i in range(cols) if i != 100]
+        assert torch.isinf(s[:, 0]).all() and torch.isnan(q[:, 100]).all() and not q[:, rest].any()
