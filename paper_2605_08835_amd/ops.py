@@ -147,6 +147,11 @@ def _bad(what):
     raise ValueError(what)
 
 
+def _int32(largest):
+    if largest >= 1 << 31:  # (ctypes would pass the low 32 bits)
+        _bad("a size of 2^31 or more")
+
+
 def _enqueue(fn, like, others, args):
     """fn(*args, stream) on the device of `like`, which the tensors `others` (or
     None) share.  (The raw-stream and device queries cost 0.2 us together, the
@@ -189,6 +194,7 @@ def rmsnorm(x, gamma=None, eps=1e-6, resid=None, sum_out=None, out=None, fp8=Fal
         raise TypeError(dt)
     shape = x.shape
     C = shape[-1] if shape else _bad("x must have rows")
+    _int32(C)
     x_ld = _row_stride(x, "x")
     r_ld = s_ld = 0
     if resid is not None:
@@ -237,6 +243,7 @@ def linear_rows_w4(x, w, scale, group, zero=None, x_scale=None, bias=None, add=N
         _bad("x must be [M, K], w uint8 [N, K / 2]")
     M, K = x.shape
     N, half = w.shape
+    _int32(max(M, K, N))
     if group != 128 and group != 64 and group != 32:
         _bad("group must be 32, 64 or 128")
     if K == 0 or K % 8 or half * 2 != K or not w.is_contiguous():
@@ -311,6 +318,7 @@ def cross_attention(q, k, v, max_len, kv_start=None, kv_len=None, kv_index=None,
         n_ctx, tokens, k_ctx, v_ctx = kshape[0], 0, ks[0], vs[0]
         if kshape[1] != max_len:
             _bad("padded k, v must be [n_ctx, max_len, kv_heads, d]")
+    _int32(max(n, n_q, heads, kv_heads, d, n_ctx, abs(max_len)))
     start_p = _index(kv_start, n_ctx, "kv_start") if packed else None
     len_p = _index(kv_len, n_ctx, "kv_len") if kv_len is not None else None
     index_p = _index(kv_index, n, "kv_index") if kv_index is not None else None
