@@ -183,3 +183,79 @@ def test_rmsnorm_e4m3_infinite_scale(ops):  # noqa: F811
         q, s = ops.rmsnorm(torch.ones(3, 384, device="cuda"), gamma, fp8=True, scale_group=group)
         q, rest = q.float(), [i for i in range(cols) if i != 100]
         assert torch.isinf(s[:, 0]).all() and torch.isnan(q[:, 100]).all() and not q[:, rest].any()
+
+
+# ------------------------------------------------------------------ sizes past 2^31
+def _room(gib):
+    if torch.cuda.mem_get_info()[0] < gib << 30:
+        pytest.skip("not enough free memory")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_rmsnorm_more_rows_than_one_launch(ops, dt):  # noqa: F811
+    """More than 2^23 rows: the same bits as each part alone, right at the seam."""
+    _room(16)
+    g = _gen(9)
+    rows, C, seam = (1 << 23) + 133, 24, 1 << 23
+    x, r = (torch.randn(rows, C, generator=g, device="cuda").to(_t(dt)) for _ in range(2))
+    gamma = 1 + 0.1 * torch.randn(C, generator=g, device="cuda")
+    for fp8 in (False, True):
+        whole = ops.rmsnorm(x, gamma, 1e-6, resid=r, fp8=fp8)
+        for a, b in ((0, 1000), (seam - 77, seam + 77), (seam, rows), (rows - 1, rows)):
+            part = ops.rmsnorm(x[a:b], gamma, 1e-6, resid=r[a:b], fp8=fp8)
+            for w, p in zip(whole, part):
+                assert torch.equal(w[a:b].view(torch.uint8), p.view(torch.uint8)), (fp8, a)
+        _check_norm(tuple(w[seam - 9:seam + 9] for w in whole), x[seam - 9:seam + 9], gamma, 1e-6, r[seam - 9:seam + 9], fp8, 0, dt, f"seam {fp8}")
+
+
+@pytest.mark.parametrize("xt,M,K,N", [("bf16", 5, 32768, 140003), ("bf16", 20, 262400, 16400), ("f32", 3, 262400, 16383),
+                                      ("f32", 2, 32768, 140003), ("e4m3", 3, 32768, 140003)])
+def test_linear_rows_w4_codes_past_2_31_bytes(ops, xt, M, K, N):  # noqa: F811
+    _room(16)
+    g = _gen(K)
+    w, scale, z, x = _w4(g, M, K, N, 128, True)
+    assert w.numel() > 1 << 31
+    x, xs = (x.to(_t(xt)), None) if xt != "e4m3" else (x.to(torch.float8_e4m3fn), torch.ones(M, 1, device="cuda"))
+    got = ops.linear_rows_w4(x, w, scale, 128, zero=z, x_scale=xs)
+    seam = (1 << 31) // (K // 2)
+    for a in (0, seam - 20, N - 40):
+        ref, size = _w4_bound(x, xs, w[a:a + 40], scale[a:a + 40], z[a:a + 40], 128)
+        _w4_close(got[:, a:a + 40], ref, size, K, f"{(xt, M, K, N, a)}", 8 * U32 * size)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_cross_attention_keys_past_2_31_elements(ops, dt):  # noqa: F811
+    """K and V rows behind 2^31 elements, for every form of the kernels."""
+    rows, ld, d, L = 70000, 33024, 40, 200
+    _room(16)
+    store = torch.empty(rows * ld, device="cuda", dtype=_t(dt))
+    k, v = store.as_strided((rows, 1, d), (ld, d, 1)), store.as_strided((rows, 1, d), (ld, d, 1), 64)
+    a = rows - L
+    g = _gen(3)
+    for t in (k, v):
+        t[a:].copy_(torch.randn(L, 1, d, generator=g, device="cuda"))
+    q = torch.randn(1, 530, 1, d, generator=g, device="cuda").to(_t(dt))
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32).cuda()  # noqa: E731
+    for nq, most in ((1, L), (8, L), (40, L), (200, 90), (200, L), (530, L), (1, 5000), (40, 5000), (200, 5000)):
+        n = min(most, L)
+        got = ops.cross_attention(q[:, :nq], k, v, most, kv_start=ints(a), kv_len=ints(n))
+        _check_attn(got, q[:, :nq], k[a:a + n], v[a:a + n], [range(n)], dt, f"far {(dt, nq, most)}")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("nq,most", [(300, 60), (300, 150), (300, 700), (128, 150)])
+def test_cross_attention_queries_past_2_31_elements(ops, nq, most, dt):  # noqa: F811
+    """Queries and results 2^23 elements apart, two images."""
+    ld, d, heads = 1 << 23, 24, 2
+    img = nq * ld + 64
+    _room(64)
+    qs, os = (torch.empty(2 * img, device="cuda", dtype=_t(dt)).as_strided((2, nq, heads, d), (img, ld, 32, 1)) for _ in range(2))
+    g = _gen(nq)
+    q = torch.randn(2, nq, heads, d, generator=g, device="cuda").to(_t(dt))
+    k, v = (torch.randn(2, 60, 1, d, generator=g, device="cuda").to(_t(dt)) for _ in range(2))
+    qs.copy_(q)
+    pad = lambda t: torch.nn.functional.pad(t, (0, 0, 0, 0, 0, most - 60))  # noqa: E731
+    kw = dict(kv_len=torch.tensor([60, 41], dtype=torch.int32, device="cuda"))
+    ops.cross_attention(qs, pad(k), pad(v), most, out=os, **kw)
+    assert torch.equal(os.contiguous(), ops.cross_attention(q, pad(k), pad(v), most, **kw))
+    _check_attn(os, q, k, v, [range(60), range(60, 101)], dt, f"{(nq, most, dt)}")
