@@ -571,8 +571,8 @@ __global__ __launch_bounds__(256, D16 <= 48 || (D16 == 64 && !SHORT) ? 3 : D16 <
     // summed as rounded, so that the rounding cancels where one key prevails.
     // Against 64 bits a result is 0.0022 off in the mean then (16 x 1024 rows
     // over 200 to 512 keys), 0.0017 with fp32 probabilities, where only the result
-    // is rounded.  Keeping the rest as a second part, as for few rows, takes 75 us in
-    // place of 59 there, and 99 in place of 91 for 48 x 4096 rows over up to 77 keys.
+    // is rounded.  Keeping the rest as a second part, as for few rows, takes 82 us in
+    // place of 59 there, and 104 in place of 91 for 48 x 4096 rows over up to 77 keys.
 #pragma unroll
     for (int u = 0; u < 2 * NKT; ++u) {
       bf16x8 vf[ND];
