@@ -112,8 +112,17 @@ static int place_together(const CrossArgs& a, int el) {
 }
 
 // The kernel of a call, by the rows of a K/V head, and its ranges of `keys` (0:
-// not split): kind 0 up to 8 rows, 1 up to 128, 2 past that.  1024 keys a range: one query over
-// 9000 to 16384 keys, 4 x 20 heads of 64 71 us (512: 77, 2048: 72), 2 x 16 queries over 4000 to 8000 19 (23, 20).
+// not split): kind 0 up to 8 rows, 1 up to 128, 2 past that.  The ranges cannot
+// follow the number of images or the longest text (a row's bits), so each is a
+// compromise between calls that fill the card and calls that do not (us; n x
+// queries, heads of 64 over so many keys):
+//   up to 128 rows 1024 keys (in brackets 512, 2048): 4 x 1, 20 heads, 9000 to
+//   16384 64 (63, 68); 1 x 16, 8 heads, 4000 to 8000 16 (13, 23); 32 x 40, 8
+//   heads, 300 to 700 15 (28, 14);
+//   up to 512 rows 512 keys (1024, not split): 1 x 200, 8 heads, 4000 to 8000 22
+//   (29, 144); 8 x 512, 20 heads, 600 to 1100 95 (96, 44);
+//   past that not split (512 keys): 16 x 1024, 20 heads, 600 to 1100 126 (337);
+//   1 x 1024, 8 heads, 16000 285 (79).
 struct Plan {
   int kind, keys, splits;
 };
@@ -408,13 +417,15 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 // becomes the sum of the (rounded) probabilities.  Four waves of 32 rows.
 // SHORT: no text is longer than the two tiles that LDS holds; they are staged
 // once, and the waves pass `passes` groups of rows each over them without
-// meeting again (48 x 4096 rows, 8 heads of 40, up to 77 keys: 95 us, staging
+// meeting again (48 x 4096 rows, 8 heads of 40, up to 77 keys: 91 us, staging
 // them for every 128 rows 149).  Its arithmetic on a row is the same.  What
 // bounds it is memory: 80-byte rows of a 640-byte token reach 3.3 TB/s with the
 // arithmetic left out, which alone takes 47 us; three waves per SIMD hide part
 // of one behind the other.
-// Otherwise the vector unit bounds it, the exponentials above all: 16 x 1024
-// rows, 20 heads of 64, padded texts of 200 to 512 keys 64 us, 400 TFLOP/s.
+// Otherwise a wave's order of work on a tile bounds it, which only other waves
+// overlap: score products, maximum, exponentials, value products (vector ALU
+// busy 54 % of the time, the matrix unit 27 %): 16 x 1024 rows, 20 heads of 64,
+// padded texts of 200 to 512 keys 59 us, 430 TFLOP/s.
 // Two waves per SIMD up to 128 channels, though a few registers spill there (8 x
 // 2048 rows, 8 heads of 128, up to 512 keys: 61 us against 66).
 template <int D16, bool SF, bool SHORT>

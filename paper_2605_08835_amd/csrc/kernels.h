@@ -186,7 +186,7 @@ struct RmsNormArgs {
   int y8;                            // 1: y is e4m3, with scale[t * blocks + b]
   void* y; long y_ld;
   float* scale;
-  int blocks, group;                 // scale blocks per row, channels per block (C: one per row)
+  int blocks;                        // scale blocks per row: 1, or one per 128 channels
 };
 hipError_t launch_rmsnorm(DType dt, const RmsNormArgs& a, hipStream_t s);
 constexpr int RMSNORM_MAX_C = 16384;

@@ -513,7 +513,7 @@ __global__ __launch_bounds__(1024) void linear_w4_f32_kernel(LinearW4Args a) {
 
 // The same for wide layers: WN waves side by side (16 weight rows each) share
 // one pass of x through LDS, wave rows wk split K.  (20160 x 1280, fp32 under
-// SiLU: 1 row 11.0 us against 14.3 above, 32 rows 17.9 against 29.6; narrower
+// SiLU: 1 row 11.3 us against 13.6 above, 32 rows 17.9 against 27.9; narrower
 // layers leave it too few waves: 8192 x 8192, 1 row 61 us against 20.)  Bound by
 // bringing x in, activated and cut, once per block, and its LDS reads.
 template <int MT, int G>
@@ -653,7 +653,7 @@ static void launch_tile(const LinearW4Args& a, hipStream_t s) {
 }
 
 // Two tiles of x rows past 16 rows, two of weight rows where a block would have
-// more than one anyway (6144 x 2048, 16 rows of bf16: 6.4 -> 5.1 us), as far as
+// more than one anyway (6144 x 2048, 16 rows of bf16: 7.1 -> 5.8 us), as far as
 // 128 registers hold them: groups of 32 take one by one, e4m3 in groups of 64
 // one tile of x.
 template <bool E8, int G>
@@ -688,12 +688,17 @@ static void launch_wide(const LinearW4Args& a, hipStream_t s) {
   linear_w4_wide_kernel<MT, G><<<grid, 64 * WN * nwk, nwk * row, s>>>(a);
 }
 
-// (the kernel follows N alone, so that a row's bits do not depend on M)
+// The kernel follows N alone, so that a row's bits do not depend on M: a
+// compromise between few rows and many.  From 16384 outputs on the wide one is
+// ahead at 64 rows, about level or ahead at 32 and for one row of a short K, and
+// behind for one row of a long K (us, this one against the one above it, at
+// 1 / 32 / 64 rows: 20160 x 1280 10 / 16 / 30 against 12 / 22 / 42, 16384 x 4000
+// 29 / 42 / 45 against 17 / 39 / 75; at 12288 x 4096 28 / 42 / 43 against 17 / 31 / 58).
 template <int G>
 static void launch_f32(const LinearW4Args& a, hipStream_t s) {
   if (a.N < 16384) {
     // two tiles of weight rows share a pass of x, where a block would have more
-    // than one anyway (6144 x 2048, 1 row: 7.9 -> 6.0 us); smaller groups spill
+    // than one anyway (6144 x 2048, 1 row: 8.2 -> 6.4 us); smaller groups spill
     if (G == 128 && a.N > 4096)
       launch_f32_tile<G == 128 ? 2 : 1, G>(a, s);
     else

@@ -314,8 +314,7 @@ sd_status synerdiff_op_rmsnorm(int32_t dtype, const void* x, int64_t x_ld, const
   a.x = x; a.x_ld = x_ld; a.resid = resid; a.resid_ld = resid_ld; a.sum = sum; a.sum_ld = sum_ld;
   a.gamma = gamma; a.eps = eps; a.tokens = tokens; a.C = C;
   a.y8 = y_type == SD_E4M3; a.y = y; a.y_ld = y_ld; a.scale = scale;
-  a.group = scale_group ? scale_group : C;
-  a.blocks = (C + a.group - 1) / a.group;
+  a.blocks = scale_group ? (C + 127) / 128 : 1;
   return op_hip(launch_rmsnorm((DType)dtype, a, (hipStream_t)stream), "rmsnorm");
 }
 
