@@ -259,3 +259,27 @@ def test_cross_attention_queries_past_2_31_elements(ops, nq, most, dt):  # noqa:
     ops.cross_attention(qs, pad(k), pad(v), most, out=os, **kw)
     assert torch.equal(os.contiguous(), ops.cross_attention(q, pad(k), pad(v), most, **kw))
     _check_attn(os, q, k, v, [range(60), range(60, 101)], dt, f"{(nq, most, dt)}")
+
+
+# ------------------------------------------------------------------ together
+def test_states_to_8_bits_to_4_bit_layer_to_attention(ops):  # noqa: F811
+    """Encoder states -> norm to 8 bits -> 4-bit layer to K and V -> queries and
+    pooled tokens over the ragged texts, every step against its own inputs."""
+    g = _gen(21)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    lens = torch.tensor([77, 5, 300], dtype=torch.int32)
+    start, tokens, b = (lens.cumsum(0).to(torch.int32) - lens), int(lens.sum()), torch.bfloat16
+    states, resid, gamma = r(tokens, 384).to(b), r(tokens, 384).to(b), 1 + 0.1 * r(384)
+    y8, sc, h = ops.rmsnorm(states, gamma, 1e-6, resid=resid, fp8=True, scale_group=128)
+    _check_norm((y8, sc, h), states, gamma, 1e-6, resid, True, 128, "bf16", "states")
+    w, ws, z, _ = _w4(g, 1, 384, 2 * 2 * 40, 64, True)
+    kv = ops.linear_rows_w4(y8, w, ws, 64, zero=z, x_scale=sc, out_dtype=b)
+    ref, size = _w4_bound(y8, sc, w, ws, z, 64)
+    _w4_close(kv, ref, size, 384, "K and V", 8 * U32 * size + U16 * np.abs(ref) * (1 + 1e-3))
+    k, v = kv.view(tokens, 2, 2, 40).unbind(1)
+    k = k * 0.05  # (scores of order 1)
+    texts = [range(int(s), int(s + n)) for s, n in zip(start, lens)]
+    for nq in (1, 200):
+        q = r(3, nq, 6, 40).to(b)
+        got = ops.cross_attention(q, k, v, 300, kv_start=start.cuda(), kv_len=lens.cuda())
+        _check_attn(got, q, k, v, texts, "bf16", f"attention {nq}")

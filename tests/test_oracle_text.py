@@ -62,3 +62,22 @@ def test_cross_attention_matches_the_library_on_each_text(rep):
     assert not o[2].any()
     assert np.allclose(o[1], np.repeat(v[7], rep, 0)[None])  # one key: its value
     assert math.isfinite(w.sum())
+
+
+def test_rmsnorm_unit_mean_square_and_scale():
+    x = rng.standard_normal((4, 33))
+    y, _ = O.rmsnorm(x, eps=0.0)
+    assert np.allclose((y * y).mean(1), 1, rtol=1e-14)
+    assert np.allclose(O.rmsnorm(x * np.array([[3.0], [1e-8], [1e12], [-2.0]]), eps=0.0)[0], y * np.array([[1], [1], [1], [-1]]), rtol=1e-13)
+
+
+def test_w4_product_brute_force():
+    codes, x = rng.integers(0, 256, (5, 36)).astype(np.uint8), rng.standard_normal((2, 72))
+    scale, zero = rng.standard_normal((5, 2)), rng.integers(0, 16, (5, 2))
+    y = x @ O.w4_weights(codes, scale, zero, 64).T
+    for m in range(2):
+        for n in range(5):
+            s = 0.0
+            for k in range(72):
+                s += x[m, k] * scale[n, k // 64] * ((int(codes[n, k // 2]) >> (4 * (k % 2))) % 16 - int(zero[n, k // 64]))
+            assert math.isclose(y[m, n], s, rel_tol=1e-12, abs_tol=1e-12)
