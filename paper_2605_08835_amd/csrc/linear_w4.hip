@@ -80,7 +80,8 @@ __device__ __forceinline__ u32x4 codes_bf16(uint32_t w, float z) {
 }
 
 // SiLU where asked: one branch around all 8 (value by value the compiler
-// computes it always and picks: fp32, 16 rows of 4096 x 4096 12.3 us against 9.5).
+// computes it always and picks: fp32, 16 rows of 4096 x 4096 12.0 us, as under
+// SiLU, against 9.0).
 __device__ __forceinline__ void silu_if(int on, float (&v)[8]) {
   if (__builtin_amdgcn_readfirstlane(on)) {
 #pragma unroll
@@ -635,8 +636,8 @@ __global__ __launch_bounds__(1024) void linear_w4_wide_kernel(LinearW4Args a) {
 }
 
 // Blocks: as many as run at once (16 waves a CU at up to 128 registers), each
-// over several tiles where there are more (bf16, 16 rows, 20160 x 1280: 12.2 ->
-// 10.5 us; 64 rows 34.6 -> 27).  A wave's sums take the place of its operands in LDS.
+// over several tiles where there are more (bf16, 16 rows, 20160 x 1280: 12.9 ->
+// 11.6 us; 64 rows 33.5 -> 27.3).  A wave's sums take the place of its operands in LDS.
 static dim3 w4_grid(int tiles, int rows, int nw) {
   const int once = 256 * (16 / nw);
   return dim3((unsigned)(tiles < once ? tiles : once), (unsigned)rows);

@@ -136,6 +136,7 @@ def groupnorm_stats_noalloc(x0, groups, eps, gamma, beta, x1=None, scale=None, s
 # tensors may live on any one device: the call runs there, on that device's
 # current stream.  (A call takes about 8 us on the host, 4 of them the launch;
 # the checks are written for that: no message is built unless it is raised.)
+# Forward only: nothing here records a gradient.
 _TYPE = {torch.float32: SD_F32, torch.bfloat16: SD_BF16, torch.float8_e4m3fn: SD_E4M3}
 
 
