@@ -275,6 +275,47 @@ sd_status synerdiff_op_cross_attention(int32_t dtype, const void* d_q, int64_t q
                                        int32_t d, int32_t n_q, float scale, float* d_scratch, int64_t scratch_floats,
                                        void* hip_stream);
 
+/* Attention inside texts of their own lengths (a text encoder's layers):
+ *   o[i, h] = sum_j p_j v[j, g] / sum_j p_j,   g = h / (heads / kv_heads)
+ *   p_j = exp(f(scale * q[i, h] . k[j, g]) + bias[h, clip(j - i, -reach, reach) + reach] - slope[h] |j - i|)
+ * i and j count from the text's first token; f(s) = cap * tanh(s / cap), or s
+ * with cap = 0; bias fp32 [heads, 2 reach + 1] and slope fp32 [heads] may be
+ * NULL (bias NULL: reach 0).  Key j takes part if it lies in the query's own
+ * text, its mask byte is not 0 (mask NULL: all) and, with causal = 1, j <= i or
+ * j < prefix[c] (int32 [n], NULL: 0; counts past the text's end end there,
+ * negative ones are 0).  Queries of masked tokens are computed like others.
+ * Keys that take no part for any query of their text are not read, and what k
+ * and v hold behind a query's causal border does not reach it, infinities and
+ * NaN included.  Keys that score -inf take no weight; a query without a key of
+ * any weight gives zeros.  A finite bias, lowest value of fp32 included, stays
+ * finite: a query whose keys all have it weighs them alike.  Scores, sums and
+ * results are fp32 until the result is rounded to dtype; bf16 probabilities
+ * are rounded to bf16 (by up to 2^-8 of each) and summed as rounded.
+ * Layouts (strides in elements, 0 or more; that of an axis of one element is
+ * not looked at).  Packed texts (d_start not NULL, int32 [n + 1], not
+ * decreasing): text c is rows start[c] .. start[c + 1] - 1 of [tokens], cut at
+ * both ends of it; element (row, h, e) of q at q + row * q_ld + h * q_head +
+ * e, k, v, o likewise, mask [tokens].  Padded texts (d_start NULL): text c is the first
+ * length[c] (int32 [n], NULL: max_len) of max_len rows at c * q_text and so on,
+ * mask [n, max_len]; tokens is not looked at.  No text is longer than max_len (what lies past
+ * it is left out).  Rows of o in no text keep what they hold; with zero_rest =
+ * 1 they become 0 (padded: all rows past the lengths; packed: those before
+ * start[0], from start[n] on, and past a text's first max_len).
+ * Constraints: d a multiple of 8, <= 256; heads a multiple of kv_heads, <=
+ * 2^16; max_len <= 2^30; q_ld, k_ld, v_ld, o_ld <= 2^23; scale 0 or 2^-60 to
+ * 2^60 in size, cap 0 or 2^-20 to 2^60; reach <= 2^24; a grid of less than 2^32 threads (a block of
+ * 256 per 128 queries of a head); q, k, v, o and their strides at multiples
+ * of 16 bytes.  o overlaps nothing.  No workspace.  n = 0 does nothing.  The
+ * bits of a query depend on its own text alone. */
+sd_status synerdiff_op_text_attention(int32_t dtype, const void* d_q, int64_t q_ld, int64_t q_head, int64_t q_text,
+                                      const void* d_k, int64_t k_ld, int64_t k_head, int64_t k_text, const void* d_v,
+                                      int64_t v_ld, int64_t v_head, int64_t v_text, void* d_o, int64_t o_ld,
+                                      int64_t o_head, int64_t o_text, int64_t tokens, int32_t n, int32_t max_len,
+                                      const int32_t* d_start, const int32_t* d_length, const uint8_t* d_mask,
+                                      int32_t causal, const int32_t* d_prefix, float cap, const float* d_bias,
+                                      int32_t reach, const float* d_slope, int32_t heads, int32_t kv_heads, int32_t d,
+                                      float scale, int32_t zero_rest, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

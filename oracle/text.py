@@ -58,3 +58,38 @@ def cross_attention(q, k, v, texts, scale):
             o[i, :, h] = p @ v[rows, h // rep]
             w[i, :, h] = p @ np.abs(v[rows, h // rep])
     return o, w
+
+
+def text_attention(q, k, v, texts, scale, mask=None, causal=False, prefix=None, cap=None, bias=None, slope=None):
+    """Attention inside texts: q [tokens, heads, d], k, v [tokens, kv_heads,
+    d], texts[c] = (first row, length), one query at a time.  Rows in no text
+    give 0, as do queries without a key that scores above -inf.  Returns (o,
+    w), w the same sum over |v|."""
+    q, k, v = (np.asarray(t, F) for t in (q, k, v))
+    heads, rep = q.shape[1], q.shape[1] // k.shape[1]
+    o, w = np.zeros(q.shape, F), np.zeros(q.shape, F)
+    for c, (first, size) in enumerate(texts):
+        for i in range(size):
+            js = [j for j in range(size) if (mask is None or mask[first + j])
+                  and (not causal or j <= i or (prefix is not None and j < prefix[c]))]
+            if not js:
+                continue
+            js = np.asarray(js)
+            far = js - i
+            for h in range(heads):
+                s = k[first + js, h // rep] @ q[first + i, h] * scale
+                if cap:
+                    s = cap * np.tanh(s / cap)
+                if bias is not None:
+                    reach = bias.shape[1] // 2
+                    s = s + np.asarray(bias, F)[h, np.clip(far, -reach, reach) + reach]
+                if slope is not None:
+                    s = s - float(slope[h]) * np.abs(far)
+                on = s > -np.inf
+                if not on.any():
+                    continue
+                p = np.exp(s[on] - s[on].max())
+                p /= p.sum()
+                o[first + i, h] = p @ v[first + js[on], h // rep]
+                w[first + i, h] = p @ np.abs(v[first + js[on], h // rep])
+    return o, w

@@ -141,6 +141,11 @@ _SIG = {
                                      [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P, _P] +
                                      [ctypes.c_int64] * 3 + [ctypes.c_int32] * 5 + [ctypes.c_float, _P,
                                                                                    ctypes.c_int64, _P]),
+    "synerdiff_op_text_attention": (ctypes.c_int, [ctypes.c_int32] + [_P, ctypes.c_int64, ctypes.c_int64,
+                                                                      ctypes.c_int64] * 4 +
+                                    [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, _P,
+                                     ctypes.c_float, _P, ctypes.c_int32, _P] + [ctypes.c_int32] * 3 +
+                                    [ctypes.c_float, ctypes.c_int32, _P]),
 }
 
 

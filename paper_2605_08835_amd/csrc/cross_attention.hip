@@ -25,15 +25,13 @@
 // become a bit per key of a tile before its loads are issued.
 #include <type_traits>
 
+#include "attention_tile.h"
 #include "device_common.h"
 #include "kernels.h"
 
 namespace sd {
 
 namespace {
-
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float TAU = 8.0f;  // the running maximum moves when a tile's passes it by this much (log2 units)
 
 // What image `img` reads: its context's first key (elements of K and V, mask byte) and the count.
 struct Text {
@@ -153,19 +151,6 @@ __device__ __forceinline__ RowAt row_at(const CrossArgs& a, int r) {
   if (a.rep == 1) return {r, 0};
   const int t = (int)(__umulhi((unsigned)r, a.rep_mul) >> a.rep_shift);
   return {t, r - t * a.rep};
-}
-
-// What a row's exponents are taken against: its running maximum, or 0 as long as
-// every key so far scored -inf (then every p is 0; -inf minus -inf is NaN).
-__device__ __forceinline__ float exp_ref(float m) { return m == -INFINITY ? 0.f : m; }
-
-__device__ __forceinline__ float2 half_swap(float v) {  // (v of lanes l and l ^ 32)
-#if defined(__HIP_DEVICE_COMPILE__)
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
-#else
-  return make_float2(v, v);
-#endif
 }
 
 }  // namespace
@@ -371,44 +356,6 @@ static void launch_join(const CrossArgs& a, const Plan& p, hipStream_t s) {
 namespace {
 
 constexpr int KT = 64;  // keys per tile
-
-// LDS row of V: a multiple of 16 channels whose four rows a transposing read
-// takes lie in different banks (an odd number of 32-byte units, or a row that
-// fills a multiple of 64 but not of 128 or 256 bytes).
-__host__ __device__ constexpr int v_row(int d16) { return d16 * 2 % 128 == 0 ? d16 + 16 : d16; }
-
-// Four keys (LDS rows) of one channel for each lane of a group of 16: lane i
-// names the 8 bytes of row i / 4, channels 4 (i % 4) on, and gets channel i of rows 0 to 3.
-__device__ __forceinline__ bf16x4 read_transposed(const bf16* p) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  typedef short s16x4 __attribute__((ext_vector_type(4)));
-  return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
-#else
-  return *(const bf16x4*)p;
-#endif
-}
-
-// l + the eight rounded probabilities, two to an instruction (taking them apart
-// again cost three each, a third of a 64-key tile's vector instructions).
-__device__ __forceinline__ float sum_probs(bf16x8 p, float l) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  const bf16x2 one = {(bf16)1.0f, (bf16)1.0f};
-  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 0, 1), one, l, false);
-  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 2, 3), one, l, false);
-  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 4, 5), one, l, false);
-  l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p, p, 6, 7), one, l, false);
-#endif
-  return l;
-}
-
-__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-#else
-  return c;
-#endif
-}
 
 }  // namespace
 
@@ -962,13 +909,6 @@ __global__ __launch_bounds__(64 * NW, D16 <= 64 ? 3 : 1) void cross_keys_kernel(
 // 37 TFLOP/s) wait for the blocks of the longest text.
 namespace {
 constexpr int FT = 32;
-__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
-#else
-  return c;
-#endif
-}
 }  // namespace
 
 template <int D32>

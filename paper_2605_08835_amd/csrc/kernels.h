@@ -229,4 +229,27 @@ struct CrossArgs {
 hipError_t launch_cross_attention(DType dt, CrossArgs a, hipStream_t s);
 long cross_attention_scratch_floats(DType dt, int n, int heads, int kv_heads, int d, int n_q, int max_len);
 
+// Attention inside texts of their own lengths, see synerdiff_op_text_attention.
+struct TextArgs {
+  const void* q; long q_ld, q_head, q_img;
+  const void* k; long k_ld, k_head, k_img;
+  const void* v; long v_ld, v_head, v_img;
+  void* o; long o_ld, o_head, o_img;
+  long tokens;          // packed rows
+  int n, max_len;
+  const int* start;     // [n + 1]; null: padded texts
+  const int* length;    // padded: [n] or null
+  const int* prefix;    // or null
+  const uint8_t* mask;  // or null
+  const float* bias;    // [heads, 2 reach + 1] or null
+  int reach;
+  const float* slope;   // [heads] or null
+  float cap, scale;     // cap 0: none
+  int causal, zero;     // zero: rows of o in no text become 0
+  int heads, kv_heads, rep, d;
+  int chunk, chunks;    // set by the launcher
+};
+hipError_t launch_text_attention(DType dt, TextArgs a, hipStream_t s);
+bool text_attention_fits(int n, int heads, int kv_heads, int max_len);
+
 }  // namespace sd

@@ -421,4 +421,62 @@ sd_status synerdiff_op_cross_attention(int32_t dtype, const void* q, int64_t q_l
   return op_hip(launch_cross_attention((DType)dtype, a, (hipStream_t)stream), "cross_attention");
 }
 
+sd_status synerdiff_op_text_attention(int32_t dtype, const void* q, int64_t q_ld, int64_t q_head, int64_t q_text,
+                                      const void* k, int64_t k_ld, int64_t k_head, int64_t k_text, const void* v,
+                                      int64_t v_ld, int64_t v_head, int64_t v_text, void* o, int64_t o_ld,
+                                      int64_t o_head, int64_t o_text, int64_t tokens, int32_t n, int32_t max_len,
+                                      const int32_t* start, const int32_t* length, const uint8_t* mask, int32_t causal,
+                                      const int32_t* prefix, float cap, const float* bias, int32_t reach,
+                                      const float* slope, int32_t heads, int32_t kv_heads, int32_t d, float scale,
+                                      int32_t zero_rest, void* stream) {
+  if (bad_dtype(dtype)) return op_fail(SD_ERR_INVALID_ARG, "bad dtype");
+  if (n < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || d < 8 || d % 8 || max_len < 0)
+    return op_fail(SD_ERR_INVALID_ARG, "bad shape (d a multiple of 8, heads of kv_heads)");
+  if (d > 256 || heads > 1 << 16 || max_len > 1 << 30)
+    return op_fail(SD_ERR_UNSUPPORTED, "heads past 256 channels, more than 2^16 of them, or texts past 2^30 tokens");
+  if (tokens < 0 || tokens > 0x7FFFFFFF) return op_fail(SD_ERR_INVALID_ARG, "bad token count");
+  if (start && length) return op_fail(SD_ERR_INVALID_ARG, "packed texts end where the next one starts: no lengths");
+  if (prefix && !causal) return op_fail(SD_ERR_INVALID_ARG, "a prefix needs causal texts");
+  if (scale - scale != 0.f) return op_fail(SD_ERR_INVALID_ARG, "scale must be finite");
+  if (!(cap >= 0.f) || cap - cap != 0.f) return op_fail(SD_ERR_INVALID_ARG, "cap must be finite and not negative");
+  const float mag = scale < 0.f ? -scale : scale;
+  if (scale != 0.f && (mag < 0x1p-60f || mag > 0x1p60f)) return op_fail(SD_ERR_UNSUPPORTED, "scale outside 2^-60 .. 2^60");
+  if (cap != 0.f && (cap < 0x1p-20f || cap > 0x1p60f)) return op_fail(SD_ERR_UNSUPPORTED, "cap outside 2^-20 .. 2^60");
+  if (bias ? reach < 0 || reach > 1 << 24 : reach != 0)
+    return op_fail(SD_ERR_INVALID_ARG, "reach is that of a bias, 0 to 2^24");
+  if (n == 0 || (start ? tokens : (int64_t)max_len) == 0) return SD_OK;
+  // (the stride of an axis of one element may hold anything)
+  if ((start ? tokens : (int64_t)max_len) == 1) q_ld = k_ld = v_ld = o_ld = 0;
+  if (heads == 1) q_head = o_head = 0;
+  if (kv_heads == 1) k_head = v_head = 0;
+  if (start || n == 1) q_text = k_text = v_text = o_text = 0;
+  if (q_ld > 1 << 23 || k_ld > 1 << 23 || v_ld > 1 << 23 || o_ld > 1 << 23)
+    return op_fail(SD_ERR_UNSUPPORTED, "more than 2^23 elements from token to token");
+  if (!q || !k || !v || !o) return op_fail(SD_ERR_INVALID_ARG, "NULL argument");
+  const int64_t strides[] = {q_ld, q_head, q_text, k_ld, k_head, k_text, v_ld, v_head, v_text, o_ld, o_head, o_text};
+  const int64_t piece = dtype == SD_BF16 ? 8 : 4;
+  for (int64_t s : strides)
+    if (s < 0 || s % piece) return op_fail(SD_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15)
+    return op_fail(SD_ERR_INVALID_ARG, "q, k, v, o must be 16-byte aligned");
+  if (((start ? tokens : (int64_t)max_len) > 1 && o_ld == 0) || (heads > 1 && o_head == 0) || (!start && n > 1 && o_text == 0))
+    return op_fail(SD_ERR_INVALID_ARG, "o overlaps itself");
+  if (((uintptr_t)start | (uintptr_t)length | (uintptr_t)prefix | (uintptr_t)bias | (uintptr_t)slope) & 3)
+    return op_fail(SD_ERR_INVALID_ARG, "an array is not aligned to its element");
+  if (o == q || o == k || o == v) return op_fail(SD_ERR_INVALID_ARG, "o overlaps an input");
+  if (!text_attention_fits(n, heads, kv_heads, max_len)) return op_fail(SD_ERR_UNSUPPORTED, "too many texts, heads and queries");
+  TextArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = q; a.q_ld = q_ld; a.q_head = q_head; a.q_img = q_text;
+  a.k = k; a.k_ld = k_ld; a.k_head = k_head; a.k_img = k_text;
+  a.v = v; a.v_ld = v_ld; a.v_head = v_head; a.v_img = v_text;
+  a.o = o; a.o_ld = o_ld; a.o_head = o_head; a.o_img = o_text;
+  a.tokens = tokens; a.n = n; a.max_len = max_len;
+  a.start = start; a.length = length; a.prefix = prefix; a.mask = mask;
+  a.bias = bias; a.reach = reach; a.slope = slope; a.cap = cap; a.scale = scale;
+  a.causal = causal ? 1 : 0; a.zero = zero_rest ? 1 : 0;
+  a.heads = heads; a.kv_heads = kv_heads; a.rep = heads / kv_heads; a.d = d;
+  return op_hip(launch_text_attention((DType)dtype, a, (hipStream_t)stream), "text_attention");
+}
+
 }  // extern "C"

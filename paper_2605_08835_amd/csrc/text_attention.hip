@@ -1,0 +1,660 @@
+// Attention inside texts of their own lengths:
+//   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(f(scale q_i . k_j) + bias(j - i))
+// over the keys j of query i's own text that take part: f is the identity or
+// cap tanh(. / cap), bias a table per head by distance, constant past its ends,
+// less a slope times the distance; a causal text shows query i the keys up to i,
+// and those of its prefix.
+//
+// A block takes 128 queries of one head and passes over their text's keys once,
+// a wave per 32 queries.  Scores are held transposed, S^T = K Q^T, so that a
+// lane has one query: its order, maximum and rescale are per lane, and P^T feeds
+// O^T = V^T P^T from the registers.  What depends on the distance alone is the
+// same along a diagonal: a tile's 64 x 128 values are 191, kept in LDS.
+// Tiles wholly behind the causal border are passed over, and keys that a mask or
+// the text's end leaves out are never read.
+#include <type_traits>
+
+#include "attention_tile.h"
+#include "device_common.h"
+#include "kernels.h"
+
+namespace sd {
+
+namespace {
+
+constexpr int TQ = 128;  // queries per block, 32 a wave
+
+// Text c: its first row (elements of q, k, v, o; mask byte), its length, and the
+// keys that all its queries see.
+struct Span {
+  long q0, k0, v0, o0, m0;
+  int len, prefix;
+};
+__device__ __forceinline__ Span span_of(const TextArgs& a, int c) {
+  Span t;
+  if (a.start) {
+    const long lo = min(max((long)a.start[c], 0L), a.tokens), hi = min(max((long)a.start[c + 1], lo), a.tokens);
+    t.q0 = lo * a.q_ld;
+    t.k0 = lo * a.k_ld;
+    t.v0 = lo * a.v_ld;
+    t.o0 = lo * a.o_ld;
+    t.m0 = lo;
+    t.len = (int)min(hi - lo, (long)a.max_len);
+  } else {
+    t.q0 = (long)c * a.q_img;
+    t.k0 = (long)c * a.k_img;
+    t.v0 = (long)c * a.v_img;
+    t.o0 = (long)c * a.o_img;
+    t.m0 = (long)c * a.max_len;
+    t.len = a.length ? min(max(a.length[c], 0), a.max_len) : a.max_len;
+  }
+  t.prefix = a.prefix ? min(max(a.prefix[c], 0), t.len) : 0;
+  return t;
+}
+
+// Block -> (text, head, tile).  Consecutive blocks go to the 8 XCDs in turn, each
+// with an L2 of its own.  `chunk` tiles of all heads that share a K/V head stay
+// on one XCD, next to each other in time, since they read the same keys; the
+// chunks furthest into their texts come first, as a causal one costs as much as
+// the keys before it.
+struct Place {
+  int c, g, h, tile;
+  bool on;
+};
+__device__ __forceinline__ Place place_of(const TextArgs& a) {
+  const unsigned id = blockIdx.x, xcd = id & 7, i = id >> 3, per = (unsigned)a.chunk * a.rep;
+  const unsigned u = i / per * 8 + xcd, in = i % per, pairs = (unsigned)a.n * a.kv_heads;
+  Place p;
+  const int ch = a.chunks - 1 - (int)(u / pairs);
+  const unsigned w = u % pairs;
+  p.on = ch >= 0;
+  p.c = w / a.kv_heads;
+  p.g = w % a.kv_heads;
+  p.h = p.g * a.rep + in % a.rep;
+  p.tile = ch * a.chunk + a.chunk - 1 - (int)(in / a.rep);
+  return p;
+}
+
+// The rows of packed texts' o that lie in no text, zeroed by the blocks of the
+// first and the last one, and those of a text that is longer than max_len says
+// (16 bytes a thread).
+template <typename T>
+__device__ __forceinline__ void zero_rest(const TextArgs& a, const Place& p) {
+  constexpr int E = 16 / sizeof(T);
+  const int per = a.d / E;
+  auto span = [&](long lo, long hi) {
+    T* o = (T*)a.o + p.h * a.o_head;
+    for (long r0 = lo + (long)p.tile * TQ; r0 < hi; r0 += (long)a.chunks * a.chunk * TQ)
+      for (int x = threadIdx.x; x < TQ * per; x += blockDim.x) {
+        const long r = r0 + x / per;
+        if (r < hi) *(uint4*)(o + r * a.o_ld + x % per * E) = make_uint4(0, 0, 0, 0);
+      }
+  };
+  const long lo = min(max((long)a.start[p.c], 0L), a.tokens);
+  span(lo + a.max_len, min((long)a.start[p.c + 1], a.tokens));
+  if (p.c == 0) span(0, min((long)max(a.start[0], 0), a.tokens));
+  if (p.c == a.n - 1) span(max((long)a.start[a.n], 0L), a.tokens);
+}
+
+// bias(j - i) at distance `far` in log2 units, over `unit`.  Finite values stay
+// finite: up to 2^126 of either unit, past any score, and sums of two do not pass fp32.
+__device__ __forceinline__ float bias_at(const TextArgs& a, int h, int far, float unit) {
+  float v = 0.f;
+  if (a.bias) v = a.bias[(long)h * (2 * a.reach + 1) + min(max(far, -a.reach), a.reach) + a.reach];
+  if (a.slope) v = fmaf(-a.slope[h], fabsf((float)far), v);
+  const float lim = 0x1p125f * fminf(unit, 1.f);
+  if (v < -lim && v != -INFINITY) v = -lim;
+  if (v > lim && v != INFINITY) v = lim;
+  return v * LOG2E / unit;
+}
+
+__device__ __forceinline__ bool odd8(uint4 v) {  // an infinity or NaN among eight bf16
+  auto two = [](uint32_t x) { return (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u; };
+  return two(v.x) || two(v.y) || two(v.z) || two(v.w);
+}
+__device__ __forceinline__ bool odd_f(float v) { return !(fabsf(v) < INFINITY); }
+
+}  // namespace
+
+// ------------------------------------------------------------------ bf16
+// D16: head width rounded up to a width the kernel is built for.  BIAS: there is
+// a term by distance.  CAP: scores are capped.
+template <int D16, bool BIAS, bool CAP>
+__global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_bf16_kernel(TextArgs a) {
+  constexpr int NW = 4, KT = 64, NJ = D16 / 16, ND = (D16 + 31) / 32, NT = 64 * NW, LDK = D16 + 8, LDV = v_row(D16);
+  // A tile is moved by passes of NT / LPR keys, LPR lanes (a power of two) a key
+  constexpr int LPR = D16 <= 32 ? 4 : D16 <= 64 ? 8 : D16 <= 128 ? 16 : 32, RPP = NT / LPR < KT ? NT / LPR : KT, CPT = KT / RPP;
+  __shared__ __attribute__((aligned(16))) bf16 Ks[2][KT * LDK];
+  __shared__ __attribute__((aligned(16))) bf16 Vs[2][KT * LDV + 32];  // (the last rows are read past their end where D16 % 32)
+  __shared__ float strip[BIAS ? 2 : 1][BIAS ? KT + TQ : 1];
+  __shared__ int odd[3];  // tile i: an infinity or NaN in V where the border passes (slot i % 3)
+  const Place p = place_of(a);
+  if (!p.on) return;
+  if (a.zero && a.start) zero_rest<bf16>(a, p);
+  const Span tx = span_of(a, p.c);
+  const int b0 = p.tile * TQ, d = a.d;
+  const int rows = a.zero && !a.start ? a.max_len : tx.len;  // (padded rows past the text get zeros)
+  if (b0 >= rows) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, lh = lane >> 5;
+  const int r0 = b0 + wave * 32;
+  int k_end = b0 < tx.len ? tx.len : 0;
+  if (a.causal) k_end = min(k_end, max(b0 + TQ, tx.prefix));
+  const int lim = a.causal ? max(r0 + lq + 1, tx.prefix) : tx.len;               // keys that this lane's query sees
+  const int lim_lo = a.causal ? max(r0 + 1, tx.prefix) : tx.len, lim_hi = a.causal ? max(r0 + 32, tx.prefix) : tx.len;
+  const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
+  // (a scale of 0 or below: uniform scores, or -q, under a positive one)
+  const float mag = a.scale == 0.f ? 1.f : fabsf(a.scale), sl2 = mag * LOG2E;
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+  // cap tanh(x / cap) = cap - 2 cap / (1 + exp(2 x / cap)), in log2 units
+  const float c_in = CAP ? 2.f * sl2 / a.cap : 0.f, c_out = CAP ? a.cap * LOG2E : 0.f;
+
+  // Q^T fragments (B operand): query r0 + lq, channels 16 j + 8 lh + [0, 8)
+  bf16x8 qf[NJ];
+  {
+    const bf16* Q = (const bf16*)a.q + tx.q0 + (long)r0 * a.q_ld + p.h * a.q_head;
+    const int n = a.scale == 0.f ? 0 : min(32, tx.len - r0);
+    const __amdgpu_buffer_rsrc_t qr = make_rsrc(Q, n <= 0 ? 0 : ((n - 1) * (long)a.q_ld + d) * 2);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      uint4 v = __builtin_bit_cast(uint4, buf_load16(qr, 16 * j + 8 * lh < d ? (lq * (int)a.q_ld + 16 * j + 8 * lh) * 2 : OOB));
+      v.x ^= flip;
+      v.y ^= flip;
+      v.z ^= flip;
+      v.w ^= flip;
+      qf[j] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+  f32x16 o[ND];
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  if (tid < 3) odd[tid] = 0;
+  __syncthreads();
+
+  // A thread's pieces of a tile: keys pk + RPP i, channels pc on.  (Offsets past a
+  // resource's end, as those of channels from d on and of keys that take no part, read as zero.)
+  const int pk = tid / LPR, pc = tid % LPR * 8;
+  const bool mine = pk < RPP && pc < D16;  // (fewer than NT threads where LPR is wide or the tile short)
+  const int ko = pc < d ? (pk * (int)a.k_ld + pc) * 2 : OOB, vo = pc < d ? (pk * (int)a.v_ld + pc) * 2 : OOB;
+  const bf16* K = (const bf16*)a.k + tx.k0 + p.g * a.k_head;
+  const bf16* V = (const bf16*)a.v + tx.v0 + p.g * a.v_head;
+  bf16x8 rk[CPT], rv[CPT];
+  float rb = 0.f;
+  auto fetch = [&](int k0, uint64_t bits) __attribute__((always_inline)) {
+    const int n = min(KT, k_end - k0);
+    const __amdgpu_buffer_rsrc_t kr = make_rsrc(K + (long)k0 * a.k_ld, ((n - 1) * (long)a.k_ld + d) * 2);
+    const __amdgpu_buffer_rsrc_t vr = make_rsrc(V + (long)k0 * a.v_ld, ((n - 1) * (long)a.v_ld + d) * 2);
+    const uint64_t b = bits >> (pk & 63);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      const bool on = (b >> (RPP * i & 63)) & 1;
+      rk[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(kr, on ? ko + i * RPP * (int)a.k_ld * 2 : OOB, 0, 0));
+      rv[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(vr, on ? vo + i * RPP * (int)a.v_ld * 2 : OOB, 0, 0));
+    }
+    // strip[e]: distance k0 - b0 + e - (TQ - 1)
+    if constexpr (BIAS)
+      if (tid < KT + TQ - 1) rb = bias_at(a, p.h, k0 - b0 + tid - (TQ - 1), CAP ? 1.f : sl2);
+  };
+  auto stage = [&](int b, int k0, int slot) __attribute__((always_inline)) {
+    // (a key's V reaches every query of the tile, with a weight of 0 behind the
+    // border: 0 times an infinity or NaN is NaN, so those are taken out here and added where they are seen)
+    const bool border = a.causal && k0 + KT > max(b0 + 1, tx.prefix);
+    if (mine)
+#pragma unroll
+      for (int i = 0; i < CPT; ++i) {
+        *(bf16x8*)&Ks[b][(pk + RPP * i) * LDK + pc] = rk[i];
+        bf16x8 v = rv[i];
+        if (border && odd8(__builtin_bit_cast(uint4, v))) {
+          odd[slot] = 1;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (odd_f((float)v[e])) v[e] = (bf16)0.f;
+        }
+        *(bf16x8*)&Vs[b][(pk + RPP * i) * LDV + pc] = v;
+      }
+    if constexpr (BIAS)
+      if (tid < KT + TQ - 1) strip[b][tid] = rb;
+  };
+  // which of the 64 keys from k0 on take part: lane's own, as loaded; then a bit per key
+  auto own_key = [&](int k0) -> bool {
+    const int k = k0 + lane;
+    return k < k_end && (!mask || mask[k]);
+  };
+
+  bf16x8 ones = {};  // B operand of the masks: ones for k = 0
+  if (lh == 0) ones[0] = (bf16)1.0f;
+  const int sb = TQ - 1 - wave * 32 - lq + 4 * lh;  // strip's element at key 4 lh for this lane's query
+
+  // NKT: 32-key halves of the tile that hold keys at all.
+  auto tile = [&](auto nkt, int b, uint64_t bits, int k0) __attribute__((always_inline)) {
+    constexpr int NKT = decltype(nkt)::value;
+    const bf16 *Kb = Ks[b], *Vb = Vs[b];
+    f32x16 s[NKT];
+    // register r of half kt: key 32 kt + 8 (r / 4) + 4 lh + r % 4
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) {
+      f32x16 start = {};
+      if constexpr (BIAS && !CAP)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) start[r] = strip[b][sb + 32 * kt + 8 * (r >> 2) + (r & 3)];
+      if constexpr (!CAP)
+        if ((uint32_t)(bits >> (32 * kt)) != ~0u) {
+          // Keys that take no part start from -inf: one product of a column of 0
+          // or -inf per key with a row of ones.
+          bf16x8 off = {};
+          if (lh == 0) off[0] = __builtin_bit_cast(bf16, (unsigned short)(bits >> (32 * kt + lq) & 1 ? 0 : 0xFF80));
+          start = mfma32(off, ones, start);
+        }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const bf16x8 kf = *(const bf16x8*)&Kb[(kt * 32 + lq) * LDK + 16 * j + 8 * lh];
+        s[kt] = mfma32(kf, qf[j], j ? s[kt] : start);
+      }
+    }
+    if constexpr (CAP) {
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float t = __builtin_amdgcn_exp2f(s[kt][r] * c_in);
+          float z = fmaf(-2.f * c_out, __builtin_amdgcn_rcpf(1.f + t), c_out);
+          if constexpr (BIAS) z += strip[b][sb + 32 * kt + 8 * (r >> 2) + (r & 3)];
+          s[kt][r] = z;
+        }
+    }
+    // the causal border, and for capped scores the keys that take no part
+    if (k0 + KT > lim_lo || (CAP && ~bits)) {
+      const int left = lim - k0 - 4 * lh;
+      const uint64_t w = bits >> (4 * lh);
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int c = 32 * kt + 8 * (r >> 2) + (r & 3);
+          if (c >= left || (CAP && !(w >> c & 1))) s[kt][r] = -INFINITY;
+        }
+    }
+    float v = s[0][0];
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) v = fmaxf(v, s[kt][r]);
+    const float2 h = half_swap(v);
+    const float mt = fmaxf(h.x, h.y) * (CAP ? 1.f : sl2);
+    const bool need = mt > m_run + TAU;
+    if (__any(need)) {  // (where a row's maximum stays, its sums are multiplied by one)
+      const float al = need ? __builtin_amdgcn_exp2f(m_run - mt) : 1.0f;
+      m_run = need ? mt : m_run;
+      l_run *= al;
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] *= al;
+    }
+    const float ref = exp_ref(m_run);
+    // (the exponent is s sl2 - ref in one rounding; past 2^20 the one that ref
+    // holds of its own product would no longer be a small part of a step)
+    float mul = CAP ? 1.f : sl2;
+    if (!CAP && __any(fabsf(ref) > 0x1p20f)) {
+      mul = 1.f;
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kt][r] *= sl2;
+    }
+    // O^T += V^T P^T, 16 keys at a time: slot (lh, i) of slice u is key 16 u +
+    // 8 (i / 4) + 4 lh + i % 4, register 8 (u % 2) + i of half u / 2.  The
+    // probabilities are rounded to bf16 (by up to 2^-8 of each, half a step) and
+    // summed as rounded, so that the rounding cancels where one key prevails.
+#pragma unroll
+    for (int u = 0; u < 2 * NKT; ++u) {
+      bf16x8 vf[ND];
+#pragma unroll
+      for (int t = 0; t < ND; ++t) {
+        const bf16* at = &Vb[(16 * u + 4 * lh + ((lane & 15) >> 2)) * LDV + t * 32 + (lane & 16) + 4 * (lane & 3)];
+        const bf16x4 lo = read_transposed(at), hi = read_transposed(at + 8 * LDV);
+        vf[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+      bf16x8 pf;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = s[u >> 1][8 * (u & 1) + i];
+        pf[i] = (bf16)__builtin_amdgcn_exp2f(CAP ? x - ref : fmaf(x, mul, -ref));
+      }
+      l_run = sum_probs(pf, l_run);
+#pragma unroll
+      for (int t = 0; t < ND; ++t) o[t] = mfma32(vf[t], pf, o[t]);
+    }
+  };
+  // What `stage` took out of V, added for the queries that see it (a weight above 0 times it is itself).
+  auto add_odd = [&](uint64_t bits, int k0) __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int j = 0; j < KT; ++j) {
+      if (!(bits >> j & 1)) continue;
+      const __amdgpu_buffer_rsrc_t vr = make_rsrc(V + (long)(k0 + j) * a.v_ld, d * 2);
+      const bool seen = k0 + j < lim;
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(vr, (32 * t + 8 * i + 4 * lh) * 2, 0, 0));
+          const bf16x4 x = __builtin_bit_cast(bf16x4, w);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[t][4 * i + e] += seen && odd_f((float)x[e]) ? (float)x[e] : 0.f;
+        }
+    }
+  };
+
+  if (k_end > 0) {
+    uint64_t bits = __ballot(own_key(0));
+    fetch(0, bits);
+    bool nk = own_key(KT);
+    stage(0, 0, 0);
+    __syncthreads();
+    for (int k0 = 0, b = 0, slot = 0; k0 < k_end; k0 += KT, b ^= 1) {
+      uint64_t next = 0;
+      const bool more = k0 + KT < k_end;
+      if (more) {
+        next = __ballot(nk);
+        fetch(k0 + KT, next);
+        nk = own_key(k0 + 2 * KT);
+      }
+      const int s1 = slot == 2 ? 0 : slot + 1;
+      if (bits && k0 < lim_hi && r0 < tx.len) {
+        if (bits >> 32 && k0 + 32 < lim_hi)
+          tile(std::integral_constant<int, 2>{}, b, bits, k0);
+        else if ((uint32_t)bits)
+          tile(std::integral_constant<int, 1>{}, b, bits, k0);
+        if (a.causal && odd[slot]) add_odd(bits, k0);
+      }
+      if (more) stage(b ^ 1, k0 + KT, s1);
+      if (tid == 0) odd[s1 == 2 ? 0 : s1 + 1] = 0;  // (read before the last barrier, set after the next)
+      __syncthreads();
+      bits = next;
+      slot = s1;
+    }
+  }
+
+  // O^T: lane holds channels 32 t + 8 (r / 4) + 4 lh + r % 4 of its query.  Rows are
+  // laid out in LDS (K's tiles are done with) and leave 16 bytes a lane.
+  const float2 h = half_swap(l_run);
+  const float l = h.x + h.y, inv = l == 0.f ? 0.f : 1.0f / l;
+  const bool live = r0 + lq < tx.len;
+  bf16* R = &Ks[0][0] + wave * 32 * LDK;
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = 32 * t + 8 * i + 4 * lh;
+      if (c < d) {
+        bf16x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (bf16)(live ? o[t][4 * i + e] * inv : 0.f);
+        *(bf16x4*)(R + lq * LDK + c) = w;
+      }
+    }
+  asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
+  const int c = lane % LPR * 8, row0 = lane / LPR;
+  if (c < d) {
+    bf16* O = (bf16*)a.o + tx.o0 + (long)r0 * a.o_ld + p.h * a.o_head + c;
+#pragma unroll
+    for (int i = 0; i < 32; i += 64 / LPR)
+      if (r0 + row0 + i < rows) *(bf16x8*)(O + (row0 + i) * (int)a.o_ld) = *(const bf16x8*)(R + (row0 + i) * LDK + c);
+  }
+}
+
+// ------------------------------------------------------------------ fp32
+// The same on fp32 MFMAs (32 x 32 x 2), tiles of 32 keys.  Channels are summed in
+// the order that makes a lane's share of them four consecutive ones (half lh
+// takes 8 i + 4 lh + [0, 4)); a key's probability meets its V row straight from the
+// register it was computed in, since the two k of an MFMA are the two lane halves' keys.
+template <int D32>
+__global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextArgs a) {
+  constexpr int NW = 4, KT = 32, NI = D32 / 8, ND = D32 / 32, NT = 64 * NW, LDK = D32 + 4, LDV = D32 + 8;  // (rows apart by banks)
+  constexpr int CPT = KT * (D32 / 4) / NT;
+  __shared__ __attribute__((aligned(16))) float Ks[2][KT * LDK];
+  __shared__ __attribute__((aligned(16))) float Vs[2][KT * LDV];
+  __shared__ float strip[2][KT + TQ];
+  __shared__ int odd[3];
+  const Place p = place_of(a);
+  if (!p.on) return;
+  if (a.zero && a.start) zero_rest<float>(a, p);
+  const Span tx = span_of(a, p.c);
+  const int b0 = p.tile * TQ, d = a.d;
+  const int rows = a.zero && !a.start ? a.max_len : tx.len;
+  if (b0 >= rows) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 31, lh = lane >> 5;
+  const int r0 = b0 + wave * 32, r = r0 + lq;
+  int k_end = b0 < tx.len ? tx.len : 0;
+  if (a.causal) k_end = min(k_end, max(b0 + TQ, tx.prefix));
+  const int lim = a.causal ? max(r + 1, tx.prefix) : tx.len;
+  const int lim_lo = a.causal ? max(r0 + 1, tx.prefix) : tx.len, lim_hi = a.causal ? max(r0 + 32, tx.prefix) : tx.len;
+  const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
+  const bool terms = a.bias || a.slope;
+  const float qs = a.scale * (a.cap > 0.f ? 1.f / a.cap : LOG2E), c_out = a.cap * LOG2E;
+
+  f32x4 qf[NI];
+  {
+    const float* Q = (const float*)a.q + tx.q0 + (long)r * a.q_ld + p.h * a.q_head;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int c = 8 * i + 4 * lh;
+      qf[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (r < tx.len && c < d) qf[i] = *(const f32x4*)(Q + c) * qs;
+    }
+  }
+  f32x16 o[ND];
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+  float m_run = -INFINITY, l = 0.f;
+  if (tid < 3) odd[tid] = 0;
+  __syncthreads();
+
+  const float* K = (const float*)a.k + tx.k0 + p.g * a.k_head;
+  const float* V = (const float*)a.v + tx.v0 + p.g * a.v_head;
+  f32x4 rk[CPT], rv[CPT];
+  float rb = 0.f;
+  auto fetch = [&](int k0, uint32_t bits) __attribute__((always_inline)) {
+    const int n = min(KT, k_end - k0);
+    const __amdgpu_buffer_rsrc_t kr = make_rsrc(K + (long)k0 * a.k_ld, ((n - 1) * (long)a.k_ld + d) * 4);
+    const __amdgpu_buffer_rsrc_t vr = make_rsrc(V + (long)k0 * a.v_ld, ((n - 1) * (long)a.v_ld + d) * 4);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      const int idx = tid + NT * i, key = idx / (D32 / 4), c = idx % (D32 / 4) * 4;
+      const bool on = (bits >> key & 1) && c < d;
+      rk[i] = __builtin_bit_cast(f32x4, buf_load16(kr, on ? (key * (int)a.k_ld + c) * 4 : OOB));
+      rv[i] = __builtin_bit_cast(f32x4, buf_load16(vr, on ? (key * (int)a.v_ld + c) * 4 : OOB));
+    }
+    if (terms && tid < KT + TQ - 1) rb = bias_at(a, p.h, k0 - b0 + tid - (TQ - 1), 1.f);
+  };
+  auto stage = [&](int b, int k0, int slot) __attribute__((always_inline)) {
+    const bool border = a.causal && k0 + KT > max(b0 + 1, tx.prefix);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      const int idx = tid + NT * i, key = idx / (D32 / 4), c = idx % (D32 / 4) * 4;
+      *(f32x4*)&Ks[b][key * LDK + c] = rk[i];
+      f32x4 v = rv[i];
+      if (border)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (odd_f(v[e])) {
+            odd[slot] = 1;
+            v[e] = 0.f;
+          }
+      *(f32x4*)&Vs[b][key * LDV + c] = v;
+    }
+    if (terms && tid < KT + TQ - 1) strip[b][tid] = rb;
+  };
+  auto own_key = [&](int k0) -> bool {
+    const int k = k0 + lq;
+    return k < k_end && (!mask || mask[k]);
+  };
+  const int sb = TQ - 1 - wave * 32 - lq + 4 * lh;
+  if (k_end > 0) {
+    uint32_t bits = (uint32_t)__ballot(own_key(0));
+    fetch(0, bits);
+    bool nk = own_key(KT);
+    stage(0, 0, 0);
+    __syncthreads();
+    for (int k0 = 0, b = 0, slot = 0; k0 < k_end; k0 += KT, b ^= 1) {
+      uint32_t next = 0;
+      const bool more = k0 + KT < k_end;
+      if (more) {
+        next = (uint32_t)__ballot(nk);
+        fetch(k0 + KT, next);
+        nk = own_key(k0 + 2 * KT);
+      }
+      const int s1 = slot == 2 ? 0 : slot + 1;
+      if (bits && k0 < lim_hi && r0 < tx.len) {
+        f32x16 s = {};
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          if (8 * i >= d) break;
+          const f32x4 kf = *(const f32x4*)&Ks[b][lq * LDK + 8 * i + 4 * lh];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s = mfma_f32(kf[e], qf[i][e], s);
+        }
+        // register i: key 8 (i / 4) + 4 lh + i % 4
+        if (a.cap > 0.f)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = c_out * tanhf(s[i]);
+        if (terms)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] += strip[b][sb + 8 * (i >> 2) + (i & 3)];
+        if (bits != ~0u || k0 + KT > lim_lo) {
+          const uint32_t bm = bits >> (4 * lh);
+          const int left = lim - k0 - 4 * lh;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int c = 8 * (i >> 2) + (i & 3);
+            if (c >= left || !(bm >> c & 1)) s[i] = -INFINITY;
+          }
+        }
+        float v = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) v = fmaxf(v, s[i]);
+        const float2 hv = half_swap(v);
+        const float mt = fmaxf(hv.x, hv.y);
+        const bool need = mt > m_run + TAU;
+        if (__any(need)) {
+          const float al = need ? __builtin_amdgcn_exp2f(m_run - mt) : 1.0f;
+          m_run = need ? mt : m_run;
+          l *= al;
+#pragma unroll
+          for (int t = 0; t < ND; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] *= al;
+        }
+        const float ref = exp_ref(m_run);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float pr = __builtin_amdgcn_exp2f(s[i] - ref);
+          l += pr;
+          const float* vr = &Vs[b][(8 * (i >> 2) + 4 * lh + (i & 3)) * LDV + lq];
+#pragma unroll
+          for (int t = 0; t < ND; ++t) o[t] = mfma_f32(vr[32 * t], pr, o[t]);
+        }
+        if (a.causal && odd[slot]) {
+#pragma unroll 1
+          for (int j = 0; j < KT; ++j) {
+            if (!(bits >> j & 1)) continue;
+            const __amdgpu_buffer_rsrc_t vr = make_rsrc(V + (long)(k0 + j) * a.v_ld, d * 4);
+            const bool seen = k0 + j < lim;
+#pragma unroll
+            for (int t = 0; t < ND; ++t)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const f32x4 x = __builtin_bit_cast(f32x4, buf_load16(vr, (32 * t + 8 * i + 4 * lh) * 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[t][4 * i + e] += seen && odd_f(x[e]) ? x[e] : 0.f;
+              }
+          }
+        }
+      }
+      if (more) stage(b ^ 1, k0 + KT, s1);
+      if (tid == 0) odd[s1 == 2 ? 0 : s1 + 1] = 0;
+      __syncthreads();
+      bits = next;
+      slot = s1;
+    }
+  }
+  const float2 hl = half_swap(l);
+  l = hl.x + hl.y;
+  if (r >= rows) return;
+  float* out = (float*)a.o + tx.o0 + (long)r * a.o_ld + p.h * a.o_head;
+  const float f = l == 0.f ? 0.f : 1.0f / l;
+  const bool live = r < tx.len;
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = 32 * t + 8 * i + 4 * lh;
+      if (c < d) {
+        f32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = live ? o[t][4 * i + e] * f : 0.f;
+        *(f32x4*)(out + c) = w;
+      }
+    }
+}
+
+// ------------------------------------------------------------------ launch
+template <int D16>
+static void launch_width(const TextArgs& a, unsigned grid, hipStream_t s) {
+  const bool terms = a.bias || a.slope;
+  if (a.cap > 0.f) {
+    if (terms) text_bf16_kernel<D16, true, true><<<grid, 256, 0, s>>>(a);
+    else text_bf16_kernel<D16, false, true><<<grid, 256, 0, s>>>(a);
+  } else {
+    if (terms) text_bf16_kernel<D16, true, false><<<grid, 256, 0, s>>>(a);
+    else text_bf16_kernel<D16, false, false><<<grid, 256, 0, s>>>(a);
+  }
+}
+
+// Blocks of a call, and how they are dealt (a.chunk, a.chunks); -1 past a grid.
+static long place_blocks(TextArgs& a) {
+  const long tiles = a.max_len < 1 ? 1 : ((long)a.max_len + TQ - 1) / TQ;  // (packed rows of no text may still be due zeros)
+  a.chunk = (int)(tiles < 8 ? tiles : 8);
+  a.chunks = (int)((tiles + a.chunk - 1) / a.chunk);
+  const double units = (double)a.n * a.kv_heads * a.chunks;
+  const double blocks = (units + 8) * a.chunk * a.rep;
+  if (blocks * 256 > 4.0e9) return -1;
+  return ((long)units + 7) / 8 * 8 * a.chunk * a.rep;
+}
+
+bool text_attention_fits(int n, int heads, int kv_heads, int max_len) {
+  TextArgs a;
+  a.n = n; a.kv_heads = kv_heads; a.rep = heads / kv_heads; a.max_len = max_len;
+  return place_blocks(a) >= 0;
+}
+
+hipError_t launch_text_attention(DType dt, TextArgs a, hipStream_t s) {
+  if (a.n <= 0) return hipSuccess;
+  const long blocks = place_blocks(a);
+  if (blocks < 0) return hipErrorInvalidValue;
+  const unsigned grid = (unsigned)blocks;
+  if (dt == BF16) {
+    if (a.d <= 32) launch_width<32>(a, grid, s);
+    else if (a.d <= 48) launch_width<48>(a, grid, s);
+    else if (a.d <= 64) launch_width<64>(a, grid, s);
+    else if (a.d <= 80) launch_width<80>(a, grid, s);
+    else if (a.d <= 96) launch_width<96>(a, grid, s);
+    else if (a.d <= 128) launch_width<128>(a, grid, s);
+    else if (a.d <= 192) launch_width<192>(a, grid, s);
+    else launch_width<256>(a, grid, s);
+  } else {
+    if (a.d <= 32) text_f32_kernel<32><<<grid, 256, 0, s>>>(a);
+    else if (a.d <= 64) text_f32_kernel<64><<<grid, 256, 0, s>>>(a);
+    else if (a.d <= 96) text_f32_kernel<96><<<grid, 256, 0, s>>>(a);
+    else if (a.d <= 128) text_f32_kernel<128><<<grid, 256, 0, s>>>(a);
+    else if (a.d <= 192) text_f32_kernel<192><<<grid, 256, 0, s>>>(a);
+    else text_f32_kernel<256><<<grid, 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace sd

@@ -343,3 +343,78 @@ def cross_attention(q, k, v, max_len, kv_start=None, kv_len=None, kv_index=None,
               v_ctx, tokens, n_ctx, max_len, start_p, len_p, index_p, _at(mask), out.data_ptr(), os[1], os[2], os[0], n,
               heads, kv_heads, d, n_q, d ** -0.5 if scale is None else scale, _at(scratch), floats))
     return out
+
+
+def text_attention(q, k, v, max_len, start=None, length=None, mask=None, causal=False, prefix=None, cap=None, bias=None,
+                   slope=None, scale=None, out=None):
+    """Attention inside texts of their own lengths.  Packed texts: q [tokens,
+    heads, d], k, v [tokens, kv_heads, d], text c at rows start[c] .. start[c +
+    1] - 1 (int32 [n + 1], not decreasing), mask (bool or uint8) [tokens].
+    Padded texts (start None): q [n, max_len, heads, d] and so on, length int32
+    [n] or None (all max_len), mask [n, max_len].  No text is longer than
+    max_len.  causal: a query sees the keys up to its own, and the first
+    prefix[c] (int32 [n]) of its text.  cap: a score s becomes cap tanh(s /
+    cap).  bias fp32 [heads, 2 reach + 1] is added by key less query, constant
+    past its ends; slope fp32 [heads] times their distance is taken off.  heads may be a
+    multiple of kv_heads (shared in order); q, k, v and out may be strided as
+    long as d is contiguous.  scale defaults to 1 / sqrt(d).  A query that sees
+    no key gives zeros.  Returns q's shape and type; rows in no text are zeros
+    in a new result and stay as they are in `out`."""
+    dt = q.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise TypeError(dt)
+    packed = start is not None
+    qshape, kshape = q.shape, k.shape
+    if len(qshape) != (3 if packed else 4) or len(kshape) != len(qshape):
+        _bad("q, k, v [tokens, heads, d] with start, [n, max_len, heads, d] without")
+    heads, d = qshape[-2:]
+    kv_heads = kshape[-2]
+    if k.dtype is not dt or v.dtype is not dt or kshape != v.shape or kshape[:-2] != qshape[:-2] or kshape[-1] != d:
+        _bad("k and v must have q's type, tokens and width, and one shape")
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    if d > 1 and (qs[-1] != 1 or ks[-1] != 1 or vs[-1] != 1):
+        _bad("d must be contiguous")
+    if packed:
+        if start.dim() != 1 or start.shape[0] < 1:
+            _bad("start must be int32 [n + 1]")
+        n, tokens, q_text, k_text, v_text = start.shape[0] - 1, qshape[0], 0, 0, 0
+        if length is not None:
+            _bad("packed texts end where the next one starts: no length")
+    else:
+        n, tokens, q_text, k_text, v_text = qshape[0], 0, qs[0], ks[0], vs[0]
+        if qshape[1] != max_len:
+            _bad("padded q, k, v must be [n, max_len, heads, d]")
+    _int32(max(n, tokens, heads, kv_heads, d, abs(max_len)))
+    start_p = _index(start, n + 1, "start") if packed else None
+    length_p = _index(length, n, "length") if length is not None else None
+    prefix_p = _index(prefix, n, "prefix") if prefix is not None else None
+    if mask is not None and ((mask.dtype is not torch.bool and mask.dtype is not torch.uint8) or mask.shape != qshape[:-2]
+                             or not mask.is_contiguous()):
+        _bad("mask must be bool or uint8, one value per token")
+    reach = 0
+    if bias is not None:
+        if bias.dtype is not torch.float32 or bias.dim() != 2 or bias.shape[0] != heads or bias.shape[1] % 2 == 0 or (
+                not bias.is_contiguous()):
+            _bad("bias must be fp32 [heads, 2 reach + 1], contiguous")
+        reach = bias.shape[1] // 2
+        _int32(reach)
+    if slope is not None and (slope.dtype is not torch.float32 or slope.shape != (heads,) or not slope.is_contiguous()):
+        _bad("slope must be fp32 [heads]")
+    if cap is not None and not cap > 0:
+        _bad("cap must be above 0")
+    fresh = out is None
+    if fresh:
+        out = q.new_empty(qshape)
+        if n == 0:
+            out.zero_()
+    elif out.shape != qshape or out.dtype is not dt:
+        _bad("out must have q's shape and type")
+    os = out.stride()
+    if d > 1 and os[-1] != 1:
+        _bad("out must have a contiguous d")
+    _enqueue(lib().synerdiff_op_text_attention, q, (k, v, start, length, mask, prefix, bias, slope, out),
+             (_TYPE[dt], q.data_ptr(), qs[-3], qs[-2], q_text, k.data_ptr(), ks[-3], ks[-2], k_text, v.data_ptr(), vs[-3],
+              vs[-2], v_text, out.data_ptr(), os[-3], os[-2], 0 if packed else os[0], tokens, n, max_len, start_p, length_p,
+              _at(mask), 1 if causal else 0, prefix_p, cap or 0.0, _at(bias), reach, _at(slope), heads, kv_heads, d,
+              d ** -0.5 if scale is None else scale, 1 if fresh else 0))
+    return out
