@@ -316,6 +316,31 @@ sd_status synerdiff_op_text_attention(int32_t dtype, const void* d_q, int64_t q_
                                       int32_t reach, const float* d_slope, int32_t heads, int32_t kv_heads, int32_t d,
                                       float scale, int32_t zero_rest, void* hip_stream);
 
+/* Linear layer that all rows share, plus a low-rank adapter for each (requests
+ * of one batch with styles of their own):
+ *   out[m, n] = bias[n] + sum_k x[m, k] w[n, k] + scale[c] sum_r v[m, r] up[c, n, r]
+ *   v[m, r] = sum_k x[m, k] down[c, r, k],   c = index[m / group]
+ * x [M, K], w [N, K], down [count, rank, K], up [count, N, rank] and out (row m
+ * at m * out_ld) in dtype; scale fp32 [count] (NULL: 1) and bias fp32 [N] (NULL:
+ * 0); index int32 [M / group rounded up].  A row whose index lies outside [0,
+ * count) has no adapter (count may be 0, down and up NULL then).  A row depends
+ * on no other row and on no other adapter than its own, whatever they hold.
+ * Narrower adapters are padded with zeros.  Sums are fp32; v is fp32 for fp32
+ * and for up to 64 rows, else held to 2^-17 of it (two bf16 parts; below 2^-110
+ * less).  Any order of indices is right; runs of 32 rows or more of one adapter are fast.
+ * Constraints: K, N, rank multiples of 8; K, N <= 2^20, rank <= 1024; w, up[c] and
+ * down[c] below 2^31 bytes; M <= 2^26, M N < 2^35 (fp32: M rank < 2^28); all
+ * buffers and rows of out at multiples of 16 bytes (scale, index: 4).  out
+ * overlaps nothing.  d_scratch (fp32, 16-byte aligned) holds
+ * synerdiff_op_linear_adapters_scratch_floats(M, rank) floats (SD_ERR_WORKSPACE
+ * if fewer), and belongs to this call until it has run.  M = 0 or N = 0 does nothing. */
+int64_t synerdiff_op_linear_adapters_scratch_floats(int32_t M, int32_t rank);
+sd_status synerdiff_op_linear_adapters(int32_t dtype, const void* d_x, int32_t M, int32_t K, const void* d_w, int32_t N,
+                                       const void* d_down, const void* d_up, int32_t rank, int32_t count,
+                                       const float* d_scale, const int32_t* d_index, int32_t group,
+                                       const float* d_bias, void* d_out, int64_t out_ld, float* d_scratch,
+                                       int64_t scratch_floats, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

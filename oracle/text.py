@@ -93,3 +93,20 @@ def text_attention(q, k, v, texts, scale, mask=None, causal=False, prefix=None, 
                 o[first + i, h] = p @ v[first + js[on], h // rep]
                 w[first + i, h] = p @ np.abs(v[first + js[on], h // rep])
     return o, w
+
+
+def linear_adapters(x, w, down, up, index, scale=None, bias=None):
+    """Rows x [M, K]: w x + bias + scale[c] up[c] (down[c] x), c = index[m]
+    where it lies in 0 .. count - 1.  Returns (y, s, t): s the sum of the terms'
+    sizes of the shared product, t that of the adapter's, of |down x| times |up|."""
+    x, w, down, up = (np.asarray(t, F) for t in (x, w, down, up))
+    b = 0 if bias is None else np.asarray(bias, F)
+    y = x @ w.T + b
+    s = np.abs(x) @ np.abs(w).T + np.abs(b)
+    t = np.zeros_like(y)
+    for m, c in enumerate(index):
+        if 0 <= c < len(down):
+            f = 1.0 if scale is None else float(scale[c])
+            y[m] += f * (up[c] @ (down[c] @ x[m]))
+            t[m] = abs(f) * (np.abs(up[c]) @ (np.abs(down[c]) @ np.abs(x[m])))
+    return y, s, t

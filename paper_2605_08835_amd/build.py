@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "libsynerdiff.so")
 SOURCES = ["manifest.cpp", "unet.cpp", "ops.cpp", "gemm.hip", "attention.hip", "misc.hip", "output.hip", "rmsnorm.hip", "linear_w4.hip",
-           "cross_attention.hip", "text_attention.hip", "vae.cpp", "vae_kernels.hip", "sched.cpp"]
+           "cross_attention.hip", "text_attention.hip", "linear_adapters.hip",
+           "vae.cpp", "vae_kernels.hip", "sched.cpp"]
 
 ARCH = "gfx950"
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-result", "-Wno-unused-variable",

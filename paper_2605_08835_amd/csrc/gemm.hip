@@ -6,6 +6,8 @@
 // matrix stored N-major with K contiguous.  bf16 runs on MFMA
 // (v_mfma_f32_32x32x16_bf16, fp32 accumulation); fp32 on v_mfma_f32_16x16x4_f32
 // (true fp32, no reduced-precision products).
+#include <type_traits>
+
 #include "device_common.h"
 #include "kernels.h"
 
@@ -665,6 +667,109 @@ __device__ __forceinline__ T pick(bool c, T a, T b) {
   return c ? a : b;
 }
 
+// The adapter's part of a block's rows, added to its accumulators: for every
+// adapter among the wave's rows, products of its `up` rows with the rows' hi and lo.
+// Rows are a lane's own, so rows of other adapters keep their sums untouched
+// (whatever this one holds), by a select where an adapter has only some of 32 rows.
+template <int BM, int BN, int WM, int WN, int TM, int TN>
+__device__ __forceinline__ void adapter_products(const AdapterArgs& a, f32x16 (&acc)[TM][TN], int m0, int n0, int wm, int wn,
+                                                 int lane) {
+  const int lr = lane & 31, lh = lane >> 5;
+  int id[TM];
+  uint64_t left[TM], any = 0;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = m0 + wm * (BM / WM) + i * 32 + lr, at = a.row0 + m;
+    id[i] = -1;
+    if (m < a.M) id[i] = a.index[a.group == 1 ? at : (int)(__umulhi((unsigned)at, a.group_mul) >> a.group_shift)];
+    if (id[i] >= a.count) id[i] = -1;
+    left[i] = __ballot(id[i] >= 0);
+    any |= left[i];
+  }
+  while (any) {
+    int cur = 0;
+#pragma unroll
+    for (int i = TM - 1; i >= 0; --i)
+      if (left[i]) cur = __builtin_amdgcn_readlane(id[i], __builtin_ctzll(left[i]));
+    uint64_t mine[TM];
+    any = 0;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      mine[i] = __ballot(id[i] == cur);
+      left[i] &= ~mine[i];
+      any |= left[i];
+    }
+    const long rows = (long)a.M * a.rank * 2;  // (read through resources: what lies past rank or N is zero)
+    const __amdgpu_buffer_rsrc_t br = make_rsrc(a.up + (long)cur * a.N * a.rank, (long)a.N * a.rank * 2);
+    const __amdgpu_buffer_rsrc_t hr = make_rsrc(a.hi + (long)a.row0 * a.rank, rows), lor = make_rsrc(a.lo + (long)a.row0 * a.rank, rows);
+#pragma unroll 1
+    for (int k = 8 * lh; k - 8 * lh < a.rank; k += 16) {
+      bf16x8 b[TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int n = n0 + wn * (BN / WN) + j * 32 + lr;
+        b[j] = buf_load16(br, k < a.rank && n < a.N ? (n * a.rank + k) * 2 : OOB);
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        if (!mine[i]) continue;
+        const int m = m0 + wm * (BM / WM) + i * 32 + lr, at = k < a.rank && m < a.M ? (m * a.rank + k) * 2 : OOB;
+        const bf16x8 h = buf_load16(hr, at), l = buf_load16(lor, at);
+        const bool whole = mine[i] == ~0ull, on = id[i] == cur;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          f32x16 t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j], h, acc[i][j], 0, 0, 0);
+          t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j], l, t, 0, 0, 0);
+          if (whole) {
+            acc[i][j] = t;
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = on ? t[r] : acc[i][j][r];
+          }
+        }
+      }
+    }
+  }
+}
+
+// The epilogue of such a GEMM: as epilogue_staged with a bias alone, for any N that is a multiple of 8.
+template <int BM, int BN, int WM, int WN, int TM, int TN>
+__device__ __forceinline__ void epilogue_adapters(const AdapterArgs& a, const f32x16 (&acc)[TM][TN], int m0, int n0, int wm,
+                                                  int wn, int lane, bf16* R) {
+  constexpr int WC = BN / WN, LD = STAGED_LD<WC>, CP = WC / 8, NCH = 32 * CP / 64;
+  const int lr = lane & 31, hq = 4 * (lane >> 5), ncol0 = n0 + wn * WC;
+  static_for<0, TM>([&](auto I) {
+    const int mrow0 = m0 + wm * (BM / WM) + I.value * 32;
+    static_for<0, TN>([&](auto J) {
+      const f32x16 v = acc[I.value][J.value];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int n = ncol0 + J.value * 32 + 8 * q + hq;
+        const float4 b = a.epi.bias && n < a.N ? *reinterpret_cast<const float4*>(a.epi.bias + n) : make_float4(0.f, 0.f, 0.f, 0.f);
+        bf16x4 o;
+        o[0] = (bf16)(v[4 * q] + b.x);
+        o[1] = (bf16)(v[4 * q + 1] + b.y);
+        o[2] = (bf16)(v[4 * q + 2] + b.z);
+        o[3] = (bf16)(v[4 * q + 3] + b.w);
+        *reinterpret_cast<bf16x4*>(R + lr * LD + J.value * 32 + 8 * q + hq) = o;
+      }
+    });
+    asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
+    bf16x8 ob[NCH];
+#pragma unroll
+    for (int u = 0; u < NCH; ++u) {
+      const int c = lane + 64 * u, row = c / CP, ch = c - row * CP;
+      ob[u] = *reinterpret_cast<const bf16x8*>(R + row * LD + ch * 8);
+    }
+#pragma unroll
+    for (int u = 0; u < NCH; ++u) {
+      const int c = lane + 64 * u, row = c / CP, ch = c - row * CP, m = mrow0 + row, n = ncol0 + ch * 8;
+      if (m < a.M && n < a.N) *reinterpret_cast<bf16x8*>(reinterpret_cast<bf16*>(a.epi.out) + (long)m * a.epi.ldo + n) = ob[u];
+    }
+    asm volatile("" ::: "memory");
+  });
+}
+
 // A and B tiles of DK-deep K slices in DNS LDS stages, one barrier per tile.
 // All stages are in flight; fragments are read ahead of their products (a
 // 16-deep substep, or a tile for the smallest wave tiles), the next tile's
@@ -678,8 +783,12 @@ __device__ __forceinline__ T pick(bool c, T a, T b) {
 // the caches: 131072 x 320 x 320 in 256x160 tiles 69 us with the general setup and
 // 61 with this one (77 and 71 after four other kernels), 512 x 1280 x 1280 18.2 and
 // 15.8 (13.8 and 11.6), 49152 x 5120 x 640 451 and 424.
-template <int BM, int BN, int WM, int WN, bool UP, int DK, int DNS, int MINB, bool TI, bool LIN = false>
-__global__ __launch_bounds__(64 * WM * WN, MINB) void gemm_bf16_dma_kernel(GemmArgs a) {
+// ARGS = AdapterArgs (with LIN): rows also get their adapter's part, and K and N
+// need only be multiples of 8 (chunks past K read as zero in the last tile).
+template <int BM, int BN, int WM, int WN, bool UP, int DK, int DNS, int MINB, bool TI, bool LIN = false, typename ARGS = GemmArgs>
+__global__ __launch_bounds__(64 * WM * WN, MINB) void gemm_bf16_dma_kernel(ARGS a) {
+  constexpr bool ADP = std::is_same<ARGS, AdapterArgs>::value;
+  static_assert(!ADP || LIN, "adapters go with plain linear layers");
   constexpr int NWV = WM * WN;                          // waves per block
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   constexpr int CPR = DK / 8, RPL = 64 / CPR;           // 16-byte chunks per row, rows per load
@@ -752,6 +861,17 @@ __global__ __launch_bounds__(64 * WM * WN, MINB) void gemm_bf16_dma_kernel(GemmA
   }
 
   const int nk_all = (a.K + DK - 1) / DK;  // K is a multiple of DK
+  // (ADP) bit j: this lane's chunk of A load j, or of B load j, lies past K in the last tile
+  uint32_t tail_a = 0, tail_b = 0;
+  if constexpr (ADP) {
+    const int last = a.K % DK * 2;
+    if (last) {
+#pragma unroll
+      for (int j = 0; j < AW; ++j) tail_a |= (uint32_t)(chunk16(wave * AW + j) >= last) << j;
+#pragma unroll
+      for (int j = 0; j < BW; ++j) tail_b |= (uint32_t)(chunk16(wave + NWV * j) >= last) << j;
+    }
+  }
   const int per = uni((nk_all + a.ksplit - 1) / a.ksplit);
   const int kb = split * per, nk = max(min(nk_all, kb + per) - kb, 0);
 
@@ -854,6 +974,7 @@ __global__ __launch_bounds__(64 * WM * WN, MINB) void gemm_bf16_dma_kernel(GemmA
   // Issue the loads of the next K tile into stage `stg`.
   auto issue = [&](int stg) __attribute__((always_inline)) {
     const __amdgpu_buffer_rsrc_t ares = make_rsrc(s.ab, 0x7FFFFFFF);
+    const uint32_t ta = ADP && s.togo == 1 ? tail_a : 0, tb = ADP && s.togo == 1 ? tail_b : 0;
     bf16* adst = As + stg * BM * DK + wave * AW * 512;
 #pragma unroll
     for (int j = 0; j < AW; ++j) {
@@ -863,14 +984,14 @@ __global__ __launch_bounds__(64 * WM * WN, MINB) void gemm_bf16_dma_kernel(GemmA
         const int iy = ((pyx[j] >> 16) + ky) >> 1, ix = ((pyx[j] & 0xFFFF) + kx) >> 1;
         v = (pix[j] + iy * Wi + ix) * s.cs2 + chunk16(wave * AW + j);
       }
-      dma16(ares, adst + j * 512, LIN ? v | s.dead : ((nmask[j] << s.sh) & OOB) | (UP ? v & 0x7FFFFFFF : v), 0);
+      dma16(ares, adst + j * 512, ADP ? v | s.dead | (int)(ta << (31 - j) & (uint32_t)OOB) : LIN ? v | s.dead : ((nmask[j] << s.sh) & OOB) | (UP ? v & 0x7FFFFFFF : v), 0);
     }
     bf16* bdst = Bs + stg * BN * DK;
     const int boff = uni(s.boff);
 #pragma unroll
     for (int j = 0; j < BW; ++j) {
       const int i = wave + NWV * j;
-      dma16(bres, (SPARE && i >= BI) ? spare : bdst + i * 512, voffB[j] | s.dead, boff);
+      dma16(bres, (SPARE && i >= BI) ? spare : bdst + i * 512, ADP ? voffB[j] | s.dead | (int)(tb << (31 - j) & (uint32_t)OOB) : voffB[j] | s.dead, boff);
     }
   };
   auto advance = [&]() __attribute__((always_inline)) {
@@ -978,9 +1099,13 @@ __global__ __launch_bounds__(64 * WM * WN, MINB) void gemm_bf16_dma_kernel(GemmA
     stage_barrier();
     __builtin_amdgcn_sched_barrier(0);
   };
+  auto adapters = [&]() __attribute__((always_inline)) {  // (beside the first tiles' loads)
+    if constexpr (ADP) adapter_products<BM, BN, WM, WN>(a, acc, m0, n0, wm, wn, lane);
+  };
   int st = 0;  // stage of the tile
   if constexpr (WT) {
     prologue(DNS);
+    adapters();
     wait_vmcnt<(DNS - 1) * LPT>();  // tile 0 has landed
     stage_barrier();
     static_for<0, KS>([&](auto K) { readf(0, K.value, fa[K.value], fb[K.value]); });
@@ -1000,6 +1125,7 @@ __global__ __launch_bounds__(64 * WM * WN, MINB) void gemm_bf16_dma_kernel(GemmA
     }
   } else if constexpr (PF) {
     prologue(DNS);
+    adapters();
     wait_vmcnt<(DNS - 1) * LPT>();  // tile 0 has landed
     stage_barrier();
     readf(0, 0, fa[0], fb[0]);
@@ -1036,6 +1162,7 @@ __global__ __launch_bounds__(64 * WM * WN, MINB) void gemm_bf16_dma_kernel(GemmA
     }
   } else {
     prologue(DNS - 1);
+    adapters();
     for (int kt = 0; kt < nk; ++kt) {
       next_ready();  // (here: tile kt may be read, the stage of tile kt - 1 refilled)
       static_for<0, KS>([&](auto KSI) {
@@ -1049,6 +1176,11 @@ __global__ __launch_bounds__(64 * WM * WN, MINB) void gemm_bf16_dma_kernel(GemmA
     }
   }
   wait_vmcnt<0>();  // the refills past the last tile have landed
+  if constexpr (ADP) {
+    __syncthreads();  // every wave is done with the operand stages
+    epilogue_adapters<BM, BN, WM, WN>(a, acc, m0, n0, wm, wn, lane, smem + wave * 32 * STAGED_LD<BN / WN>);
+    return;
+  }
   if (a.ksplit > 1) {
     // raw fp32 partial sums; the reduction kernel applies the epilogue
     const int lr = lane & 31, hq = 4 * (lane >> 5);
@@ -1642,6 +1774,52 @@ hipError_t launch_gemm(DType dt, const GemmArgs& args, hipStream_t s) {
       launch_f32<4>(a, s);
     else
       launch_f32<2>(a, s);
+  }
+  return hipGetLastError();
+}
+
+// The tiles above for a linear layer with adapters, by the same model of their
+// time (columns of a last tile that N does not fill are computed and not stored).
+template <int BM, int BN, int WM, int WN, int DNS, int MINB>
+static void launch_adapters(const AdapterArgs& a, hipStream_t s) {
+  const long blocks = (long)((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN);
+  gemm_bf16_dma_kernel<BM, BN, WM, WN, false, 64, DNS, MINB, false, true, AdapterArgs>
+      <<<dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s>>>(a);
+}
+
+hipError_t launch_gemm_adapters(const AdapterArgs& args, hipStream_t s) {
+  AdapterArgs a = args;
+  a.ksplit = 1;
+  if (a.K % 8 || a.N % 8 || a.rank % 8 || (long)a.M * a.K >= 1L << 30 || (long)a.N * a.K >= 1L << 30)
+    return hipErrorInvalidValue;
+  if ((long)a.M * a.rank >= 1L << 30 || (long)a.N * a.rank >= 1L << 30) return hipErrorInvalidValue;
+  if (a.group > 1) {  // m = q group + s, m < 2^31: with l = ceil(log2 group), mul = ceil(2^(31 + l) / group), q = m mul >> (31 + l)
+    int l = 0;
+    while ((1u << l) < (unsigned)a.group) ++l;
+    a.group_mul = (unsigned)(((1ull << (31 + l)) + a.group - 1) / a.group);
+    a.group_shift = l - 1;
+  }
+  const float nk = (float)((a.K + 63) / 64);
+  int best = 0;
+  float tbest = 0.f;
+  for (int i = 0; i < (int)(sizeof(kTiles64) / sizeof(kTiles64[0])); ++i) {
+    const Tile64& t = kTiles64[i];
+    const long blocks = (long)((a.M + t.bm - 1) / t.bm) * ((a.N + t.bn - 1) / t.bn), slots = 256L * t.occ;
+    const long full = blocks / slots, rest = (blocks - full * slots + 255) / 256;
+    const float tr = t.occ > 1 ? t.t1 + (t.tf - t.t1) * (float)(rest - 1) / (float)(t.occ - 1) : t.t1;
+    const float us = (float)full * (nk * t.tf + t.eb) + (rest > 0 ? nk * tr + t.eb : 0.f);
+    if (i == 0 || us < tbest) {
+      best = i;
+      tbest = us;
+    }
+  }
+  switch (best) {
+    case 0: launch_adapters<64, 64, 2, 2, 4, 2>(a, s); break;
+    case 1: launch_adapters<128, 64, 2, 2, 3, 2>(a, s); break;
+    case 2: launch_adapters<128, 128, 2, 2, 2, 2>(a, s); break;
+    case 3: launch_adapters<128, 160, 4, 1, 2, 2>(a, s); break;
+    case 4: launch_adapters<256, 256, 2, 4, 2, 1>(a, s); break;
+    default: launch_adapters<256, 320, 4, 2, 2, 1>(a, s); break;
   }
   return hipGetLastError();
 }

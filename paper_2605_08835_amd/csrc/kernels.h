@@ -71,6 +71,20 @@ struct GemmArgs {
 
 // bf16 requires N % 4 == 0, 8-byte aligned outputs and ldo, ldr % 4 == 0.
 hipError_t launch_gemm(DType dt, const GemmArgs& a, hipStream_t s);
+
+// A GEMM of one contiguous 1x1 source whose rows also get their adapter's part:
+//   out[m, n] = bias[n] + sum_k A[m, k] B[n, k] + sum_r (hi + lo)[m, r] up[id(m), n, r]
+// with id(m) = index[m / group] (none if outside 0 .. count - 1).
+struct AdapterArgs : GemmArgs {
+  const bf16_t *hi, *lo;  // [M, rank]
+  const bf16_t* up;       // [count, N, rank]
+  const int* index;
+  int group, count, rank; // rank a multiple of 8
+  int row0;               // row 0 of the GEMM is row row0 of hi, lo and the index
+  unsigned group_mul, group_shift;  // m / group = umulhi(m, mul) >> shift (group > 1)
+};
+// bf16; K and N multiples of 8; M K and N K below 2^30; out and ldo at multiples of 16 bytes.
+hipError_t launch_gemm_adapters(const AdapterArgs& a, hipStream_t s);
 // Split-K factor launch_gemm supports for this bf16 GEMM (1 = no split).
 int gemm_ksplit(const GemmArgs& a);
 
@@ -208,6 +222,21 @@ struct LinearW4Args {
   void* out; long out_ld; int out_f32;
 };
 hipError_t launch_linear_w4(const LinearW4Args& a, hipStream_t s);
+
+// Linear layer with a low-rank adapter per row, see synerdiff_op_linear_adapters.
+struct LinearAdaptersArgs {
+  const void* x;       // [M, K]
+  const void* w;       // [N, K]
+  const void *down, *up;  // [count, rank, K], [count, N, rank]
+  const float* scale;  // [count] or null
+  const int* index;    // one entry per `group` rows
+  const float* bias;   // [N] or null
+  void* out; long out_ld;
+  int M, K, N, rank, count, group;
+  float* scratch;
+};
+hipError_t launch_linear_adapters(DType dt, const LinearAdaptersArgs& a, hipStream_t s);
+long linear_adapters_scratch_floats(int M, int rank);
 
 // Attention over contexts of their own lengths, see synerdiff_op_cross_attention.
 struct CrossArgs {

@@ -1,0 +1,349 @@
+// Linear layer whose rows may each have a low-rank adapter of their own:
+//   out[m] = bias + W x[m] + scale[c] up[c] (down[c] x[m]),  c = index[m / group].
+//
+// Two launches: v = scale[c] down[c] x first, then the layer, which adds up[c] v.
+//  * Many rows (bf16): v on MFMAs, 32 rows a block; then the GEMM of gemm.hip,
+//    whose accumulators start with the adapters' part.  v is kept as two bf16 parts
+//    (2^-17 of it), so that the second product is one of bf16 MFMAs too.
+//  * Few rows (bf16, at most 64): bound by the bytes of W and of the adapters in use.
+//    A block has 16 outputs of all rows, its waves share out K.  v is fp32.
+//  * fp32: the adapters' part goes to `out` first and is the GEMM's residual.
+// A row sees its own adapter only: what others hold, infinities and NaN included,
+// does not reach it.
+#include <string.h>
+
+#include "device_common.h"
+#include "kernels.h"
+
+namespace sd {
+
+namespace {
+
+__device__ __forceinline__ int adapter_of(const LinearAdaptersArgs& a, int m) {
+  const int c = a.index[a.group == 1 ? m : m / a.group];
+  return c >= 0 && c < a.count ? c : -1;
+}
+
+__device__ __forceinline__ f32x16 mfma32(bf16x8 x, bf16x8 y, f32x16 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+__device__ __forceinline__ f32x4 mfma16(bf16x8 x, bf16x8 y, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------ v, few rows
+// A wave has one row and four of its adapter's rows, lanes share out K 8 at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void adapters_down_rows_kernel(LinearAdaptersArgs a) {
+  constexpr int RW = 4;
+  const int per = (a.rank + RW - 1) / RW, lane = threadIdx.x & 63;
+  const long id = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (id >= (long)a.M * per) return;
+  const int m = (int)(id / per), r0 = (int)(id % per) * RW;
+  const int c = adapter_of(a, m);
+  if (c < 0) return;  // (its v is not read)
+  const T* x = (const T*)a.x + (long)m * a.K;
+  const T* d = (const T*)a.down + ((long)c * a.rank + r0) * a.K;
+  float s[RW];
+#pragma unroll
+  for (int r = 0; r < RW; ++r) s[r] = 0.f;
+  for (int k = lane * 8; k < a.K; k += 512) {
+    float xv[8], dv[RW][8];
+    load8f(x + k, xv);
+#pragma unroll
+    for (int r = 0; r < RW; ++r) load8f(d + (long)r * a.K + k, dv[r]);  // (rank is a multiple of 8)
+#pragma unroll
+    for (int r = 0; r < RW; ++r)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[r] = fmaf(xv[e], dv[r][e], s[r]);
+  }
+#pragma unroll
+  for (int r = 0; r < RW; ++r) s[r] = wave_sum(s[r]);
+  const float f = a.scale ? a.scale[c] : 1.f;
+  if (lane == 0) *(float4*)(a.scratch + (long)m * a.rank + r0) = make_float4(s[0] * f, s[1] * f, s[2] * f, s[3] * f);
+}
+
+// ------------------------------------------------------------------ v, many rows
+// A block has 32 rows and RT x 32 of the rank, its KW waves share out K 64 at a
+// time: V^T = down x^T, so that a lane has one row's values.  v's two parts go to
+// scratch, [M, rank] each.
+template <int RT, int KW>
+__global__ __launch_bounds__(64 * KW) void adapters_down_kernel(LinearAdaptersArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 31, lh = lane >> 5;
+  const int m = blockIdx.x * 32 + lr, r0 = blockIdx.y * RT * 32;
+  __shared__ float part[KW > 1 ? KW - 1 : 1][KW > 1 ? RT * 16 * 64 : 1];
+  const int c = m < a.M ? adapter_of(a, m) : -1;
+  uint64_t left = __ballot(c >= 0);
+  const int rows = min(32, a.M - (int)blockIdx.x * 32);
+  const __amdgpu_buffer_rsrc_t xr = make_rsrc((const bf16*)a.x + (long)blockIdx.x * 32 * a.K, (long)rows * a.K * 2);
+  while (left) {
+    const int cur = __builtin_amdgcn_readlane(c, __builtin_ctzll(left));
+    left &= ~__ballot(c == cur);
+    const __amdgpu_buffer_rsrc_t dr =
+        make_rsrc((const bf16*)a.down + ((long)cur * a.rank + r0) * a.K, (long)(a.rank - r0) * a.K * 2);
+    f32x16 acc[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+    for (int k0 = wave * 64; k0 < a.K; k0 += KW * 64) {
+      bf16x8 xv[4], dv[RT][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = k0 + 16 * j + 8 * lh;
+        xv[j] = buf_load16(xr, k < a.K ? (lr * a.K + k) * 2 : OOB);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) dv[t][j] = buf_load16(dr, k < a.K ? ((32 * t + lr) * a.K + k) * 2 : OOB);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[t] = mfma32(dv[t][j], xv[j], acc[t]);
+    }
+    if constexpr (KW > 1) {
+      __syncthreads();
+      if (wave > 0)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) part[wave - 1][(t * 16 + i) * 64 + lane] = acc[t][i];
+      __syncthreads();
+      if (wave == 0)
+#pragma unroll
+        for (int w = 0; w < KW - 1; ++w)
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[t][i] += part[w][(t * 16 + i) * 64 + lane];
+    }
+    if (wave == 0 && c == cur) {
+      const float f = a.scale ? a.scale[c] : 1.f;
+      bf16 *hi = (bf16*)a.scratch + (long)m * a.rank, *lo = hi + (long)a.M * a.rank;
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int r = r0 + 32 * t + 8 * q + 4 * lh;
+          if (r < a.rank) {
+            bf16x4 h, l;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = acc[t][4 * q + e] * f;
+              h[e] = (bf16)v;
+              l[e] = (bf16)(v - (float)h[e]);
+            }
+            *(bf16x4*)(hi + r) = h;
+            *(bf16x4*)(lo + r) = l;
+          }
+        }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ few rows, bf16
+// A block has 16 outputs of all rows (MT x 16), its 8 waves share out K 64 at a
+// time and are summed in order.
+template <int MT>
+__global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a) {
+  constexpr int NW = 8;
+  __shared__ float part[NW][MT][256];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, lk = 8 * (lane >> 4);
+  const int n0 = blockIdx.x * 16;
+  const __amdgpu_buffer_rsrc_t wr = make_rsrc((const bf16*)a.w + (long)n0 * a.K, (long)min(16, a.N - n0) * a.K * 2);
+  const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.x, (long)a.M * a.K * 2);
+  f32x4 acc[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+  for (int k0 = wave * 64; k0 < a.K; k0 += NW * 64) {
+    bf16x8 wv[2], xv[2][MT];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int k = k0 + 32 * j + lk;
+      wv[j] = buf_load16(wr, k < a.K ? (lr * a.K + k) * 2 : OOB);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) xv[j][t] = buf_load16(xr, k < a.K ? ((16 * t + lr) * a.K + k) * 2 : OOB);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int t = 0; t < MT; ++t) acc[t] = mfma16(wv[j], xv[j][t], acc[t]);  // (outputs 4 (lane / 16) + i of row lane % 16)
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) *(f32x4*)&part[wave][t][4 * lane] = acc[t];
+  __syncthreads();
+  for (int i = threadIdx.x; i < MT * 256; i += 512) {
+    // element i % 4 of lane i / 4: output 4 (lane / 16) + i % 4, row lane % 16
+    const int t = i >> 8, at = i & 255, m = 16 * t + (at >> 2 & 15), n = n0 + 4 * (at >> 6) + (at & 3);
+    if (m >= a.M || n >= a.N) continue;
+    float s = a.bias ? a.bias[n] : 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) s += part[w][t][at];
+    const int c = adapter_of(a, m);
+    if (c >= 0) {
+      const float* v = a.scratch + (long)m * a.rank;
+      const bf16* u = (const bf16*)a.up + ((long)c * a.N + n) * a.rank;
+      for (int r = 0; r < a.rank; r += 8) {
+        float uv[8], vv[8];
+        load8f(u + r, uv);
+        load8f(v + r, vv);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(uv[e], vv[e], s);
+      }
+    }
+    ((bf16*)a.out)[(long)m * a.out_ld + n] = (bf16)s;
+  }
+}
+
+// ------------------------------------------------------------------ fp32: the adapters' part
+// A thread has one output column of 8 rows; rows with the first one's adapter share its loads.
+__global__ __launch_bounds__(256) void adapters_up_f32_kernel(LinearAdaptersArgs a) {
+  constexpr int MR = 8;
+  const int n = blockIdx.y * 256 + threadIdx.x;
+  const long m0 = (long)blockIdx.x * MR;
+  if (n >= a.N) return;
+  const int rows = (int)min((long)MR, a.M - m0);
+  int c[MR];
+  float s[MR];
+  for (int i = 0; i < MR; ++i) {
+    c[i] = i < rows ? adapter_of(a, (int)m0 + i) : -1;
+    s[i] = 0.f;
+  }
+  int left = 0;
+#pragma unroll
+  for (int i = 0; i < MR; ++i) left |= (c[i] >= 0) << i;
+  while (left) {
+    int cur = -1;
+#pragma unroll
+    for (int i = MR - 1; i >= 0; --i)
+      if (left >> i & 1) cur = c[i];
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < MR; ++i) mine |= (c[i] == cur) << i;
+    left &= ~mine;
+    const float* u = (const float*)a.up + ((long)cur * a.N + n) * a.rank;
+    const float* v = a.scratch + m0 * a.rank;
+    for (int r = 0; r < a.rank; r += 4) {
+      const float4 uv = *(const float4*)(u + r);
+#pragma unroll
+      for (int i = 0; i < MR; ++i)
+        if (mine >> i & 1) {
+          const float4 vv = *(const float4*)(v + (long)i * a.rank + r);
+          s[i] = fmaf(uv.x, vv.x, fmaf(uv.y, vv.y, fmaf(uv.z, vv.z, fmaf(uv.w, vv.w, s[i]))));
+        }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MR; ++i)
+    if (i < rows) ((float*)a.out)[(m0 + i) * a.out_ld + n] = s[i];
+}
+
+// ------------------------------------------------------------------ launch
+constexpr int FEW = 64;  // rows of the few-row kernel
+
+long linear_adapters_scratch_floats(int M, int rank) { return (long)M * rank; }
+
+template <int RT>
+static void launch_down(const LinearAdaptersArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.M + 31) / 32), (unsigned)((a.rank + 32 * RT - 1) / (32 * RT)));
+  if (a.M < 32768 && a.K > 64)
+    adapters_down_kernel<RT, 4><<<grid, 256, 0, s>>>(a);
+  else
+    adapters_down_kernel<RT, 1><<<grid, 64, 0, s>>>(a);
+}
+
+template <typename T>
+static void launch_down_rows(const LinearAdaptersArgs& a, hipStream_t s) {
+  const long waves = (long)a.M * (a.rank / 4);
+  adapters_down_rows_kernel<T><<<dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s>>>(a);
+}
+
+static hipError_t launch_bf16(const LinearAdaptersArgs& a, hipStream_t s) {
+  if (a.M <= FEW) {
+    launch_down_rows<bf16>(a, s);
+    const dim3 grid((unsigned)((a.N + 15) / 16));
+    if (a.M <= 16) adapters_rows_kernel<1><<<grid, 512, 0, s>>>(a);
+    else if (a.M <= 32) adapters_rows_kernel<2><<<grid, 512, 0, s>>>(a);
+    else adapters_rows_kernel<4><<<grid, 512, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  if (a.rank <= 32) launch_down<1>(a, s);
+  else if (a.rank <= 64) launch_down<2>(a, s);
+  else launch_down<4>(a, s);
+  // (rows in parts whose offsets fit 32 bits)
+  const long widest = a.K > a.rank ? a.K : a.rank;
+  const long step = ((1L << 30) - 1) / widest / 256 * 256;
+  for (long m0 = 0; m0 < a.M; m0 += step) {
+    AdapterArgs g;
+    memset(&g, 0, sizeof(g));
+    g.M = (int)(a.M - m0 < step ? a.M - m0 : step);
+    g.N = a.N;
+    g.K = a.K;
+    ASeg& seg = g.seg[0];
+    seg.src0 = (const bf16_t*)a.x + m0 * a.K;
+    seg.c0 = seg.cin = seg.K = a.K;
+    seg.ks = seg.stride = 1;
+    seg.Hi = seg.Ho = 1;
+    seg.Wi = seg.Wo = g.M;
+    g.B = a.w;
+    g.ldb = a.K;
+    g.epi.bias = a.bias;
+    g.epi.out = (bf16_t*)a.out + m0 * a.out_ld;
+    g.epi.ldo = (int)a.out_ld;
+    g.hi = (const bf16_t*)a.scratch;
+    g.lo = g.hi + (long)a.M * a.rank;
+    g.up = (const bf16_t*)a.up;
+    g.index = a.index;
+    g.group = a.group;
+    g.count = a.count;
+    g.rank = a.rank;
+    g.row0 = (int)m0;
+    const hipError_t e = launch_gemm_adapters(g, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+static hipError_t launch_f32(const LinearAdaptersArgs& a, hipStream_t s) {
+  launch_down_rows<float>(a, s);
+  adapters_up_f32_kernel<<<dim3((unsigned)((a.M + 7) / 8), (unsigned)((a.N + 255) / 256)), dim3(256), 0, s>>>(a);
+  GemmArgs g;
+  memset(&g, 0, sizeof(g));
+  g.M = a.M;
+  g.N = a.N;
+  g.K = a.K;
+  ASeg& seg = g.seg[0];
+  seg.src0 = a.x;
+  seg.c0 = seg.cin = seg.K = a.K;
+  seg.ks = seg.stride = 1;
+  seg.Hi = seg.Ho = 1;
+  seg.Wi = seg.Wo = a.M;
+  g.B = a.w;
+  g.ldb = a.K;
+  g.epi.bias = a.bias;
+  g.epi.hw = 1;
+  g.epi.resid = a.out;
+  g.epi.ldr = (int)a.out_ld;
+  g.epi.out = a.out;
+  g.epi.ldo = (int)a.out_ld;
+  g.epi.out_f32 = 1;
+  g.ksplit = 1;
+  return launch_gemm(F32, g, s);
+}
+
+hipError_t launch_linear_adapters(DType dt, const LinearAdaptersArgs& a, hipStream_t s) {
+  if (a.M <= 0 || a.N <= 0) return hipSuccess;
+  return dt == BF16 ? launch_bf16(a, s) : launch_f32(a, s);
+}
+
+}  // namespace sd

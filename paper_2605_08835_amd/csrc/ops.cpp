@@ -479,4 +479,41 @@ sd_status synerdiff_op_text_attention(int32_t dtype, const void* q, int64_t q_ld
   return op_hip(launch_text_attention((DType)dtype, a, (hipStream_t)stream), "text_attention");
 }
 
+int64_t synerdiff_op_linear_adapters_scratch_floats(int32_t M, int32_t rank) {
+  return M > 0 && rank > 0 ? linear_adapters_scratch_floats(M, rank) : 0;
+}
+
+sd_status synerdiff_op_linear_adapters(int32_t dtype, const void* x, int32_t M, int32_t K, const void* w, int32_t N,
+                                       const void* down, const void* up, int32_t rank, int32_t count,
+                                       const float* scale, const int32_t* index, int32_t group, const float* bias,
+                                       void* out, int64_t out_ld, float* scratch, int64_t scratch_floats, void* stream) {
+  if (bad_dtype(dtype)) return op_fail(SD_ERR_INVALID_ARG, "bad dtype");
+  if (M < 0 || N < 0 || K <= 0 || K % 8 || N % 8 || rank <= 0 || rank % 8 || count < 0 || group < 1)
+    return op_fail(SD_ERR_INVALID_ARG, "bad shape (K, N and rank multiples of 8)");
+  const int64_t whole = dtype == SD_BF16 ? 1ll << 30 : 1ll << 29;
+  if ((int64_t)N * K >= whole || (int64_t)N * rank >= whole || (int64_t)rank * K >= whole || K > 1 << 20 || N > 1 << 20 ||
+      rank > 1 << 10)
+    return op_fail(SD_ERR_UNSUPPORTED, "weights of 2^31 bytes, more than 2^20 columns or ranks past 1024");
+  if (M > 1 << 26 || (int64_t)M * N >= 1ll << 35 || (int64_t)M * rank >= 1ll << 33 ||
+      (dtype == SD_F32 && (int64_t)M * rank >= 1ll << 28))
+    return op_fail(SD_ERR_UNSUPPORTED, "too many rows");
+  if (M == 0 || N == 0) return SD_OK;
+  if (!x || !w || !index || !out || (count > 0 && (!down || !up))) return op_fail(SD_ERR_INVALID_ARG, "NULL argument");
+  if (out_ld < N || out_ld > 1 << 30) return op_fail(SD_ERR_INVALID_ARG, "the row stride is below a row or past 2^30");
+  if (out_ld % (dtype == SD_BF16 ? 8 : 4) ||
+      (((uintptr_t)x | (uintptr_t)w | (uintptr_t)down | (uintptr_t)up | (uintptr_t)out | (uintptr_t)bias) & 15))
+    return op_fail(SD_ERR_INVALID_ARG, "buffers and rows of out must be 16-byte aligned");
+  if (((uintptr_t)scale | (uintptr_t)index) & 3) return op_fail(SD_ERR_INVALID_ARG, "an array is not aligned to its element");
+  if (out == x || out == w || out == down || out == up) return op_fail(SD_ERR_INVALID_ARG, "out overlaps an input");
+  if (!scratch || scratch_floats < linear_adapters_scratch_floats(M, rank))
+    return op_fail(SD_ERR_WORKSPACE, "scratch is too small");
+  if ((uintptr_t)scratch & 15) return op_fail(SD_ERR_INVALID_ARG, "scratch must be 16-byte aligned");
+  LinearAdaptersArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = x; a.w = w; a.down = down; a.up = up; a.scale = scale; a.index = index; a.bias = bias;
+  a.out = out; a.out_ld = out_ld; a.M = M; a.K = K; a.N = N; a.rank = rank; a.count = count; a.group = group;
+  a.scratch = scratch;
+  return op_hip(launch_linear_adapters((DType)dtype, a, (hipStream_t)stream), "linear_adapters");
+}
+
 }  // extern "C"

@@ -418,3 +418,57 @@ def text_attention(q, k, v, max_len, start=None, length=None, mask=None, causal=
               _at(mask), 1 if causal else 0, prefix_p, cap or 0.0, _at(bias), reach, _at(slope), heads, kv_heads, d,
               d ** -0.5 if scale is None else scale, 1 if fresh else 0))
     return out
+
+
+def linear_adapters(x, w, down, up, index, scale=None, bias=None, out=None):
+    """x [..., K] (fp32 or bf16, contiguous) times w [N, K], plus a low-rank
+    adapter of each row's own: + scale[c] up[c] (down[c] x), with down [count,
+    rank, K] and up [count, N, rank] in x's type.  index int32, c of every row
+    (shape x.shape[:-1]) or of every x[i] (shape x.shape[:1]); outside [0,
+    count): none.  scale fp32 [count] (default 1), bias fp32 [N].  K, N and
+    rank are multiples of 8 (narrower adapters padded with zeros).  Returns
+    [..., N] in x's type, out when given (a matrix out may have rows further apart)."""
+    dt = x.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise TypeError(dt)
+    shape = x.shape
+    if len(shape) < 2 or w.dim() != 2 or down.dim() != 3 or up.dim() != 3:
+        _bad("x [..., K], w [N, K], down [count, rank, K], up [count, N, rank]")
+    K, N = shape[-1], w.shape[0]
+    count, rank = down.shape[:2]
+    if w.dtype is not dt or down.dtype is not dt or up.dtype is not dt:
+        _bad("w, down and up must have x's type")
+    if w.shape[1] != K or down.shape[2] != K or up.shape != (count, N, rank):
+        _bad("w, down and up must be [N, K], [count, rank, K] and [count, N, rank]")
+    if not (x.is_contiguous() and w.is_contiguous() and down.is_contiguous() and up.is_contiguous()):
+        _bad("x, w, down and up must be contiguous")
+    if K == 0:
+        _bad("K must be above 0")
+    M = x.numel() // K
+    _int32(max(M, K, N, count, rank))
+    if index.dtype is not torch.int32 or not index.is_contiguous():
+        _bad("index must be int32, contiguous")
+    if index.shape == shape[:-1]:
+        group = 1
+    elif index.shape == shape[:1]:
+        group = max(M // shape[0], 1) if shape[0] else 1
+    else:
+        _bad("index must have one entry per row of x, or per x[i]")
+    if scale is not None and (scale.dtype is not torch.float32 or scale.shape != (count,) or not scale.is_contiguous()):
+        _bad("scale must be fp32 [count]")
+    if bias is not None and (bias.dtype is not torch.float32 or bias.shape != (N,) or not bias.is_contiguous()):
+        _bad("bias must be fp32 [N]")
+    if out is None:
+        out, out_ld = x.new_empty(shape[:-1] + (N,)), N
+    else:
+        if out.shape != shape[:-1] + (N,) or out.dtype is not dt:
+            _bad("out has another shape or type than the result")
+        out_ld = _row_stride(out, "out")
+    L = lib()
+    floats = M * rank
+    scratch = x.new_empty(floats, dtype=torch.float32)
+    _enqueue(L.synerdiff_op_linear_adapters, x, (w, down, up, index, scale, bias, out),
+             (_TYPE[dt], x.data_ptr(), M, K, w.data_ptr(), N, down.data_ptr() if count else None,
+              up.data_ptr() if count else None, rank, count, _at(scale), index.data_ptr(), group, _at(bias), out.data_ptr(),
+              out_ld, scratch.data_ptr(), floats))
+    return out

@@ -1,0 +1,180 @@
+"""Linear layers with a low-rank adapter per row (linear_adapters) on the GPU
+against the oracle's float64 definition.  Tolerances count roundings."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import text as O
+from tests.test_gpu_text_ops import NAN, U16, U32, _close, _gen, _np, _t, ops  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+def _case(seed, dt, M, K, N, rank, count):
+    g = _gen(seed)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    x, w = r(M, K).to(_t(dt)), (r(N, K) / math.sqrt(K)).to(_t(dt))
+    down, up = (r(count, rank, K) / math.sqrt(K)).to(_t(dt)), r(count, N, rank).to(_t(dt))
+    return x, w, down, up, 0.5 + torch.rand(count, generator=g, device="cuda"), r(N)
+
+
+def _order(kind, M, count, seed):
+    """Index of every row."""
+    rng = np.random.default_rng(seed)
+    if kind == "runs":  # runs of uneven length, some rows without an adapter
+        out = []
+        while len(out) < M:
+            out += [int(rng.integers(-1, count))] * int(rng.integers(1, 90))
+        return np.asarray(out[:M], np.int32)
+    if kind == "mixed":  # every row its own, and indices outside the adapters
+        return rng.integers(-3, count + 3, M).astype(np.int32)
+    return np.full(M, {"none": -1, "one": count - 1}[kind], np.int32)
+
+
+def _check(got, x, w, down, up, index, scale, bias, dt, what):
+    K, rank = x.shape[-1], down.shape[1]
+    y, s, t = O.linear_adapters(_np(x).reshape(-1, K), _np(w), _np(down), _np(up), index, None if scale is None else _np(scale),
+                                None if bias is None else _np(bias))
+    # Sums of K (and of K, then rank, products): below K, K + rank roundings of the
+    # terms' sizes; scale and the parts of v (2^-16) three more; the result's own.
+    tol = (K + 12) * U32 * s + ((K + rank + 12) * U32 + 2.0 ** -16) * t
+    tol = tol + (U16 if dt == "bf16" else U32) * (np.abs(y) + tol)
+    _close(_np(got).reshape(y.shape), y, tol + 1e-37, what)
+
+
+SHAPES = [
+    # M, K, N, rank, count
+    (1, 8, 8, 8, 1),
+    (1, 320, 1280, 16, 4),
+    (7, 1280, 24, 8, 3),
+    (17, 72, 168, 24, 40),
+    (33, 200, 320, 40, 9),
+    (64, 768, 72, 128, 70),
+    (65, 64, 64, 8, 2),
+    (100, 8, 320, 16, 5),
+    (130, 320, 40, 136, 3),
+    (200, 328, 648, 32, 7),
+    (257, 1000, 328, 64, 4),
+    (700, 640, 1288, 16, 6),
+]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N,rank,count", SHAPES)
+def test_linear_adapters(ops, M, K, N, rank, count, dt):  # noqa: F811
+    x, w, down, up, scale, bias = _case(M + K + N, dt, M, K, N, rank, count)
+    for at, kind in enumerate(("runs", "mixed", "none", "one")):
+        index = _order(kind, M, count, M + at)
+        sc, b = (scale, bias) if at % 2 == 0 else (None, None)
+        got = ops.linear_adapters(x, w, down, up, torch.from_numpy(index).cuda(), scale=sc, bias=b)
+        _check(got, x, w, down, up, index, sc, b, dt, f"{(M, K, N, rank, count, kind, dt)}")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N,rank", [(16384, 64, 320, 8), (20000, 320, 64, 16), (40000, 72, 136, 24), (3000, 256, 640, 32),
+                                        (9000, 640, 256, 64)])
+def test_linear_adapters_many_rows(ops, M, K, N, rank, dt):  # noqa: F811
+    """All tiles of the product: a sample of rows, and the first and last ones, are checked."""
+    x, w, down, up, scale, bias = _case(M, dt, M, K, N, rank, 5)
+    index = _order("runs", M, 5, M)
+    got = ops.linear_adapters(x, w, down, up, torch.from_numpy(index).cuda(), scale=scale, bias=bias)
+    rows = np.unique(np.concatenate((np.arange(40), np.arange(M - 300, M), np.random.default_rng(1).integers(0, M, 400))))
+    at = torch.from_numpy(rows).cuda()
+    _check(got[at], x[at], w, down, up, index[rows], scale, bias, dt, f"{(M, K, N, rank, dt)}")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,t,K,N", [(3, 1, 64, 64), (5, 3, 40, 72), (6, 77, 128, 320), (3, 300, 320, 64)])
+def test_linear_adapters_index_per_request(ops, n, t, K, N, dt):  # noqa: F811
+    x, w, down, up, scale, bias = _case(n * t, dt, n * t, K, N, 16, 3)
+    index = np.asarray([(2 * i) % 4 - (i == 1) for i in range(n)], np.int32)
+    x3 = x.view(n, t, K)
+    got = ops.linear_adapters(x3, w, down, up, torch.from_numpy(index).cuda(), scale=scale, bias=bias)
+    assert got.shape == (n, t, N)
+    _check(got, x, w, down, up, np.repeat(index, t), scale, bias, dt, f"{(n, t, K, N, dt)}")
+    rows = torch.from_numpy(np.repeat(index, t)).cuda()
+    assert torch.equal(ops.linear_adapters(x3, w, down, up, rows.view(n, t), scale=scale, bias=bias), got)
+    assert torch.equal(ops.linear_adapters(x, w, down, up, rows, scale=scale, bias=bias), got.view(n * t, N))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [5, 40, 300])
+def test_linear_adapters_other_rows_and_adapters_do_not_matter(ops, M, dt):  # noqa: F811
+    """Infinities and NaN in another row or another row's adapter stay there."""
+    K, N, rank, count = 136, 200, 24, 4
+    x, w, down, up, scale, bias = _case(M, dt, M, K, N, rank, count)
+    index = np.arange(M, dtype=np.int32) % 5 - 1
+    ix = torch.from_numpy(index).cuda()
+    clean = ops.linear_adapters(x, w, down, up, ix, scale=scale, bias=bias)
+    for bad in (math.inf, NAN):
+        d2, u2, s2, x2 = down.clone(), up.clone(), scale.clone(), x.clone()
+        d2[2], u2[2], s2[2] = bad, -bad, bad
+        x2[1] = bad
+        got = ops.linear_adapters(x2, w, d2, u2, ix, scale=s2, bias=bias)
+        keep = torch.from_numpy((index != 2) & (np.arange(M) != 1)).cuda()
+        assert torch.equal(got[keep], clean[keep])
+        assert not torch.isfinite(got[~keep]).any()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [1, 30, 200])
+def test_linear_adapters_out_and_empty(ops, M, dt):  # noqa: F811
+    K, N = 64, 72
+    x, w, down, up, scale, bias = _case(M, dt, M, K, N, 8, 2)
+    ix = torch.zeros(M, dtype=torch.int32, device="cuda")
+    ref = ops.linear_adapters(x, w, down, up, ix)
+    wide = torch.full((M, N + 24), 7.0, device="cuda", dtype=_t(dt))
+    ops.linear_adapters(x, w, down, up, ix, out=wide[:, 8:8 + N])
+    assert torch.equal(wide[:, 8:8 + N], ref) and (wide[:, :8] == 7).all() and (wide[:, 8 + N:] == 7).all()
+    assert torch.equal(ops.linear_adapters(x, w, down, up, ix), ref)
+    assert ops.linear_adapters(x[:0], w, down, up, ix[:0]).shape == (0, N)
+    assert ops.linear_adapters(x, w[:0], down, up[:, :0], ix).shape == (M, 0)
+    bare = ops.linear_adapters(x, w, down[:0], up[:0], ix)
+    assert torch.equal(bare, ops.linear_adapters(x, w, down, up, ix - 1))
+
+
+@pytest.mark.parametrize("dt", ["bf16"])
+def test_linear_adapters_past_2_31_elements(ops, dt):  # noqa: F811
+    """x and out past 2^31 elements: the product runs in parts, rows at their seams are checked."""
+    K, N, M = 1024, 1032, (1 << 21) + 300
+    g = _gen(3)
+    x = torch.empty(M, K, device="cuda", dtype=_t(dt))
+    rows = np.unique(np.concatenate([np.arange(a - 3, a + 3) for a in (3, 1048320, 1 << 20, 2096640, 1 << 21, M - 3)]))
+    at = torch.from_numpy(rows).cuda()
+    x.zero_()
+    x[at] = torch.randn(len(rows), K, generator=g, device="cuda").to(_t(dt))
+    _, w, down, up, scale, bias = _case(4, dt, 1, K, N, 8, 3)
+    index = (torch.arange(M, device="cuda") // 100 % 4 - 1).to(torch.int32)
+    got = ops.linear_adapters(x, w, down, up, index, scale=scale, bias=bias)
+    _check(got[at], x[at], w, down, up, index[at].cpu().numpy(), scale, bias, dt, "parts")
+
+
+def test_linear_adapters_streams_and_graphs(ops):  # noqa: F811
+    for M in (20, 500):
+        x, w, down, up, scale, bias = _case(M, "bf16", M, 192, 320, 16, 4)
+        ix = torch.from_numpy(_order("runs", M, 4, 1)).cuda()
+        ix2 = torch.from_numpy(_order("mixed", M, 4, 2)).cuda()
+        x1, x2, i1 = x.clone(), x.flip(0).contiguous(), ix.clone()
+        want = {0: ops.linear_adapters(x1, w, down, up, i1, scale=scale), 1: ops.linear_adapters(x2, w, down, up, ix2, scale=scale)}
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            got = ops.linear_adapters(x, w, down, up, ix, scale=scale)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got, want[0])
+        graphs = []
+        for _ in range(2):  # (two graphs, each with a workspace of its own)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                out = ops.linear_adapters(x, w, down, up, ix, scale=scale)
+            graphs.append((graph, out))
+        for turn in range(6):
+            x.copy_((x1, x2)[turn % 2])
+            ix.copy_((i1, ix2)[turn % 2])
+            for graph, out in graphs:
+                graph.replay()
+                assert torch.equal(out, want[turn % 2])
+            assert torch.equal(ops.linear_adapters(x, w, down, up, ix, scale=scale), want[turn % 2])
+            torch.cuda.synchronize()
