@@ -96,16 +96,40 @@ __device__ __forceinline__ void zero_rest(const TextArgs& a, const Place& p) {
   if (p.c == a.n - 1) span(max((long)a.start[a.n], 0L), a.tokens);
 }
 
-// bias(j - i) at distance `far` in log2 units, over `unit`.  Finite values stay
-// finite: up to 2^126 of either unit, past any score, and sums of two do not pass fp32.
-__device__ __forceinline__ float bias_at(const TextArgs& a, int h, int far, float unit) {
-  float v = 0.f;
-  if (a.bias) v = a.bias[(long)h * (2 * a.reach + 1) + min(max(far, -a.reach), a.reach) + a.reach];
-  if (a.slope) v = fmaf(-a.slope[h], fabsf((float)far), v);
+// bias(j - i) at distance `far` in log2 units, over `unit`, from what the table holds
+// there.  Finite values stay finite: up to 2^126 of either unit, past any score, and
+// sums of two do not pass fp32.
+__device__ __forceinline__ float table_at(const TextArgs& a, int h, int far) {
+  return a.bias ? a.bias[(long)h * (2 * a.reach + 1) + min(max(far, -a.reach), a.reach) + a.reach] : 0.f;
+}
+__device__ __forceinline__ float term_of(float v, int far, float slope, float unit) {
+  v = fmaf(-slope, fabsf((float)far), v);
   const float lim = 0x1p125f * fminf(unit, 1.f);
   if (v < -lim && v != -INFINITY) v = -lim;
   if (v > lim && v != INFINITY) v = lim;
   return v * LOG2E / unit;
+}
+
+// 16 bytes a lane from `base` + off straight to LDS, 1 KB from `to` on (uniform).  In
+// asm, so that the compiler does not know of it: it cannot tell which LDS reads the
+// load concerns and waited for it at the next one, a tile too early.  Whoever reads
+// waits (vmcnt 0, then a barrier); no register is written.  (The five wait states are
+// those between a vector instruction that wrote a resource word and its use here.)
+typedef int rsrc4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ rsrc4 resource(const void* base, long bytes) {
+  const uint64_t b = (uint64_t)base;
+  rsrc4 r;
+  r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)b);
+  r[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32) & 0xFFFF);
+  r[2] = __builtin_amdgcn_readfirstlane((int)bytes);
+  r[3] = 0x00020000;
+  return r;
+}
+__device__ __forceinline__ void to_lds16(rsrc4 r, bf16* to, int off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int m = __builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) bf16*)to);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m), "v"(off), "s"(r) : "memory");
+#endif
 }
 
 __device__ __forceinline__ bool odd8(uint4 v) {  // an infinity or NaN among eight bf16
@@ -117,17 +141,38 @@ __device__ __forceinline__ bool odd_f(float v) { return !(fabsf(v) < INFINITY); 
 }  // namespace
 
 // ------------------------------------------------------------------ bf16
+// Slots of a key's CH 16-byte chunks in LDS, where the loads put them next to each
+// other without gaps: chunk c of key r lies in slot c ^ k_swz(r) (K, whose fragment
+// reads take 16 keys at one chunk) or c ^ v_swz(r) (V, whose transposing reads take
+// 4 keys at four chunks), so that either set is spread over all 16 columns of 16
+// bytes.  (32 chunks: over 8, so that rows 8 apart are turned alike.)
+__host__ __device__ constexpr int k_low(int ch) { return (ch == 32 ? 8 : ch % 16 == 0 ? 16 : ch % 8 == 0 ? 8 : ch % 4 == 0 ? 4 : 2) - 1; }
+__host__ __device__ constexpr int v_low(int ch) { return (ch % 16 == 0 ? 16 : ch % 8 == 0 ? 8 : 1) - 1; }
+template <int CH>
+__device__ __forceinline__ int k_swz(int r) {
+  constexpr int L = k_low(CH);
+  return (CH == 32 || L == 15 ? r : L == 7 ? r >> 1 : L == 3 ? r >> 2 : r >> 3) & L;
+}
+template <int CH>
+__device__ __forceinline__ int v_swz(int r) {
+  constexpr int L = v_low(CH);
+  return L == 15 ? 4 * (r & 3) : L == 7 ? 2 * (r & 2) : 0;
+}
+
 // D16: head width rounded up to a width the kernel is built for.  BIAS: there is
-// a term by distance.  CAP: scores are capped.
+// a term by distance.  CAP: scores are capped.  Tiles of 64 keys go from memory
+// straight to LDS.  While a tile's probabilities are formed, the next tile's scores
+// are multiplied: the two do not depend on each other, and the matrix unit would
+// wait for the vector ALU otherwise.
 template <int D16, bool BIAS, bool CAP>
 __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_bf16_kernel(TextArgs a) {
-  constexpr int NW = 4, KT = 64, NJ = D16 / 16, ND = (D16 + 31) / 32, NT = 64 * NW, LDK = D16 + 8, LDV = v_row(D16);
-  // A tile is moved by passes of NT / LPR keys, LPR lanes (a power of two) a key
-  constexpr int LPR = D16 <= 32 ? 4 : D16 <= 64 ? 8 : D16 <= 128 ? 16 : 32, RPP = NT / LPR < KT ? NT / LPR : KT, CPT = KT / RPP;
-  __shared__ __attribute__((aligned(16))) bf16 Ks[2][KT * LDK];
-  __shared__ __attribute__((aligned(16))) bf16 Vs[2][KT * LDV + 32];  // (the last rows are read past their end where D16 % 32)
+  constexpr int NW = 4, KT = 64, NJ = D16 / 16, ND = (D16 + 31) / 32, CH = D16 / 8, NI = (CH + NW - 1) / NW, LDR = D16 + 8;
+  constexpr int TILE = KT * D16;
+  static_assert(NW * 32 * LDR <= 4 * TILE, "the result's rows take the place of the tiles");
+  // K, K, V, V (the last rows of V are read past their end where D16 % 32)
+  __shared__ __attribute__((aligned(1024))) bf16 smem[4 * TILE + 64];
   __shared__ float strip[BIAS ? 2 : 1][BIAS ? KT + TQ : 1];
-  __shared__ int odd[3];  // tile i: an infinity or NaN in V where the border passes (slot i % 3)
+  __shared__ int odd[2];  // tile t: an infinity or NaN in V where the border passes (slot t % 2)
   const Place p = place_of(a);
   if (!p.on) return;
   if (a.zero && a.start) zero_rest<bf16>(a, p);
@@ -140,14 +185,18 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
   int k_end = b0 < tx.len ? tx.len : 0;
   if (a.causal) k_end = min(k_end, max(b0 + TQ, tx.prefix));
   const int lim = a.causal ? max(r0 + lq + 1, tx.prefix) : tx.len;               // keys that this lane's query sees
-  const int lim_lo = a.causal ? max(r0 + 1, tx.prefix) : tx.len, lim_hi = a.causal ? max(r0 + 32, tx.prefix) : tx.len;
+  const int lim_lo = a.causal ? max(r0 + 1, tx.prefix) : tx.len;                 // ... that all of the wave's see
+  const int lim_hi = r0 >= tx.len ? 0 : a.causal ? max(r0 + 32, tx.prefix) : tx.len;  // ... that any does
+  const int border = a.causal ? max(b0 + 1, tx.prefix) : 0x7FFFFFFF;             // ... that all of the block's see
   const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
   // (a scale of 0 or below: uniform scores, or -q, under a positive one)
   const float mag = a.scale == 0.f ? 1.f : fabsf(a.scale), sl2 = mag * LOG2E;
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
   // cap tanh(x / cap) = cap - 2 cap / (1 + exp(2 x / cap)), in log2 units
   const float c_in = CAP ? 2.f * sl2 / a.cap : 0.f, c_out = CAP ? a.cap * LOG2E : 0.f;
-
+  auto capped = [&](float x, float add) __attribute__((always_inline)) {  // (add: c_out and what else is added)
+    return fmaf(-2.f * c_out, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * c_in)), add);
+  };
   // Q^T fragments (B operand): query r0 + lq, channels 16 j + 8 lh + [0, 8)
   bf16x8 qf[NJ];
   {
@@ -170,165 +219,91 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
-  if (tid < 3) odd[tid] = 0;
-  __syncthreads();
+  if (tid < 2) odd[tid] = 0;
 
-  // A thread's pieces of a tile: keys pk + RPP i, channels pc on.  (Offsets past a
-  // resource's end, as those of channels from d on and of keys that take no part, read as zero.)
-  const int pk = tid / LPR, pc = tid % LPR * 8;
-  const bool mine = pk < RPP && pc < D16;  // (fewer than NT threads where LPR is wide or the tile short)
-  const int ko = pc < d ? (pk * (int)a.k_ld + pc) * 2 : OOB, vo = pc < d ? (pk * (int)a.v_ld + pc) * 2 : OOB;
+  // Load i of this wave moves chunks 64 (wave + NW i) + lane of a tile: key, and
+  // byte offsets in K and V.  (Offsets past a resource's end, as those of channels
+  // from d on and of keys that take no part, write zeros.)
   const bf16* K = (const bf16*)a.k + tx.k0 + p.g * a.k_head;
   const bf16* V = (const bf16*)a.v + tx.v0 + p.g * a.v_head;
-  bf16x8 rk[CPT], rv[CPT];
-  float rb = 0.f;
-  auto fetch = [&](int k0, uint64_t bits) __attribute__((always_inline)) {
+  // Where CH is a power of two, load i has load 0's slots, 256 / CH keys on.
+  constexpr bool EVEN = 256 % CH == 0;
+  constexpr int NO = EVEN ? 1 : NI, STEP = 256 / CH;
+  int lkey[NO], ko[NO], vo[NO];
+#pragma unroll
+  for (int i = 0; i < NO; ++i) {
+    const int q = 64 * (wave + NW * i) + lane, r = q / CH, slot = q - r * CH, kc = (slot ^ k_swz<CH>(r)) * 8, vc = (slot ^ v_swz<CH>(r)) * 8;
+    lkey[i] = r & 63;  // (past the tile where NW does not divide CH: not issued)
+    ko[i] = kc < d ? (r * (int)a.k_ld + kc) * 2 : OOB;
+    vo[i] = vc < d ? (r * (int)a.v_ld + vc) * 2 : OOB;
+  }
+  auto load = [&](const bf16* base, long ld, const int (&off)[NO], bf16* to, int k0, uint64_t bits) __attribute__((always_inline)) {
     const int n = min(KT, k_end - k0);
-    const __amdgpu_buffer_rsrc_t kr = make_rsrc(K + (long)k0 * a.k_ld, ((n - 1) * (long)a.k_ld + d) * 2);
-    const __amdgpu_buffer_rsrc_t vr = make_rsrc(V + (long)k0 * a.v_ld, ((n - 1) * (long)a.v_ld + d) * 2);
-    const uint64_t b = bits >> (pk & 63);
+    const rsrc4 res = resource(base + (long)k0 * ld, ((n - 1) * ld + d) * 2);
+    const bool all = !~bits;
+    const uint64_t mine = EVEN ? bits >> lkey[0] : 0;
 #pragma unroll
-    for (int i = 0; i < CPT; ++i) {
-      const bool on = (b >> (RPP * i & 63)) & 1;
-      rk[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(kr, on ? ko + i * RPP * (int)a.k_ld * 2 : OOB, 0, 0));
-      rv[i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(vr, on ? vo + i * RPP * (int)a.v_ld * 2 : OOB, 0, 0));
-    }
-    // strip[e]: distance k0 - b0 + e - (TQ - 1)
-    if constexpr (BIAS)
-      if (tid < KT + TQ - 1) rb = bias_at(a, p.h, k0 - b0 + tid - (TQ - 1), CAP ? 1.f : sl2);
-  };
-  auto stage = [&](int b, int k0, int slot) __attribute__((always_inline)) {
-    // (a key's V reaches every query of the tile, with a weight of 0 behind the
-    // border: 0 times an infinity or NaN is NaN, so those are taken out here and added where they are seen)
-    const bool border = a.causal && k0 + KT > max(b0 + 1, tx.prefix);
-    if (mine)
-#pragma unroll
-      for (int i = 0; i < CPT; ++i) {
-        *(bf16x8*)&Ks[b][(pk + RPP * i) * LDK + pc] = rk[i];
-        bf16x8 v = rv[i];
-        if (border && odd8(__builtin_bit_cast(uint4, v))) {
-          odd[slot] = 1;
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (odd_f((float)v[e])) v[e] = (bf16)0.f;
-        }
-        *(bf16x8*)&Vs[b][(pk + RPP * i) * LDV + pc] = v;
+    for (int i = 0; i < NI; ++i)
+      if (CH % NW == 0 || wave + NW * i < CH) {
+        int at = EVEN ? off[0] + i * STEP * (int)ld * 2 : off[EVEN ? 0 : i];
+        if (EVEN && off[0] < 0) at = OOB;
+        if (!all && !((EVEN ? mine >> (STEP * i & 63) : bits >> lkey[EVEN ? 0 : i]) & 1)) at = OOB;
+        to_lds16(res, to + 512 * (wave + NW * i), at);
       }
-    if constexpr (BIAS)
-      if (tid < KT + TQ - 1) strip[b][tid] = rb;
   };
-  // which of the 64 keys from k0 on take part: lane's own, as loaded; then a bit per key
-  auto own_key = [&](int k0) -> bool {
-    const int k = k0 + lane;
-    return k < k_end && (!mask || mask[k]);
+  // strip[e] of the tile at k0: the term at distance k0 - b0 + e - (TQ - 1), loaded and then made
+  const float slope = BIAS && a.slope ? a.slope[p.h] : 0.f;
+  auto far_of = [&](int k0) { return k0 - b0 + min(tid, KT + TQ - 2) - (TQ - 1); };
+  auto strip_set = [&](int b, int k0, float v) __attribute__((always_inline)) {
+    if (tid < KT + TQ - 1) strip[BIAS ? b : 0][BIAS ? tid : 0] = term_of(v, far_of(k0), slope, CAP ? 1.f : sl2);
   };
+  // which of the 64 keys from k0 on take part: lane's own mask byte, as loaded; then a bit per key
+  const __amdgpu_buffer_rsrc_t mr = make_rsrc(mask, k_end);
+  auto own_mask = [&](int k0) -> int {
+    return mask ? (int)__builtin_amdgcn_raw_buffer_load_b8(mr, k0 + lane, 0, 0) : 1;
+  };
+  auto ballot = [&](int k0, int own) -> uint64_t { return __ballot(k0 + lane < k_end && own); };
 
+  // K fragment of slice j: chunk 2 j + lh of key lq, V fragment t: keys 4 lh + (lane % 16) / 4
+  // and 8 on, channels 32 t + (lane & 16) on.  A slot is the chunk's number with
+  // some of its low bits turned, so both addresses are one xor and a constant away.
+  constexpr int KL = k_low(CH), VL = v_low(CH);
+  const int k_at = lq * D16 + (lh ^ k_swz<CH>(lq)) * 8;
+  const int v_row = 4 * lh + ((lane & 15) >> 2);
+  const int v_at = v_row * D16 + ((((lane & 16) >> 3) + ((lane & 3) >> 1)) ^ v_swz<CH>(v_row)) * 8 + 4 * (lane & 1);
+  auto k_frag = [&](const bf16* Kb, int kt, int j) __attribute__((always_inline)) {
+    return *(const bf16x8*)(Kb + (k_at ^ ((2 * j & KL) * 8)) + (2 * j & ~KL) * 8 + kt * 32 * D16);
+  };
+  auto v_frag = [&](const bf16* Vb, int u, int t) __attribute__((always_inline)) {
+    const bf16* at = Vb + (v_at ^ ((4 * t & VL) * 8)) + (4 * t & ~VL) * 8 + 16 * u * D16;
+    const bf16x4 lo = read_transposed(at), hi = read_transposed(at + 8 * D16);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
   bf16x8 ones = {};  // B operand of the masks: ones for k = 0
   if (lh == 0) ones[0] = (bf16)1.0f;
   const int sb = TQ - 1 - wave * 32 - lq + 4 * lh;  // strip's element at key 4 lh for this lane's query
 
-  // NKT: 32-key halves of the tile that hold keys at all.
-  auto tile = [&](auto nkt, int b, uint64_t bits, int k0) __attribute__((always_inline)) {
-    constexpr int NKT = decltype(nkt)::value;
-    const bf16 *Kb = Ks[b], *Vb = Vs[b];
-    f32x16 s[NKT];
-    // register r of half kt: key 32 kt + 8 (r / 4) + 4 lh + r % 4
+  // Register r of half kt of a tile's scores: key 32 kt + 8 (r / 4) + 4 lh + r % 4.
+  // What they start from: the term by distance, and -inf for keys that take no part
+  // (one product of a column of 0 or -inf per key with a row of ones).
+  auto start = [&](f32x16 (&s)[2], int b, uint64_t bits) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kt = 0; kt < NKT; ++kt) {
-      f32x16 start = {};
-      if constexpr (BIAS && !CAP)
+    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) start[r] = strip[b][sb + 32 * kt + 8 * (r >> 2) + (r & 3)];
-      if constexpr (!CAP)
-        if ((uint32_t)(bits >> (32 * kt)) != ~0u) {
-          // Keys that take no part start from -inf: one product of a column of 0
-          // or -inf per key with a row of ones.
-          bf16x8 off = {};
-          if (lh == 0) off[0] = __builtin_bit_cast(bf16, (unsigned short)(bits >> (32 * kt + lq) & 1 ? 0 : 0xFF80));
-          start = mfma32(off, ones, start);
-        }
+      for (int r = 0; r < 16; ++r) s[kt][r] = BIAS && !CAP ? strip[b][sb + 32 * kt + 8 * (r >> 2) + (r & 3)] : 0.f;
+    if (!CAP && ~bits)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const bf16x8 kf = *(const bf16x8*)&Kb[(kt * 32 + lq) * LDK + 16 * j + 8 * lh];
-        s[kt] = mfma32(kf, qf[j], j ? s[kt] : start);
+      for (int kt = 0; kt < 2; ++kt) {
+        bf16x8 off = {};
+        if (lh == 0) off[0] = __builtin_bit_cast(bf16, (unsigned short)(bits >> (32 * kt + lq) & 1 ? 0 : 0xFF80));
+        s[kt] = mfma32(off, ones, s[kt]);
       }
-    }
-    if constexpr (CAP) {
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float t = __builtin_amdgcn_exp2f(s[kt][r] * c_in);
-          float z = fmaf(-2.f * c_out, __builtin_amdgcn_rcpf(1.f + t), c_out);
-          if constexpr (BIAS) z += strip[b][sb + 32 * kt + 8 * (r >> 2) + (r & 3)];
-          s[kt][r] = z;
-        }
-    }
-    // the causal border, and for capped scores the keys that take no part
-    if (k0 + KT > lim_lo || (CAP && ~bits)) {
-      const int left = lim - k0 - 4 * lh;
-      const uint64_t w = bits >> (4 * lh);
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int c = 32 * kt + 8 * (r >> 2) + (r & 3);
-          if (c >= left || (CAP && !(w >> c & 1))) s[kt][r] = -INFINITY;
-        }
-    }
-    float v = s[0][0];
-#pragma unroll
-    for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) v = fmaxf(v, s[kt][r]);
-    const float2 h = half_swap(v);
-    const float mt = fmaxf(h.x, h.y) * (CAP ? 1.f : sl2);
-    const bool need = mt > m_run + TAU;
-    if (__any(need)) {  // (where a row's maximum stays, its sums are multiplied by one)
-      const float al = need ? __builtin_amdgcn_exp2f(m_run - mt) : 1.0f;
-      m_run = need ? mt : m_run;
-      l_run *= al;
-#pragma unroll
-      for (int t = 0; t < ND; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[t][r] *= al;
-    }
-    const float ref = exp_ref(m_run);
-    // (the exponent is s sl2 - ref in one rounding; past 2^20 the one that ref
-    // holds of its own product would no longer be a small part of a step)
-    float mul = CAP ? 1.f : sl2;
-    if (!CAP && __any(fabsf(ref) > 0x1p20f)) {
-      mul = 1.f;
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[kt][r] *= sl2;
-    }
-    // O^T += V^T P^T, 16 keys at a time: slot (lh, i) of slice u is key 16 u +
-    // 8 (i / 4) + 4 lh + i % 4, register 8 (u % 2) + i of half u / 2.  The
-    // probabilities are rounded to bf16 (by up to 2^-8 of each, half a step) and
-    // summed as rounded, so that the rounding cancels where one key prevails.
-#pragma unroll
-    for (int u = 0; u < 2 * NKT; ++u) {
-      bf16x8 vf[ND];
-#pragma unroll
-      for (int t = 0; t < ND; ++t) {
-        const bf16* at = &Vb[(16 * u + 4 * lh + ((lane & 15) >> 2)) * LDV + t * 32 + (lane & 16) + 4 * (lane & 3)];
-        const bf16x4 lo = read_transposed(at), hi = read_transposed(at + 8 * LDV);
-        vf[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-      bf16x8 pf;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = s[u >> 1][8 * (u & 1) + i];
-        pf[i] = (bf16)__builtin_amdgcn_exp2f(CAP ? x - ref : fmaf(x, mul, -ref));
-      }
-      l_run = sum_probs(pf, l_run);
-#pragma unroll
-      for (int t = 0; t < ND; ++t) o[t] = mfma32(vf[t], pf, o[t]);
-    }
   };
-  // What `stage` took out of V, added for the queries that see it (a weight above 0 times it is itself).
+  // O^T += V^T P^T, 16 keys at a time: slot (lh, i) of slice u is key 16 u +
+  // 8 (i / 4) + 4 lh + i % 4, register 8 (u % 2) + i of half u / 2.  The
+  // probabilities are rounded to bf16 (by up to 2^-8 of each, half a step) and
+  // summed as rounded, so that the rounding cancels where one key prevails.
+  // What was taken out of V, added for the queries that see it (a weight above 0 times it is itself).
   auto add_odd = [&](uint64_t bits, int k0) __attribute__((always_inline)) {
 #pragma unroll 1
     for (int j = 0; j < KT; ++j) {
@@ -348,41 +323,170 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
   };
 
   if (k_end > 0) {
-    uint64_t bits = __ballot(own_key(0));
-    fetch(0, bits);
-    bool nk = own_key(KT);
-    stage(0, 0, 0);
-    __syncthreads();
-    for (int k0 = 0, b = 0, slot = 0; k0 < k_end; k0 += KT, b ^= 1) {
-      uint64_t next = 0;
-      const bool more = k0 + KT < k_end;
-      if (more) {
-        next = __ballot(nk);
-        fetch(k0 + KT, next);
-        nk = own_key(k0 + 2 * KT);
+    int own = own_mask(0);
+    float f = BIAS ? table_at(a, p.h, far_of(0)) : 0.f;
+    uint64_t bits = ballot(0, own);
+    own = own_mask(KT);
+    load(K, a.k_ld, ko, smem, 0, bits);
+    load(V, a.v_ld, vo, smem + 2 * TILE, 0, bits);
+    if constexpr (BIAS) strip_set(0, 0, f);
+    wait_vmcnt<0>();
+    wait_lgkm0();
+    stage_barrier();
+    for (int k0 = 0, t = 0; k0 < k_end; k0 += KT, t ^= 1) {
+      const uint64_t next = ballot(k0 + KT, own);
+      if (k0 + KT < k_end) {  // (what the registers get is waited for at the end of the tile, with the rest)
+        if (BIAS) f = table_at(a, p.h, far_of(k0 + KT));
+        own = own_mask(k0 + 2 * KT);
+        load(K, a.k_ld, ko, smem + (t ^ 1) * TILE, k0 + KT, next);
+        load(V, a.v_ld, vo, smem + (2 + (t ^ 1)) * TILE, k0 + KT, next);
       }
-      const int s1 = slot == 2 ? 0 : slot + 1;
-      if (bits && k0 < lim_hi && r0 < tx.len) {
-        if (bits >> 32 && k0 + 32 < lim_hi)
-          tile(std::integral_constant<int, 2>{}, b, bits, k0);
-        else if ((uint32_t)bits)
-          tile(std::integral_constant<int, 1>{}, b, bits, k0);
-        if (a.causal && odd[slot]) add_odd(bits, k0);
+      const bf16* Kb = smem + t * TILE;
+      bf16* Vb = smem + (2 + t) * TILE;
+      const bool at_border = k0 + KT > border;
+      if (at_border) {
+        // (a key's V reaches every query of the tile, with a weight of 0 behind the
+        // border: 0 times an infinity or NaN is NaN, so those are taken out here and added where they are seen)
+        bool any = false;
+        for (int q = tid; q < KT * CH; q += 64 * NW) {
+          bf16x8 v = *(const bf16x8*)&Vb[8 * q];
+          if (odd8(__builtin_bit_cast(uint4, v))) {
+            any = true;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (odd_f((float)v[e])) v[e] = (bf16)0.f;
+            *(bf16x8*)&Vb[8 * q] = v;
+          }
+        }
+        if (any) odd[t] = 1;
+        wait_lgkm0();
+        stage_barrier();
+        if (tid == 0) odd[t ^ 1] = 0;  // (read before the last barrier, set after the next)
       }
-      if (more) stage(b ^ 1, k0 + KT, s1);
-      if (tid == 0) odd[s1 == 2 ? 0 : s1 + 1] = 0;  // (read before the last barrier, set after the next)
-      __syncthreads();
+      if (k0 < lim_hi) {  // (uniform in a wave)
+        // Fragments are read ahead of the products that use them, K's all at once,
+        // V's two slices at a time, the first ones before the softmax.
+        f32x16 s[2];
+        {
+          bf16x8 kf[2][NJ];
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) kf[kt][j] = k_frag(Kb, kt, j);
+          start(s, t, bits);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) s[kt] = mfma32(kf[kt][j], qf[j], s[kt]);
+        }
+        bf16x8 vf[2][ND];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < ND; ++i) vf[u][i] = v_frag(Vb, u, i);
+        __builtin_amdgcn_sched_barrier(0);
+        const bool part = k0 + KT > lim_lo || (CAP && ~bits);
+        const bool late = CAP && !BIAS && !part;  // whole tiles without a term: the cap is taken with the exponents
+        if (CAP && !late)
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              s[kt][r] = capped(s[kt][r], BIAS ? c_out + strip[t][sb + 32 * kt + 8 * (r >> 2) + (r & 3)] : c_out);
+        // the causal border, and for capped scores the keys that take no part
+        if (part) {
+          const int left = lim - k0 - 4 * lh;
+          const uint64_t w = bits >> (4 * lh);
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int c = 32 * kt + 8 * (r >> 2) + (r & 3);
+              if (c >= left || (CAP && !(w >> c & 1))) s[kt][r] = -INFINITY;
+            }
+        }
+        float v = s[0][0];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) v = fmaxf(v, s[kt][r]);
+        const float2 h = half_swap(v);
+        float mt = fmaxf(h.x, h.y);
+        if constexpr (!CAP) mt *= sl2;
+        else if (late) mt = capped(mt, c_out);  // (the cap keeps the order of scores)
+        const bool need = mt > m_run + TAU;
+        if (__any(need)) {  // (where a row's maximum stays, its sums are multiplied by one)
+          const float al = need ? __builtin_amdgcn_exp2f(m_run - mt) : 1.0f;
+          m_run = need ? mt : m_run;
+          l_run *= al;
+#pragma unroll
+          for (int t2 = 0; t2 < ND; ++t2)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[t2][r] *= al;
+        }
+        const float ref = exp_ref(m_run);
+        // (the exponent is s sl2 - ref in one rounding; past 2^20 the one that ref
+        // holds of its own product would no longer be a small part of a step)
+        float mul = sl2;
+        if (!CAP && __any(fabsf(ref) > 0x1p20f)) {
+          mul = 1.f;
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kt][r] *= sl2;
+        }
+        if constexpr (CAP) {
+          if (late) {
+            const float add = c_out - ref;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) s[kt][r] = capped(s[kt][r], add);
+          } else {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) s[kt][r] -= ref;
+          }
+        }
+        auto probs = [&](int u) __attribute__((always_inline)) {
+          bf16x8 pf;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float x = s[u >> 1][8 * (u & 1) + i];
+            pf[i] = (bf16)__builtin_amdgcn_exp2f(CAP ? x : fmaf(x, mul, -ref));
+          }
+          l_run = sum_probs(pf, l_run);
+          return pf;
+        };
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const bf16x8 pf = probs(u);
+#pragma unroll
+          for (int i = 0; i < ND; ++i) o[i] = mfma32(vf[u & 1][i], pf, o[i]);
+          if (u < 2) {
+#pragma unroll
+            for (int i = 0; i < ND; ++i) vf[u][i] = v_frag(Vb, u + 2, i);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        if (at_border && odd[t]) add_odd(bits, k0);
+      }
+      if constexpr (BIAS) strip_set(t ^ 1, k0 + KT, f);
       bits = next;
-      slot = s1;
+      wait_vmcnt<0>();
+      wait_lgkm0();
+      stage_barrier();
     }
   }
 
   // O^T: lane holds channels 32 t + 8 (r / 4) + 4 lh + r % 4 of its query.  Rows are
-  // laid out in LDS (K's tiles are done with) and leave 16 bytes a lane.
+  // laid out in LDS (the tiles are done with) and leave 16 bytes a lane.
   const float2 h = half_swap(l_run);
   const float l = h.x + h.y, inv = l == 0.f ? 0.f : 1.0f / l;
   const bool live = r0 + lq < tx.len;
-  bf16* R = &Ks[0][0] + wave * 32 * LDK;
+  bf16* R = smem + wave * 32 * LDR;
 #pragma unroll
   for (int t = 0; t < ND; ++t)
 #pragma unroll
@@ -392,16 +496,17 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
         bf16x4 w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = (bf16)(live ? o[t][4 * i + e] * inv : 0.f);
-        *(bf16x4*)(R + lq * LDK + c) = w;
+        *(bf16x4*)(R + lq * LDR + c) = w;
       }
     }
   asm volatile("" ::: "memory");  // (one wave's LDS accesses complete in order)
+  constexpr int LPR = D16 <= 32 ? 4 : D16 <= 64 ? 8 : D16 <= 128 ? 16 : 32;  // lanes a row
   const int c = lane % LPR * 8, row0 = lane / LPR;
   if (c < d) {
     bf16* O = (bf16*)a.o + tx.o0 + (long)r0 * a.o_ld + p.h * a.o_head + c;
 #pragma unroll
     for (int i = 0; i < 32; i += 64 / LPR)
-      if (r0 + row0 + i < rows) *(bf16x8*)(O + (row0 + i) * (int)a.o_ld) = *(const bf16x8*)(R + (row0 + i) * LDK + c);
+      if (r0 + row0 + i < rows) *(bf16x8*)(O + (row0 + i) * (int)a.o_ld) = *(const bf16x8*)(R + (row0 + i) * LDR + c);
   }
 }
 
@@ -433,6 +538,7 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextAr
   const int lim_lo = a.causal ? max(r0 + 1, tx.prefix) : tx.len, lim_hi = a.causal ? max(r0 + 32, tx.prefix) : tx.len;
   const uint8_t* mask = a.mask ? a.mask + tx.m0 : nullptr;
   const bool terms = a.bias || a.slope;
+  const float slope = a.slope ? a.slope[p.h] : 0.f;
   const float qs = a.scale * (a.cap > 0.f ? 1.f / a.cap : LOG2E), c_out = a.cap * LOG2E;
 
   f32x4 qf[NI];
@@ -469,7 +575,10 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextAr
       rk[i] = __builtin_bit_cast(f32x4, buf_load16(kr, on ? (key * (int)a.k_ld + c) * 4 : OOB));
       rv[i] = __builtin_bit_cast(f32x4, buf_load16(vr, on ? (key * (int)a.v_ld + c) * 4 : OOB));
     }
-    if (terms && tid < KT + TQ - 1) rb = bias_at(a, p.h, k0 - b0 + tid - (TQ - 1), 1.f);
+    if (terms && tid < KT + TQ - 1) {
+      const int far = k0 - b0 + tid - (TQ - 1);
+      rb = term_of(table_at(a, p.h, far), far, slope, 1.f);
+    }
   };
   auto stage = [&](int b, int k0, int slot) __attribute__((always_inline)) {
     const bool border = a.causal && k0 + KT > max(b0 + 1, tx.prefix);
