@@ -56,22 +56,21 @@ __device__ __forceinline__ Span span_of(const TextArgs& a, int c) {
 // with an L2 of its own.  `chunk` tiles of all heads that share a K/V head stay
 // on one XCD, next to each other in time, since they read the same keys; the
 // chunks furthest into their texts come first, as a causal one costs as much as
-// the keys before it.
+// the keys before it.  The grid is (8 XCDs x tiles and heads of a chunk, text and K/V
+// head in eights, chunk): a division costs some 40 instructions before the first load.
 struct Place {
   int c, g, h, tile;
   bool on;
 };
 __device__ __forceinline__ Place place_of(const TextArgs& a) {
-  const unsigned id = blockIdx.x, xcd = id & 7, i = id >> 3, per = (unsigned)a.chunk * a.rep;
-  const unsigned u = i / per * 8 + xcd, in = i % per, pairs = (unsigned)a.n * a.kv_heads;
+  const unsigned in = blockIdx.x >> 3, w = blockIdx.y * 8 + (blockIdx.x & 7);
   Place p;
-  const int ch = a.chunks - 1 - (int)(u / pairs);
-  const unsigned w = u % pairs;
-  p.on = ch >= 0;
-  p.c = w / a.kv_heads;
-  p.g = w % a.kv_heads;
-  p.h = p.g * a.rep + in % a.rep;
-  p.tile = ch * a.chunk + a.chunk - 1 - (int)(in / a.rep);
+  p.on = w < (unsigned)a.n * a.kv_heads;
+  p.c = w / (unsigned)a.kv_heads;
+  p.g = w - p.c * a.kv_heads;
+  const unsigned t = a.rep == 1 ? in : in / (unsigned)a.rep;
+  p.h = p.g * a.rep + in - t * a.rep;
+  p.tile = (int)((a.chunks - blockIdx.z) * a.chunk - 1 - t);
   return p;
 }
 
@@ -133,8 +132,8 @@ __device__ __forceinline__ void to_lds16(rsrc4 r, bf16* to, int off) {
 }
 
 __device__ __forceinline__ bool odd8(uint4 v) {  // an infinity or NaN among eight bf16
-  auto two = [](uint32_t x) { return (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u; };
-  return two(v.x) || two(v.y) || two(v.z) || two(v.w);
+  auto two = [](uint32_t x) { return (x & 0x7F807F80u) + 0x00800080u; };  // (an exponent of ones carries into the sign's place)
+  return ((two(v.x) | two(v.y) | two(v.z) | two(v.w)) & 0x80008000u) != 0;
 }
 __device__ __forceinline__ bool odd_f(float v) { return !(fabsf(v) < INFINITY); }
 
@@ -164,15 +163,19 @@ __device__ __forceinline__ int v_swz(int r) {
 // straight to LDS.  While a tile's probabilities are formed, the next tile's scores
 // are multiplied: the two do not depend on each other, and the matrix unit would
 // wait for the vector ALU otherwise.
-template <int D16, bool BIAS, bool CAP>
-__global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_bf16_kernel(TextArgs a) {
+// SHORT: no text is longer than the two tiles that LDS holds.  They are loaded at
+// once and nothing waits afterwards; a block is as long as its chain of latencies,
+// so four blocks share a CU where registers allow, which leaves fewer for fragments
+// read ahead.  The sums are the same.
+template <int D16, bool BIAS, bool CAP, bool SHORT>
+__global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 : 1) void text_bf16_kernel(TextArgs a) {
   constexpr int NW = 4, KT = 64, NJ = D16 / 16, ND = (D16 + 31) / 32, CH = D16 / 8, NI = (CH + NW - 1) / NW, LDR = D16 + 8;
   constexpr int TILE = KT * D16;
   static_assert(NW * 32 * LDR <= 4 * TILE, "the result's rows take the place of the tiles");
   // K, K, V, V (the last rows of V are read past their end where D16 % 32)
   __shared__ __attribute__((aligned(1024))) bf16 smem[4 * TILE + 64];
   __shared__ float strip[BIAS ? 2 : 1][BIAS ? KT + TQ : 1];
-  __shared__ int odd[2];  // tile t: an infinity or NaN in V where the border passes (slot t % 2)
+  __shared__ int odd[3];  // tile i: an infinity or NaN in V where the border passes (slot i % 3)
   const Place p = place_of(a);
   if (!p.on) return;
   if (a.zero && a.start) zero_rest<bf16>(a, p);
@@ -197,21 +200,16 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
   auto capped = [&](float x, float add) __attribute__((always_inline)) {  // (add: c_out and what else is added)
     return fmaf(-2.f * c_out, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * c_in)), add);
   };
-  // Q^T fragments (B operand): query r0 + lq, channels 16 j + 8 lh + [0, 8)
-  bf16x8 qf[NJ];
+  // Q^T fragments (B operand): query r0 + lq, channels 16 j + 8 lh + [0, 8), as loaded
+  // (their sign comes behind the first tile's loads, or those would wait for them)
+  uint4 qv[NJ];
   {
     const bf16* Q = (const bf16*)a.q + tx.q0 + (long)r0 * a.q_ld + p.h * a.q_head;
     const int n = a.scale == 0.f ? 0 : min(32, tx.len - r0);
     const __amdgpu_buffer_rsrc_t qr = make_rsrc(Q, n <= 0 ? 0 : ((n - 1) * (long)a.q_ld + d) * 2);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      uint4 v = __builtin_bit_cast(uint4, buf_load16(qr, 16 * j + 8 * lh < d ? (lq * (int)a.q_ld + 16 * j + 8 * lh) * 2 : OOB));
-      v.x ^= flip;
-      v.y ^= flip;
-      v.z ^= flip;
-      v.w ^= flip;
-      qf[j] = __builtin_bit_cast(bf16x8, v);
-    }
+    for (int j = 0; j < NJ; ++j)
+      qv[j] = __builtin_bit_cast(uint4, buf_load16(qr, 16 * j + 8 * lh < d ? (lq * (int)a.q_ld + 16 * j + 8 * lh) * 2 : OOB));
   }
   f32x16 o[ND];
 #pragma unroll
@@ -219,7 +217,9 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
-  if (tid < 2) odd[tid] = 0;
+  if (tid < 3) odd[tid] = 0;
+  wait_lgkm0();
+  stage_barrier();
 
   // Load i of this wave moves chunks 64 (wave + NW i) + lane of a tile: key, and
   // byte offsets in K and V.  (Offsets past a resource's end, as those of channels
@@ -249,6 +249,25 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
         if (EVEN && off[0] < 0) at = OOB;
         if (!all && !((EVEN ? mine >> (STEP * i & 63) : bits >> lkey[EVEN ? 0 : i]) & 1)) at = OOB;
         to_lds16(res, to + 512 * (wave + NW * i), at);
+      }
+  };
+  // A key's V reaches every query of a tile, with a weight of 0 behind the causal
+  // border: 0 times an infinity or NaN is NaN.  So those are taken out of a tile that the border
+  // passes (by the wave whose loads brought them, once they have landed), and
+  // added where they are seen.
+  auto clean = [&](bf16* Vt, int slot) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (CH % NW == 0 || wave + NW * i < CH) {
+        bf16* at = Vt + 512 * (wave + NW * i) + 8 * lane;
+        bf16x8 v = *(const bf16x8*)at;
+        if (odd8(__builtin_bit_cast(uint4, v))) {
+          odd[slot] = 1;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (odd_f((float)v[e])) v[e] = (bf16)0.f;
+          *(bf16x8*)at = v;
+        }
       }
   };
   // strip[e] of the tile at k0: the term at distance k0 - b0 + e - (TQ - 1), loaded and then made
@@ -323,46 +342,45 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
   };
 
   if (k_end > 0) {
-    int own = own_mask(0);
-    float f = BIAS ? table_at(a, p.h, far_of(0)) : 0.f;
-    uint64_t bits = ballot(0, own);
-    own = own_mask(KT);
+    int own = own_mask(0), own1 = own_mask(KT);
+    float f = BIAS ? table_at(a, p.h, far_of(0)) : 0.f, f1 = BIAS && SHORT ? table_at(a, p.h, far_of(KT)) : 0.f;
+    uint64_t bits = ballot(0, own), next = 0;
     load(K, a.k_ld, ko, smem, 0, bits);
     load(V, a.v_ld, vo, smem + 2 * TILE, 0, bits);
+    if (SHORT && KT < k_end) {
+      next = ballot(KT, own1);
+      load(K, a.k_ld, ko, smem + TILE, KT, next);
+      load(V, a.v_ld, vo, smem + 3 * TILE, KT, next);
+    }
     if constexpr (BIAS) strip_set(0, 0, f);
+    if constexpr (BIAS && SHORT) strip_set(1, KT, f1);
     wait_vmcnt<0>();
+    if (KT > border) clean(smem + 2 * TILE, 0);
+    if (SHORT && KT < k_end && 2 * KT > border) clean(smem + 3 * TILE, 1);
     wait_lgkm0();
     stage_barrier();
-    for (int k0 = 0, t = 0; k0 < k_end; k0 += KT, t ^= 1) {
-      const uint64_t next = ballot(k0 + KT, own);
-      if (k0 + KT < k_end) {  // (what the registers get is waited for at the end of the tile, with the rest)
-        if (BIAS) f = table_at(a, p.h, far_of(k0 + KT));
-        own = own_mask(k0 + 2 * KT);
-        load(K, a.k_ld, ko, smem + (t ^ 1) * TILE, k0 + KT, next);
-        load(V, a.v_ld, vo, smem + (2 + (t ^ 1)) * TILE, k0 + KT, next);
-      }
-      const bf16* Kb = smem + t * TILE;
-      bf16* Vb = smem + (2 + t) * TILE;
-      const bool at_border = k0 + KT > border;
-      if (at_border) {
-        // (a key's V reaches every query of the tile, with a weight of 0 behind the
-        // border: 0 times an infinity or NaN is NaN, so those are taken out here and added where they are seen)
-        bool any = false;
-        for (int q = tid; q < KT * CH; q += 64 * NW) {
-          bf16x8 v = *(const bf16x8*)&Vb[8 * q];
-          if (odd8(__builtin_bit_cast(uint4, v))) {
-            any = true;
+    bf16x8 qf[NJ];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (odd_f((float)v[e])) v[e] = (bf16)0.f;
-            *(bf16x8*)&Vb[8 * q] = v;
-          }
+    for (int j = 0; j < NJ; ++j) {
+      qv[j].x ^= flip;
+      qv[j].y ^= flip;
+      qv[j].z ^= flip;
+      qv[j].w ^= flip;
+      qf[j] = __builtin_bit_cast(bf16x8, qv[j]);
+    }
+    own = own1;
+    for (int k0 = 0, t = 0, slot = 0; k0 < k_end; k0 += KT, t ^= 1) {
+      const int s1 = slot == 2 ? 0 : slot + 1;
+      if constexpr (!SHORT) {
+        next = ballot(k0 + KT, own);
+        if (k0 + KT < k_end) {  // (what the registers get is waited for at the end of the tile, with the rest)
+          if (BIAS) f = table_at(a, p.h, far_of(k0 + KT));
+          own = own_mask(k0 + 2 * KT);
+          load(K, a.k_ld, ko, smem + (t ^ 1) * TILE, k0 + KT, next);
+          load(V, a.v_ld, vo, smem + (2 + (t ^ 1)) * TILE, k0 + KT, next);
         }
-        if (any) odd[t] = 1;
-        wait_lgkm0();
-        stage_barrier();
-        if (tid == 0) odd[t ^ 1] = 0;  // (read before the last barrier, set after the next)
       }
+      const bf16 *Kb = smem + t * TILE, *Vb = smem + (2 + t) * TILE;
       if (k0 < lim_hi) {  // (uniform in a wave)
         // Fragments are read ahead of the products that use them, K's all at once,
         // V's two slices at a time, the first ones before the softmax.
@@ -374,7 +392,7 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
 #pragma unroll
             for (int j = 0; j < NJ; ++j) kf[kt][j] = k_frag(Kb, kt, j);
           start(s, t, bits);
-          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (!SHORT) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < NJ; ++j)
 #pragma unroll
@@ -385,7 +403,7 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int i = 0; i < ND; ++i) vf[u][i] = v_frag(Vb, u, i);
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!SHORT) __builtin_amdgcn_sched_barrier(0);
         const bool part = k0 + KT > lim_lo || (CAP && ~bits);
         const bool late = CAP && !BIAS && !part;  // whole tiles without a term: the cap is taken with the exponents
         if (CAP && !late)
@@ -468,17 +486,23 @@ __global__ __launch_bounds__(256, D16 <= 64 ? 3 : D16 <= 128 ? 2 : 1) void text_
           if (u < 2) {
 #pragma unroll
             for (int i = 0; i < ND; ++i) vf[u][i] = v_frag(Vb, u + 2, i);
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (!SHORT) __builtin_amdgcn_sched_barrier(0);
           }
         }
-        if (at_border && odd[t]) add_odd(bits, k0);
+        if (k0 + KT > border && odd[slot]) add_odd(bits, k0);
       }
-      if constexpr (BIAS) strip_set(t ^ 1, k0 + KT, f);
       bits = next;
-      wait_vmcnt<0>();
-      wait_lgkm0();
-      stage_barrier();
+      slot = s1;
+      if constexpr (!SHORT) {
+        if constexpr (BIAS) strip_set(t ^ 1, k0 + KT, f);
+        wait_vmcnt<0>();
+        if (k0 + 2 * KT > border && k0 + KT < k_end) clean(smem + (2 + (t ^ 1)) * TILE, s1);
+        if (tid == 0) odd[s1 == 2 ? 0 : s1 + 1] = 0;  // (read before the last barrier, set after the next)
+        wait_lgkm0();
+        stage_barrier();
+      }
     }
+    if constexpr (SHORT) stage_barrier();  // (the result's rows take the place of the tiles)
   }
 
   // O^T: lane holds channels 32 t + 8 (r / 4) + 4 lh + r % 4 of its query.  Rows are
@@ -712,40 +736,43 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextAr
 }
 
 // ------------------------------------------------------------------ launch
-template <int D16>
-static void launch_width(const TextArgs& a, unsigned grid, hipStream_t s) {
+template <int D16, bool SHORT>
+static void launch_kind(const TextArgs& a, dim3 grid, hipStream_t s) {
   const bool terms = a.bias || a.slope;
   if (a.cap > 0.f) {
-    if (terms) text_bf16_kernel<D16, true, true><<<grid, 256, 0, s>>>(a);
-    else text_bf16_kernel<D16, false, true><<<grid, 256, 0, s>>>(a);
+    if (terms) text_bf16_kernel<D16, true, true, SHORT><<<grid, 256, 0, s>>>(a);
+    else text_bf16_kernel<D16, false, true, SHORT><<<grid, 256, 0, s>>>(a);
   } else {
-    if (terms) text_bf16_kernel<D16, true, false><<<grid, 256, 0, s>>>(a);
-    else text_bf16_kernel<D16, false, false><<<grid, 256, 0, s>>>(a);
+    if (terms) text_bf16_kernel<D16, true, false, SHORT><<<grid, 256, 0, s>>>(a);
+    else text_bf16_kernel<D16, false, false, SHORT><<<grid, 256, 0, s>>>(a);
   }
 }
+template <int D16>
+static void launch_width(const TextArgs& a, dim3 grid, hipStream_t s) {
+  if (a.max_len <= 128) launch_kind<D16, true>(a, grid, s);
+  else launch_kind<D16, false>(a, grid, s);
+}
 
-// Blocks of a call, and how they are dealt (a.chunk, a.chunks); -1 past a grid.
-static long place_blocks(TextArgs& a) {
+// The grid of a call (x = 0 past its limits), and how it is dealt (a.chunk, a.chunks).
+static dim3 grid_of(TextArgs& a) {
   const long tiles = a.max_len < 1 ? 1 : ((long)a.max_len + TQ - 1) / TQ;  // (packed rows of no text may still be due zeros)
   a.chunk = (int)(tiles < 8 ? tiles : 8);
   a.chunks = (int)((tiles + a.chunk - 1) / a.chunk);
-  const double units = (double)a.n * a.kv_heads * a.chunks;
-  const double blocks = (units + 8) * a.chunk * a.rep;
-  if (blocks * 256 > 4.0e9) return -1;
-  return ((long)units + 7) / 8 * 8 * a.chunk * a.rep;
+  const long y = ((long)a.n * a.kv_heads + 7) / 8, x = 8L * a.chunk * a.rep;
+  if (y > 65535 || a.chunks > 65535 || (double)x * y * a.chunks * 256 > 4.0e9) return dim3(0);
+  return dim3((unsigned)x, (unsigned)y, (unsigned)a.chunks);
 }
 
 bool text_attention_fits(int n, int heads, int kv_heads, int max_len) {
   TextArgs a;
   a.n = n; a.kv_heads = kv_heads; a.rep = heads / kv_heads; a.max_len = max_len;
-  return place_blocks(a) >= 0;
+  return grid_of(a).x > 0;
 }
 
 hipError_t launch_text_attention(DType dt, TextArgs a, hipStream_t s) {
   if (a.n <= 0) return hipSuccess;
-  const long blocks = place_blocks(a);
-  if (blocks < 0) return hipErrorInvalidValue;
-  const unsigned grid = (unsigned)blocks;
+  const dim3 grid = grid_of(a);
+  if (grid.x == 0) return hipErrorInvalidValue;
   if (dt == BF16) {
     if (a.d <= 32) launch_width<32>(a, grid, s);
     else if (a.d <= 48) launch_width<48>(a, grid, s);
