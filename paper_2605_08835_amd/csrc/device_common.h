@@ -91,6 +91,28 @@ __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, bf16* lds, int o
 #endif
 }
 
+// dma16 in asm, so that the compiler does not know of it: it cannot tell which LDS
+// reads the load concerns, and in the loops that use this one it waited for it at the
+// next one, a tile too early.  Whoever reads
+// waits (vmcnt 0, then a barrier); no register is written.  (The five wait states are
+// those between a vector instruction that wrote a resource word and its use here.)
+typedef int rsrc4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ rsrc4 resource(const void* base, long bytes) {
+  const uint64_t b = (uint64_t)base;
+  rsrc4 r;
+  r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)b);
+  r[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32) & 0xFFFF);
+  r[2] = __builtin_amdgcn_readfirstlane((int)bytes);
+  r[3] = 0x00020000;
+  return r;
+}
+__device__ __forceinline__ void to_lds16(rsrc4 r, bf16* to, int off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int m = __builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) bf16*)to);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m), "v"(off), "s"(r) : "memory");
+#endif
+}
+
 // Workgroup barrier for the direct-to-LDS pipelines.  __syncthreads()
 // carries a workgroup release fence, for which the compiler waits for every
 // outstanding load that writes LDS (vmcnt(0)), including the prefetches of

@@ -702,18 +702,17 @@ __device__ __forceinline__ void adapter_products(const AdapterArgs& a, f32x16 (&
     const long rows = (long)a.M * a.rank * 2;  // (read through resources: what lies past rank or N is zero)
     const __amdgpu_buffer_rsrc_t br = make_rsrc(a.up + (long)cur * a.N * a.rank, (long)a.N * a.rank * 2);
     const __amdgpu_buffer_rsrc_t hr = make_rsrc(a.hi + (long)a.row0 * a.rank, rows), lor = make_rsrc(a.lo + (long)a.row0 * a.rank, rows);
+    const int nl = n0 + wn * (BN / WN) + lr, ml = m0 + wm * (BM / WM) + lr;
 #pragma unroll 1
-    for (int k = 8 * lh; k - 8 * lh < a.rank; k += 16) {
+    for (int k = 0; k < a.rank; k += 16) {
+      const int kk = k + 8 * lh;
       bf16x8 b[TN];
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int n = n0 + wn * (BN / WN) + j * 32 + lr;
-        b[j] = buf_load16(br, k < a.rank && n < a.N ? (n * a.rank + k) * 2 : OOB);
-      }
+      for (int j = 0; j < TN; ++j) b[j] = buf_load16(br, kk < a.rank && nl + 32 * j < a.N ? ((nl + 32 * j) * a.rank + kk) * 2 : OOB);
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
         if (!mine[i]) continue;
-        const int m = m0 + wm * (BM / WM) + i * 32 + lr, at = k < a.rank && m < a.M ? (m * a.rank + k) * 2 : OOB;
+        const int at = kk < a.rank && ml + 32 * i < a.M ? ((ml + 32 * i) * a.rank + kk) * 2 : OOB;
         const bf16x8 h = buf_load16(hr, at), l = buf_load16(lor, at);
         const bool whole = mine[i] == ~0ull, on = id[i] == cur;
 #pragma unroll
@@ -745,7 +744,8 @@ __device__ __forceinline__ void epilogue_adapters(const AdapterArgs& a, const f3
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int n = ncol0 + J.value * 32 + 8 * q + hq;
-        const float4 b = a.epi.bias && n < a.N ? *reinterpret_cast<const float4*>(a.epi.bias + n) : make_float4(0.f, 0.f, 0.f, 0.f);
+        // (columns from N on are not stored)
+        const float4 b = a.epi.bias ? *reinterpret_cast<const float4*>(a.epi.bias + (n < a.N ? n : 0)) : make_float4(0.f, 0.f, 0.f, 0.f);
         bf16x4 o;
         o[0] = (bf16)(v[4 * q] + b.x);
         o[1] = (bf16)(v[4 * q + 1] + b.y);

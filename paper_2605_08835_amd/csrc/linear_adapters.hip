@@ -74,79 +74,118 @@ __global__ __launch_bounds__(256) void adapters_down_rows_kernel(LinearAdaptersA
 }
 
 // ------------------------------------------------------------------ v, many rows
-// A block has 32 rows and RT x 32 of the rank, its KW waves share out K 64 at a
-// time: V^T = down x^T, so that a lane has one row's values.  v's two parts go to
-// scratch, [M, rank] each.
-template <int RT, int KW>
-__global__ __launch_bounds__(64 * KW) void adapters_down_kernel(LinearAdaptersArgs a) {
+// A block has 32 MW rows and RT x 32 of the rank: V^T = down x^T, so that a lane has
+// one row's values.  Tiles of 64 k of x and `down` go straight to LDS, two ahead of
+// the one that is multiplied; MW waves have 32 rows each, the rest share out a tile's
+// k and are summed at the end.  v's two parts go to scratch, [M, rank] each.
+// Chunk c (16 bytes) of a tile's row r lies in slot c ^ (r / 2 % 8): fragment reads of
+// 16 rows are spread over all banks.
+template <int MW, int RT>
+__global__ __launch_bounds__(256, 2) void adapters_down_kernel(LinearAdaptersArgs a) {
+  constexpr int NW = 4, KW = NW / MW, BM = 32 * MW, BR = 32 * RT, NS = 3, XI = MW, DI = RT, LPT = XI + DI, STAGE = (BM + BR) * 64;
+  constexpr int PART = (KW - 1) * MW * RT * 16 * 64;  // floats of the partial sums
+  __shared__ __attribute__((aligned(1024))) bf16 smem[NS * STAGE > 2 * PART ? NS * STAGE : 2 * PART];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 31, lh = lane >> 5;
-  const int m = blockIdx.x * 32 + lr, r0 = blockIdx.y * RT * 32;
-  __shared__ float part[KW > 1 ? KW - 1 : 1][KW > 1 ? RT * 16 * 64 : 1];
-  const int c = m < a.M ? adapter_of(a, m) : -1;
-  uint64_t left = __ballot(c >= 0);
-  const int rows = min(32, a.M - (int)blockIdx.x * 32);
-  const __amdgpu_buffer_rsrc_t xr = make_rsrc((const bf16*)a.x + (long)blockIdx.x * 32 * a.K, (long)rows * a.K * 2);
+  const int wm = wave % MW, wk = wave / MW;
+  const int m0 = blockIdx.x * BM, r0 = blockIdx.y * BR, rows = min(BM, a.M - m0);
+  const int row_id = lane < rows ? adapter_of(a, m0 + lane) : -1;  // (lane: a row of the block)
+  uint64_t left = __ballot(row_id >= 0);
+  if (!left) return;
+  const int own = __shfl(row_id, wm * 32 + lr, 64);
+  const rsrc4 xr = resource((const bf16*)a.x + (long)m0 * a.K, (long)rows * a.K * 2);
+  // loads i of a tile: rows 8 (wave + NW i) on, 8 lanes a row
+  const int lrow = lane >> 3, slot = lane & 7;
+  int xo[XI], dof[DI], kc[XI > DI ? XI : DI];
+#pragma unroll
+  for (int i = 0; i < (XI > DI ? XI : DI); ++i) {
+    const int r = 8 * (wave + NW * i) + lrow, c = (slot ^ (r >> 1 & 7)) * 8;
+    kc[i] = c;
+    if (i < XI) xo[i] = r < rows ? (r * a.K + c) * 2 : OOB;
+    if (i < DI) dof[i] = r0 + r < a.rank ? (r * a.K + c) * 2 : OOB;
+  }
+  const int tiles = (a.K + 63) / 64;
   while (left) {
-    const int cur = __builtin_amdgcn_readlane(c, __builtin_ctzll(left));
-    left &= ~__ballot(c == cur);
-    const __amdgpu_buffer_rsrc_t dr =
-        make_rsrc((const bf16*)a.down + ((long)cur * a.rank + r0) * a.K, (long)(a.rank - r0) * a.K * 2);
+    const int cur = __builtin_amdgcn_readlane(row_id, __builtin_ctzll(left));
+    left &= ~__ballot(row_id == cur);
+    const rsrc4 dr = resource((const bf16*)a.down + ((long)cur * a.rank + r0) * a.K, (long)(a.rank - r0) * a.K * 2);
+    auto issue = [&](int t, int stage) __attribute__((always_inline)) {  // (past the last tile: zeros)
+      bf16* to = smem + stage * STAGE;
+      const int k0 = 64 * t;
+#pragma unroll
+      for (int i = 0; i < XI; ++i) to_lds16(xr, to + 512 * (wave + NW * i), k0 + kc[i] < a.K && xo[i] >= 0 ? xo[i] + 2 * k0 : OOB);
+#pragma unroll
+      for (int i = 0; i < DI; ++i)
+        to_lds16(dr, to + BM * 64 + 512 * (wave + NW * i), k0 + kc[i] < a.K && dof[i] >= 0 ? dof[i] + 2 * k0 : OOB);
+    };
     f32x16 acc[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
-    for (int k0 = wave * 64; k0 < a.K; k0 += KW * 64) {
-      bf16x8 xv[4], dv[RT][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int k = k0 + 16 * j + 8 * lh;
-        xv[j] = buf_load16(xr, k < a.K ? (lr * a.K + k) * 2 : OOB);
+    for (int t = 0; t < NS - 1; ++t) issue(t, t);
+    int st = 0;
+    for (int t = 0; t < tiles; ++t) {
+      wait_vmcnt<(NS - 2) * LPT>();
+      stage_barrier();
+      issue(t + NS - 1, st == 0 ? NS - 1 : st - 1);
+      const bf16 *X = smem + st * STAGE + wm * 32 * 64, *D = smem + st * STAGE + BM * 64;
+      bf16x8 xf[4 / KW], df[4 / KW][RT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) dv[t][j] = buf_load16(dr, k < a.K ? ((32 * t + lr) * a.K + k) * 2 : OOB);
+      for (int j = 0; j < 4 / KW; ++j) {
+        const int c = ((2 * (wk + KW * j) + lh) ^ (lr >> 1 & 7)) * 8;
+        xf[j] = *(const bf16x8*)(X + lr * 64 + c);
+#pragma unroll
+        for (int u = 0; u < RT; ++u) df[j][u] = *(const bf16x8*)(D + (32 * u + lr) * 64 + c);
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 4 / KW; ++j)
 #pragma unroll
-        for (int t = 0; t < RT; ++t) acc[t] = mfma32(dv[t][j], xv[j], acc[t]);
+        for (int u = 0; u < RT; ++u) acc[u] = mfma32(df[j][u], xf[j], acc[u]);
+      wait_lgkm0();
+      st = st == NS - 1 ? 0 : st + 1;
     }
-    if constexpr (KW > 1) {
-      __syncthreads();
-      if (wave > 0)
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) part[wave - 1][(t * 16 + i) * 64 + lane] = acc[t][i];
-      __syncthreads();
-      if (wave == 0)
-#pragma unroll
-        for (int w = 0; w < KW - 1; ++w)
-#pragma unroll
-          for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[t][i] += part[w][(t * 16 + i) * 64 + lane];
-    }
-    if (wave == 0 && c == cur) {
-      const float f = a.scale ? a.scale[c] : 1.f;
-      bf16 *hi = (bf16*)a.scratch + (long)m * a.rank, *lo = hi + (long)a.M * a.rank;
+    wait_vmcnt<0>();
+    stage_barrier();
+    float* part = (float*)smem;
+    if (wk > 0)
 #pragma unroll
       for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int r = r0 + 32 * t + 8 * q + 4 * lh;
-          if (r < a.rank) {
-            bf16x4 h, l;
+        for (int i = 0; i < 16; ++i) part[(((wk - 1) * MW + wm) * RT * 16 + t * 16 + i) * 64 + lane] = acc[t][i];
+    wait_lgkm0();
+    stage_barrier();
+    if (wk == 0) {
+#pragma unroll 1
+      for (int w = 0; w < KW - 1; ++w)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float v = acc[t][4 * q + e] * f;
-              h[e] = (bf16)v;
-              l[e] = (bf16)(v - (float)h[e]);
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[t][i] += part[((w * MW + wm) * RT * 16 + t * 16 + i) * 64 + lane];
+      if (own == cur) {
+        const float f = a.scale ? a.scale[cur] : 1.f;
+        bf16 *hi = (bf16*)a.scratch + (long)(m0 + wm * 32 + lr) * a.rank, *lo = hi + (long)a.M * a.rank;
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int r = r0 + 32 * t + 8 * q + 4 * lh;
+            if (r < a.rank) {
+              bf16x4 h, l;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float v = acc[t][4 * q + e] * f;
+                h[e] = (bf16)v;
+                l[e] = (bf16)(v - (float)h[e]);
+              }
+              *(bf16x4*)(hi + r) = h;
+              *(bf16x4*)(lo + r) = l;
             }
-            *(bf16x4*)(hi + r) = h;
-            *(bf16x4*)(lo + r) = l;
           }
-        }
+      }
     }
+    wait_lgkm0();
+    stage_barrier();  // (the next adapter's tiles take the place of the partial sums)
   }
 }
 
@@ -164,7 +203,6 @@ __global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a
   f32x4 acc[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
   for (int k0 = wave * 64; k0 < a.K; k0 += NW * 64) {
     bf16x8 wv[2], xv[2][MT];
 #pragma unroll
@@ -255,11 +293,11 @@ long linear_adapters_scratch_floats(int M, int rank) { return (long)M * rank; }
 
 template <int RT>
 static void launch_down(const LinearAdaptersArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.M + 31) / 32), (unsigned)((a.rank + 32 * RT - 1) / (32 * RT)));
-  if (a.M < 32768 && a.K > 64)
-    adapters_down_kernel<RT, 4><<<grid, 256, 0, s>>>(a);
+  const unsigned y = (unsigned)((a.rank + 32 * RT - 1) / (32 * RT));
+  if (a.M < 16384)
+    adapters_down_kernel<1, RT><<<dim3((unsigned)((a.M + 31) / 32), y), 256, 0, s>>>(a);
   else
-    adapters_down_kernel<RT, 1><<<grid, 64, 0, s>>>(a);
+    adapters_down_kernel<2, RT><<<dim3((unsigned)((a.M + 63) / 64), y), 256, 0, s>>>(a);
 }
 
 template <typename T>
