@@ -329,12 +329,12 @@ sd_status synerdiff_op_text_attention(int32_t dtype, const void* d_q, int64_t q_
  * and for up to 64 rows, else held to 2^-17 of it (two bf16 parts; below 2^-110
  * less).  Any order of indices is right; runs of 32 rows or more of one adapter are fast.
  * Constraints: K, N, rank multiples of 8; K, N <= 2^20, rank <= 1024; w, up[c] and
- * down[c] below 2^31 bytes; M <= 2^26, M N < 2^35 (fp32: M rank < 2^28); all
+ * down[c] below 2^31 bytes; M <= 2^26, M N < 2^35, M rank < 2^33; all
  * buffers and rows of out at multiples of 16 bytes (scale, index: 4).  out
  * overlaps nothing.  d_scratch (fp32, 16-byte aligned) holds
- * synerdiff_op_linear_adapters_scratch_floats(M, rank) floats (SD_ERR_WORKSPACE
- * if fewer), and belongs to this call until it has run.  M = 0 or N = 0 does nothing. */
-int64_t synerdiff_op_linear_adapters_scratch_floats(int32_t M, int32_t rank);
+ * synerdiff_op_linear_adapters_scratch_floats(...) floats (0: none needed;
+ * SD_ERR_WORKSPACE if fewer), and belongs to this call until it has run.  M = 0 or N = 0 does nothing. */
+int64_t synerdiff_op_linear_adapters_scratch_floats(int32_t dtype, int32_t M, int32_t rank);
 sd_status synerdiff_op_linear_adapters(int32_t dtype, const void* d_x, int32_t M, int32_t K, const void* d_w, int32_t N,
                                        const void* d_down, const void* d_up, int32_t rank, int32_t count,
                                        const float* d_scale, const int32_t* d_index, int32_t group,

@@ -146,7 +146,7 @@ _SIG = {
                                     [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, _P,
                                      ctypes.c_float, _P, ctypes.c_int32, _P] + [ctypes.c_int32] * 3 +
                                     [ctypes.c_float, ctypes.c_int32, _P]),
-    "synerdiff_op_linear_adapters_scratch_floats": (ctypes.c_int64, [ctypes.c_int32] * 2),
+    "synerdiff_op_linear_adapters_scratch_floats": (ctypes.c_int64, [ctypes.c_int32] * 3),
     "synerdiff_op_linear_adapters": (ctypes.c_int, [ctypes.c_int32, _P, ctypes.c_int32, ctypes.c_int32, _P, ctypes.c_int32,
                                                     _P, _P, ctypes.c_int32, ctypes.c_int32, _P, _P, ctypes.c_int32, _P, _P,
                                                     ctypes.c_int64, _P, ctypes.c_int64, _P]),

@@ -236,7 +236,7 @@ struct LinearAdaptersArgs {
   float* scratch;
 };
 hipError_t launch_linear_adapters(DType dt, const LinearAdaptersArgs& a, hipStream_t s);
-long linear_adapters_scratch_floats(int M, int rank);
+long linear_adapters_scratch_floats(DType dt, int M, int rank);
 
 // Attention over contexts of their own lengths, see synerdiff_op_cross_attention.
 struct CrossArgs {

@@ -2,11 +2,12 @@
 //   out[m] = bias + W x[m] + scale[c] up[c] (down[c] x[m]),  c = index[m / group].
 //
 // Two launches: v = scale[c] down[c] x first, then the layer, which adds up[c] v.
-//  * Many rows (bf16): v on MFMAs, 32 rows a block; then the GEMM of gemm.hip,
-//    whose accumulators start with the adapters' part.  v is kept as two bf16 parts
-//    (2^-17 of it), so that the second product is one of bf16 MFMAs too.
+//  * Many rows (bf16): v on MFMAs; then the GEMM of gemm.hip, whose accumulators
+//    start with the adapters' part.  v is kept as two bf16 parts (2^-17 of it), so
+//    that the second product is one of bf16 MFMAs too.
 //  * Few rows (bf16, at most 64): bound by the bytes of W and of the adapters in use.
-//    A block has 16 outputs of all rows, its waves share out K.  v is fp32.
+//    A block has 16 outputs of all rows, its waves share out K.  v is fp32; up to
+//    64 values of it every block makes for itself, in one launch.
 //  * fp32: the adapters' part goes to `out` first and is the GEMM's residual.
 // A row sees its own adapter only: what others hold, infinities and NaN included,
 // does not reach it.
@@ -42,16 +43,11 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 x, bf16x8 y, f32x4 c) {
 }  // namespace
 
 // ------------------------------------------------------------------ v, few rows
-// A wave has one row and four of its adapter's rows, lanes share out K 8 at a time.
+// v of row m and four of its adapter's rows from r0 on, by one wave: lanes share out
+// K 8 at a time.  (rank is a multiple of 8.)
 template <typename T>
-__global__ __launch_bounds__(256) void adapters_down_rows_kernel(LinearAdaptersArgs a) {
+__device__ __forceinline__ float4 down_four(const LinearAdaptersArgs& a, int m, int c, int r0, int lane) {
   constexpr int RW = 4;
-  const int per = (a.rank + RW - 1) / RW, lane = threadIdx.x & 63;
-  const long id = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= (long)a.M * per) return;
-  const int m = (int)(id / per), r0 = (int)(id % per) * RW;
-  const int c = adapter_of(a, m);
-  if (c < 0) return;  // (its v is not read)
   const T* x = (const T*)a.x + (long)m * a.K;
   const T* d = (const T*)a.down + ((long)c * a.rank + r0) * a.K;
   float s[RW];
@@ -61,7 +57,7 @@ __global__ __launch_bounds__(256) void adapters_down_rows_kernel(LinearAdaptersA
     float xv[8], dv[RW][8];
     load8f(x + k, xv);
 #pragma unroll
-    for (int r = 0; r < RW; ++r) load8f(d + (long)r * a.K + k, dv[r]);  // (rank is a multiple of 8)
+    for (int r = 0; r < RW; ++r) load8f(d + (long)r * a.K + k, dv[r]);
 #pragma unroll
     for (int r = 0; r < RW; ++r)
 #pragma unroll
@@ -70,7 +66,16 @@ __global__ __launch_bounds__(256) void adapters_down_rows_kernel(LinearAdaptersA
 #pragma unroll
   for (int r = 0; r < RW; ++r) s[r] = wave_sum(s[r]);
   const float f = a.scale ? a.scale[c] : 1.f;
-  if (lane == 0) *(float4*)(a.scratch + (long)m * a.rank + r0) = make_float4(s[0] * f, s[1] * f, s[2] * f, s[3] * f);
+  return make_float4(s[0] * f, s[1] * f, s[2] * f, s[3] * f);
+}
+
+__global__ __launch_bounds__(256) void adapters_down_rows_kernel(LinearAdaptersArgs a) {
+  const int per = a.rank / 4, lane = threadIdx.x & 63, id = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (id >= a.M * per) return;
+  const int m = id / per, r0 = (id - m * per) * 4, c = adapter_of(a, m);
+  if (c < 0) return;  // (its v is not read)
+  const float4 v = down_four<bf16>(a, m, c, r0, lane);
+  if (lane == 0) *(float4*)(a.scratch + (long)m * a.rank + r0) = v;
 }
 
 // ------------------------------------------------------------------ v, many rows
@@ -104,9 +109,10 @@ __global__ __launch_bounds__(256, 2) void adapters_down_kernel(LinearAdaptersArg
     if (i < DI) dof[i] = r0 + r < a.rank ? (r * a.K + c) * 2 : OOB;
   }
   const int tiles = (a.K + 63) / 64;
-  while (left) {
+  for (unsigned turn = 0; left; ++turn) {  // (adapters in order of their first rows; blocks in z share them out)
     const int cur = __builtin_amdgcn_readlane(row_id, __builtin_ctzll(left));
     left &= ~__ballot(row_id == cur);
+    if (turn % gridDim.z != blockIdx.z) continue;
     const rsrc4 dr = resource((const bf16*)a.down + ((long)cur * a.rank + r0) * a.K, (long)(a.rank - r0) * a.K * 2);
     auto issue = [&](int t, int stage) __attribute__((always_inline)) {  // (past the last tile: zeros)
       bf16* to = smem + stage * STAGE;
@@ -191,11 +197,14 @@ __global__ __launch_bounds__(256, 2) void adapters_down_kernel(LinearAdaptersArg
 
 // ------------------------------------------------------------------ few rows, bf16
 // A block has 16 outputs of all rows (MT x 16), its 8 waves share out K 64 at a
-// time and are summed in order.
-template <int MT>
+// time and are summed in order.  OWN: it makes v itself (at most OWN_V values), beside the others'
+// loads: 1 row, 1280 x 1280, rank 16 in one launch of 4.6 us against two of 2.9 and 4.3.
+constexpr int OWN_V = 64;
+template <int MT, bool OWN>
 __global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a) {
   constexpr int NW = 8;
   __shared__ float part[NW][MT][256];
+  __shared__ __attribute__((aligned(16))) float own_v[OWN ? OWN_V : 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, lk = 8 * (lane >> 4);
   const int n0 = blockIdx.x * 16;
   const __amdgpu_buffer_rsrc_t wr = make_rsrc((const bf16*)a.w + (long)n0 * a.K, (long)min(16, a.N - n0) * a.K * 2);
@@ -219,6 +228,15 @@ __global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a
   }
 #pragma unroll
   for (int t = 0; t < MT; ++t) *(f32x4*)&part[wave][t][4 * lane] = acc[t];
+  if constexpr (OWN) {
+    const int per = a.rank / 4;
+    for (int id = wave; id < a.M * per; id += NW) {
+      const int m = id / per, r0 = (id - m * per) * 4, c = adapter_of(a, m);
+      if (c < 0) continue;
+      const float4 v = down_four<bf16>(a, m, c, r0, lane);
+      if (lane == 0) *(float4*)(own_v + m * a.rank + r0) = v;
+    }
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < MT * 256; i += 512) {
     // element i % 4 of lane i / 4: output 4 (lane / 16) + i % 4, row lane % 16
@@ -229,7 +247,7 @@ __global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a
     for (int w = 0; w < NW; ++w) s += part[w][t][at];
     const int c = adapter_of(a, m);
     if (c >= 0) {
-      const float* v = a.scratch + (long)m * a.rank;
+      const float* v = OWN ? own_v + m * a.rank : a.scratch + (long)m * a.rank;
       const bf16* u = (const bf16*)a.up + ((long)c * a.N + n) * a.rank;
       for (int r = 0; r < a.rank; r += 8) {
         float uv[8], vv[8];
@@ -244,75 +262,90 @@ __global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a
 }
 
 // ------------------------------------------------------------------ fp32: the adapters' part
-// A thread has one output column of 8 rows; rows with the first one's adapter share its loads.
-__global__ __launch_bounds__(256) void adapters_up_f32_kernel(LinearAdaptersArgs a) {
-  constexpr int MR = 8;
-  const int n = blockIdx.y * 256 + threadIdx.x;
-  const long m0 = (long)blockIdx.x * MR;
-  if (n >= a.N) return;
-  const int rows = (int)min((long)MR, a.M - m0);
-  int c[MR];
-  float s[MR];
+// A block has 8 rows: their v to LDS, then a thread per output column of all 8; rows
+// of one adapter share the loads of its `up`.
+constexpr int F32_ROWS = 8;
+__global__ __launch_bounds__(256) void adapters_f32_kernel(LinearAdaptersArgs a) {
+  constexpr int MR = F32_ROWS;
+  extern __shared__ __attribute__((aligned(16))) float v[];  // [MR, rank]
+  const int m0 = blockIdx.x * MR, rows = min(MR, a.M - m0), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = a.rank / 4;
+  for (int id = wave; id < rows * per; id += 4) {
+    const int i = id / per, r0 = (id - i * per) * 4, c = adapter_of(a, m0 + i);
+    if (c < 0) continue;
+    const float4 f = down_four<float>(a, m0 + i, c, r0, lane);
+    if (lane == 0) *(float4*)(v + i * a.rank + r0) = f;
+  }
+  int c[MR], all = 0;
+#pragma unroll
   for (int i = 0; i < MR; ++i) {
-    c[i] = i < rows ? adapter_of(a, (int)m0 + i) : -1;
-    s[i] = 0.f;
+    c[i] = i < rows ? adapter_of(a, m0 + i) : -1;
+    all |= (c[i] >= 0) << i;
   }
-  int left = 0;
+  __syncthreads();
+  for (int n = threadIdx.x; n < a.N; n += 256) {
+    float s[MR];
 #pragma unroll
-  for (int i = 0; i < MR; ++i) left |= (c[i] >= 0) << i;
-  while (left) {
-    int cur = -1;
+    for (int i = 0; i < MR; ++i) s[i] = 0.f;
+    for (int left = all; left;) {
+      int cur = -1, mine = 0;
 #pragma unroll
-    for (int i = MR - 1; i >= 0; --i)
-      if (left >> i & 1) cur = c[i];
-    int mine = 0;
+      for (int i = MR - 1; i >= 0; --i)
+        if (left >> i & 1) cur = c[i];
 #pragma unroll
-    for (int i = 0; i < MR; ++i) mine |= (c[i] == cur) << i;
-    left &= ~mine;
-    const float* u = (const float*)a.up + ((long)cur * a.N + n) * a.rank;
-    const float* v = a.scratch + m0 * a.rank;
-    for (int r = 0; r < a.rank; r += 4) {
-      const float4 uv = *(const float4*)(u + r);
+      for (int i = 0; i < MR; ++i) mine |= (c[i] == cur) << i;
+      left &= ~mine;
+      const float* u = (const float*)a.up + ((long)cur * a.N + n) * a.rank;
+      for (int r = 0; r < a.rank; r += 4) {
+        const float4 uv = *(const float4*)(u + r);
 #pragma unroll
-      for (int i = 0; i < MR; ++i)
-        if (mine >> i & 1) {
-          const float4 vv = *(const float4*)(v + (long)i * a.rank + r);
-          s[i] = fmaf(uv.x, vv.x, fmaf(uv.y, vv.y, fmaf(uv.z, vv.z, fmaf(uv.w, vv.w, s[i]))));
-        }
+        for (int i = 0; i < MR; ++i)
+          if (mine >> i & 1) {
+            const float4 vv = *(const float4*)(v + i * a.rank + r);
+            s[i] = fmaf(uv.x, vv.x, fmaf(uv.y, vv.y, fmaf(uv.z, vv.z, fmaf(uv.w, vv.w, s[i]))));
+          }
+      }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < MR; ++i)
-    if (i < rows) ((float*)a.out)[(m0 + i) * a.out_ld + n] = s[i];
+    for (int i = 0; i < MR; ++i)
+      if (i < rows) ((float*)a.out)[(long)(m0 + i) * a.out_ld + n] = s[i];
+  }
 }
 
 // ------------------------------------------------------------------ launch
 constexpr int FEW = 64;  // rows of the few-row kernel
 
-long linear_adapters_scratch_floats(int M, int rank) { return (long)M * rank; }
+long linear_adapters_scratch_floats(DType dt, int M, int rank) {
+  return dt != BF16 || (M <= FEW && (long)M * rank <= OWN_V) ? 0 : (long)M * rank;
+}
 
+// 64 rows a block once that gives every CU one, else 32.  An index per row may bring
+// several adapters to a block: up to 4 blocks share them out then (runs of 1 to 77
+// rows, 1872 x 768, rank 16: 10.5 us alone).
 template <int RT>
 static void launch_down(const LinearAdaptersArgs& a, hipStream_t s) {
   const unsigned y = (unsigned)((a.rank + 32 * RT - 1) / (32 * RT));
   if (a.M < 16384)
-    adapters_down_kernel<1, RT><<<dim3((unsigned)((a.M + 31) / 32), y), 256, 0, s>>>(a);
+    adapters_down_kernel<1, RT><<<dim3((unsigned)((a.M + 31) / 32), y, a.group < 32 ? 4 : 1), 256, 0, s>>>(a);
   else
     adapters_down_kernel<2, RT><<<dim3((unsigned)((a.M + 63) / 64), y), 256, 0, s>>>(a);
 }
 
-template <typename T>
-static void launch_down_rows(const LinearAdaptersArgs& a, hipStream_t s) {
-  const long waves = (long)a.M * (a.rank / 4);
-  adapters_down_rows_kernel<T><<<dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s>>>(a);
+template <int MT>
+static void launch_rows(const LinearAdaptersArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.N + 15) / 16));
+  if ((long)a.M * a.rank <= OWN_V)
+    adapters_rows_kernel<MT, true><<<grid, 512, 0, s>>>(a);
+  else {
+    adapters_down_rows_kernel<<<dim3((unsigned)(((long)a.M * (a.rank / 4) + 3) / 4)), dim3(256), 0, s>>>(a);
+    adapters_rows_kernel<MT, false><<<grid, 512, 0, s>>>(a);
+  }
 }
 
 static hipError_t launch_bf16(const LinearAdaptersArgs& a, hipStream_t s) {
   if (a.M <= FEW) {
-    launch_down_rows<bf16>(a, s);
-    const dim3 grid((unsigned)((a.N + 15) / 16));
-    if (a.M <= 16) adapters_rows_kernel<1><<<grid, 512, 0, s>>>(a);
-    else if (a.M <= 32) adapters_rows_kernel<2><<<grid, 512, 0, s>>>(a);
-    else adapters_rows_kernel<4><<<grid, 512, 0, s>>>(a);
+    if (a.M <= 16) launch_rows<1>(a, s);
+    else if (a.M <= 32) launch_rows<2>(a, s);
+    else launch_rows<4>(a, s);
     return hipGetLastError();
   }
   if (a.rank <= 32) launch_down<1>(a, s);
@@ -353,8 +386,7 @@ static hipError_t launch_bf16(const LinearAdaptersArgs& a, hipStream_t s) {
 }
 
 static hipError_t launch_f32(const LinearAdaptersArgs& a, hipStream_t s) {
-  launch_down_rows<float>(a, s);
-  adapters_up_f32_kernel<<<dim3((unsigned)((a.M + 7) / 8), (unsigned)((a.N + 255) / 256)), dim3(256), 0, s>>>(a);
+  adapters_f32_kernel<<<dim3((unsigned)((a.M + F32_ROWS - 1) / F32_ROWS)), dim3(256), (unsigned)(F32_ROWS * a.rank * 4), s>>>(a);
   GemmArgs g;
   memset(&g, 0, sizeof(g));
   g.M = a.M;

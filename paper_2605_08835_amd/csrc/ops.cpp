@@ -479,8 +479,8 @@ sd_status synerdiff_op_text_attention(int32_t dtype, const void* q, int64_t q_ld
   return op_hip(launch_text_attention((DType)dtype, a, (hipStream_t)stream), "text_attention");
 }
 
-int64_t synerdiff_op_linear_adapters_scratch_floats(int32_t M, int32_t rank) {
-  return M > 0 && rank > 0 ? linear_adapters_scratch_floats(M, rank) : 0;
+int64_t synerdiff_op_linear_adapters_scratch_floats(int32_t dtype, int32_t M, int32_t rank) {
+  return !bad_dtype(dtype) && M > 0 && rank > 0 ? linear_adapters_scratch_floats((DType)dtype, M, rank) : 0;
 }
 
 sd_status synerdiff_op_linear_adapters(int32_t dtype, const void* x, int32_t M, int32_t K, const void* w, int32_t N,
@@ -494,8 +494,7 @@ sd_status synerdiff_op_linear_adapters(int32_t dtype, const void* x, int32_t M, 
   if ((int64_t)N * K >= whole || (int64_t)N * rank >= whole || (int64_t)rank * K >= whole || K > 1 << 20 || N > 1 << 20 ||
       rank > 1 << 10)
     return op_fail(SD_ERR_UNSUPPORTED, "weights of 2^31 bytes, more than 2^20 columns or ranks past 1024");
-  if (M > 1 << 26 || (int64_t)M * N >= 1ll << 35 || (int64_t)M * rank >= 1ll << 33 ||
-      (dtype == SD_F32 && (int64_t)M * rank >= 1ll << 28))
+  if (M > 1 << 26 || (int64_t)M * N >= 1ll << 35 || (int64_t)M * rank >= 1ll << 33)
     return op_fail(SD_ERR_UNSUPPORTED, "too many rows");
   if (M == 0 || N == 0) return SD_OK;
   if (!x || !w || !index || !out || (count > 0 && (!down || !up))) return op_fail(SD_ERR_INVALID_ARG, "NULL argument");
@@ -505,8 +504,8 @@ sd_status synerdiff_op_linear_adapters(int32_t dtype, const void* x, int32_t M, 
     return op_fail(SD_ERR_INVALID_ARG, "buffers and rows of out must be 16-byte aligned");
   if (((uintptr_t)scale | (uintptr_t)index) & 3) return op_fail(SD_ERR_INVALID_ARG, "an array is not aligned to its element");
   if (out == x || out == w || out == down || out == up) return op_fail(SD_ERR_INVALID_ARG, "out overlaps an input");
-  if (!scratch || scratch_floats < linear_adapters_scratch_floats(M, rank))
-    return op_fail(SD_ERR_WORKSPACE, "scratch is too small");
+  const int64_t need = linear_adapters_scratch_floats((DType)dtype, M, rank);
+  if (need > 0 && (!scratch || scratch_floats < need)) return op_fail(SD_ERR_WORKSPACE, "scratch is too small");
   if ((uintptr_t)scratch & 15) return op_fail(SD_ERR_INVALID_ARG, "scratch must be 16-byte aligned");
   LinearAdaptersArgs a;
   memset(&a, 0, sizeof(a));

@@ -464,11 +464,13 @@ def linear_adapters(x, w, down, up, index, scale=None, bias=None, out=None):
         if out.shape != shape[:-1] + (N,) or out.dtype is not dt:
             _bad("out has another shape or type than the result")
         out_ld = _row_stride(out, "out")
-    L = lib()
-    floats = M * rank
-    scratch = x.new_empty(floats, dtype=torch.float32)
+    L, t = lib(), _TYPE[dt]
+    floats, scratch = 0, None
+    if t == SD_BF16 and M * rank > 64:  # (fp32 and fewer need none)
+        floats = L.synerdiff_op_linear_adapters_scratch_floats(t, M, rank)
+        if floats > 0:
+            scratch = x.new_empty(floats, dtype=torch.float32)
     _enqueue(L.synerdiff_op_linear_adapters, x, (w, down, up, index, scale, bias, out),
-             (_TYPE[dt], x.data_ptr(), M, K, w.data_ptr(), N, down.data_ptr() if count else None,
-              up.data_ptr() if count else None, rank, count, _at(scale), index.data_ptr(), group, _at(bias), out.data_ptr(),
-              out_ld, scratch.data_ptr(), floats))
+             (t, x.data_ptr(), M, K, w.data_ptr(), N, down.data_ptr() if count else None, up.data_ptr() if count else None, rank,
+              count, _at(scale), index.data_ptr(), group, _at(bias), out.data_ptr(), out_ld, _at(scratch), floats))
     return out
