@@ -513,6 +513,20 @@ __global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 :
 }
 
 // ------------------------------------------------------------------ fp32
+// tanh to 3e-7 of it: from |x| = 0.6 on 1 - 2 / (1 + e^2|x|), below that x + x^3 (c1 +
+// c2 x^2 + ..) of least largest relative error (points of a Chebyshev grid, reweighted
+// by their errors until those are level).  A third of the library function's
+// instructions, which took half of a capped tile's time.
+__device__ __forceinline__ float tanh_f32(float x) {
+  constexpr float C1 = -0.33333298563957214f, C2 = 0.13331924378871918f, C3 = -0.053783830255270004f,
+                  C4 = 0.020795971155166626f, C5 = -0.005895158275961876f;
+  const float y = x * x, m = fabsf(x);
+  const float lo = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, C5, C4), C3), C2), C1), x);
+  const float e = __builtin_amdgcn_exp2f(m * (2.f * LOG2E));
+  const float hi = copysignf(fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + e), 1.f), x);
+  return m < 0.6f ? lo : hi;  // (NaN takes the second)
+}
+
 // The same on fp32 MFMAs (32 x 32 x 2), tiles of 32 keys.  Channels are summed in
 // the order that makes a lane's share of them four consecutive ones (half lh
 // takes 8 i + 4 lh + [0, 4)); a key's probability meets its V row straight from the
@@ -566,6 +580,7 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextAr
   const float* V = (const float*)a.v + tx.v0 + p.g * a.v_head;
   f32x4 rk[CPT], rv[CPT];
   float rb = 0.f;
+  auto far_of = [&](int k0) { return k0 - b0 + min(tid, KT + TQ - 2) - (TQ - 1); };
   auto fetch = [&](int k0, uint32_t bits) __attribute__((always_inline)) {
     const int n = min(KT, k_end - k0);
     const __amdgpu_buffer_rsrc_t kr = make_rsrc(K + (long)k0 * a.k_ld, ((n - 1) * (long)a.k_ld + d) * 4);
@@ -577,10 +592,7 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextAr
       rk[i] = __builtin_bit_cast(f32x4, buf_load16(kr, on ? (key * (int)a.k_ld + c) * 4 : OOB));
       rv[i] = __builtin_bit_cast(f32x4, buf_load16(vr, on ? (key * (int)a.v_ld + c) * 4 : OOB));
     }
-    if (terms && tid < KT + TQ - 1) {
-      const int far = k0 - b0 + tid - (TQ - 1);
-      rb = term_of(table_at(a, p.h, far), far, slope, 1.f);
-    }
+    if (terms) rb = table_at(a, p.h, far_of(k0));  // (and `stage` makes the term of it, behind the products)
   };
   auto stage = [&](int b, int k0, int slot) __attribute__((always_inline)) {
     const bool border = a.causal && k0 + KT > max(b0 + 1, tx.prefix);
@@ -598,41 +610,46 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextAr
           }
       *(f32x4*)&Vs[b][key * LDV + c] = v;
     }
-    if (terms && tid < KT + TQ - 1) strip[b][tid] = rb;
+    if (terms && tid < KT + TQ - 1) strip[b][tid] = term_of(rb, far_of(k0), slope, 1.f);
   };
-  auto own_key = [&](int k0) -> bool {
-    const int k = k0 + lq;
-    return k < k_end && (!mask || mask[k]);
-  };
+  const __amdgpu_buffer_rsrc_t mr = make_rsrc(mask, k_end);
+  auto own_mask = [&](int k0) -> int { return mask ? (int)__builtin_amdgcn_raw_buffer_load_b8(mr, k0 + lq, 0, 0) : 1; };
+  auto ballot = [&](int k0, int own) -> uint32_t { return (uint32_t)__ballot(k0 + lq < k_end && own); };
   const int sb = TQ - 1 - wave * 32 - lq + 4 * lh;
   if (k_end > 0) {
-    uint32_t bits = (uint32_t)__ballot(own_key(0));
+    int own = own_mask(0);
+    uint32_t bits = ballot(0, own);
+    own = own_mask(KT);
     fetch(0, bits);
-    bool nk = own_key(KT);
     stage(0, 0, 0);
     __syncthreads();
     for (int k0 = 0, b = 0, slot = 0; k0 < k_end; k0 += KT, b ^= 1) {
       uint32_t next = 0;
       const bool more = k0 + KT < k_end;
       if (more) {
-        next = (uint32_t)__ballot(nk);
+        next = ballot(k0 + KT, own);
+        own = own_mask(k0 + 2 * KT);
         fetch(k0 + KT, next);
-        nk = own_key(k0 + 2 * KT);
       }
       const int s1 = slot == 2 ? 0 : slot + 1;
       if (bits && k0 < lim_hi && r0 < tx.len) {
+        // (fragments ahead of their products where registers allow; channels from d on are zeros)
         f32x16 s = {};
+        constexpr int AHEAD = D32 <= 128 ? NI : 4;
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          if (8 * i >= d) break;
-          const f32x4 kf = *(const f32x4*)&Ks[b][lq * LDK + 8 * i + 4 * lh];
+        for (int i0 = 0; i0 < NI; i0 += AHEAD) {
+          f32x4 kf[AHEAD];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s = mfma_f32(kf[e], qf[i][e], s);
+          for (int i = 0; i < AHEAD; ++i) kf[i] = *(const f32x4*)&Ks[b][lq * LDK + 8 * (i0 + i) + 4 * lh];
+#pragma unroll
+          for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = mfma_f32(kf[i][e], qf[i0 + i][e], s);
         }
         // register i: key 8 (i / 4) + 4 lh + i % 4
         if (a.cap > 0.f)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = c_out * tanhf(s[i]);
+          for (int i = 0; i < 16; ++i) s[i] = c_out * tanh_f32(s[i]);
         if (terms)
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] += strip[b][sb + 8 * (i >> 2) + (i & 3)];
