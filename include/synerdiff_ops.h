@@ -302,11 +302,11 @@ sd_status synerdiff_op_cross_attention(int32_t dtype, const void* d_q, int64_t q
  * 1 they become 0 (padded: all rows past the lengths; packed: those before
  * start[0], from start[n] on, and past a text's first max_len).
  * Constraints: d a multiple of 8, <= 256; heads a multiple of kv_heads, <=
- * 2^16; max_len <= 2^30; q_ld, k_ld, v_ld, o_ld <= 2^23; scale 0 or 2^-60 to
- * 2^60 in size, cap 0 or 2^-20 to 2^60; reach <= 2^24; a grid of less than 2^32 threads (a block of
- * 256 per 128 queries of a head); q, k, v, o and their strides at multiples
- * of 16 bytes.  o overlaps nothing.  No workspace.  n = 0 does nothing.  The
- * bits of a query depend on its own text alone. */
+ * 2^16; n kv_heads <= 2^19 - 8; max_len <= 2^30; q_ld, k_ld, v_ld, o_ld <= 2^23;
+ * scale 0 or 2^-60 to 2^60 in size, cap 0 or 2^-20 to 2^60; reach <= 2^24; a grid
+ * of less than 2^32 threads (256 per 128 queries of a head, in chunks of 8); q,
+ * k, v, o and their strides at multiples of 16 bytes.  o overlaps nothing.  No
+ * workspace.  n = 0 does nothing.  The bits of a query depend on its own text alone. */
 sd_status synerdiff_op_text_attention(int32_t dtype, const void* d_q, int64_t q_ld, int64_t q_head, int64_t q_text,
                                       const void* d_k, int64_t k_ld, int64_t k_head, int64_t k_text, const void* d_v,
                                       int64_t v_ld, int64_t v_head, int64_t v_text, void* d_o, int64_t o_ld,
@@ -326,8 +326,9 @@ sd_status synerdiff_op_text_attention(int32_t dtype, const void* d_q, int64_t q_
  * count) has no adapter (count may be 0, down and up NULL then).  A row depends
  * on no other row and on no other adapter than its own, whatever they hold.
  * Narrower adapters are padded with zeros.  Sums are fp32; v is fp32 for fp32
- * and for up to 64 rows, else held to 2^-17 of it (two bf16 parts; below 2^-110
- * less).  Any order of indices is right; runs of 32 rows or more of one adapter are fast.
+ * and for up to 32 rows (64 up to K = 2048), else held to 2^-17 of it (two bf16
+ * parts; below 2^-110 less).  Any order of indices is right; runs of 32 rows or
+ * more of one adapter are fast.
  * Constraints: K, N, rank multiples of 8; K, N <= 2^20, rank <= 1024; w, up[c] and
  * down[c] below 2^31 bytes; M <= 2^26, M N < 2^35, M rank < 2^33; all
  * buffers and rows of out at multiples of 16 bytes (scale, index: 4).  out

@@ -5,10 +5,10 @@
 //  * Many rows (bf16): v on MFMAs; then the GEMM of gemm.hip, whose accumulators
 //    start with the adapters' part.  v is kept as two bf16 parts (2^-17 of it), so
 //    that the second product is one of bf16 MFMAs too.
-//  * Few rows (bf16, at most 64): bound by the bytes of W and of the adapters in use.
+//  * Few rows (at most 64): bound by the bytes of W and of the adapters in use.
 //    A block has 16 outputs of all rows, its waves share out K.  v is fp32; up to
 //    64 values of it every block makes for itself, in one launch.
-//  * fp32: the adapters' part goes to `out` first and is the GEMM's residual.
+//  * Many rows, fp32: the adapters' part goes to `out` first and is the GEMM's residual.
 // A row sees its own adapter only: what others hold, infinities and NaN included,
 // does not reach it.
 #include <string.h>
@@ -32,6 +32,8 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 x, bf16x8 y, f32x16 c) {
   return c;
 #endif
 }
+// c + x y^T of 16 bytes a lane: row lane % 16, of 16 bytes' k values times 4 the
+// lane / 16-th.  (fp32: the products take one element of every lane at a time.)
 __device__ __forceinline__ f32x4 mfma16(bf16x8 x, bf16x8 y, f32x4 c) {
 #if defined(__HIP_DEVICE_COMPILE__)
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
@@ -39,6 +41,16 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 x, bf16x8 y, f32x4 c) {
   return c;
 #endif
 }
+__device__ __forceinline__ f32x4 mfma16(f32x4 x, f32x4 y, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+#endif
+  return c;
+}
+template <typename T> struct Piece;  // 16 bytes
+template <> struct Piece<bf16> { typedef bf16x8 type; };
+template <> struct Piece<float> { typedef f32x4 type; };
 
 }  // namespace
 
@@ -69,12 +81,13 @@ __device__ __forceinline__ float4 down_four(const LinearAdaptersArgs& a, int m, 
   return make_float4(s[0] * f, s[1] * f, s[2] * f, s[3] * f);
 }
 
+template <typename T>
 __global__ __launch_bounds__(256) void adapters_down_rows_kernel(LinearAdaptersArgs a) {
   const int per = a.rank / 4, lane = threadIdx.x & 63, id = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (id >= a.M * per) return;
   const int m = id / per, r0 = (id - m * per) * 4, c = adapter_of(a, m);
   if (c < 0) return;  // (its v is not read)
-  const float4 v = down_four<bf16>(a, m, c, r0, lane);
+  const float4 v = down_four<T>(a, m, c, r0, lane);
   if (lane == 0) *(float4*)(a.scratch + (long)m * a.rank + r0) = v;
 }
 
@@ -195,34 +208,36 @@ __global__ __launch_bounds__(256, 2) void adapters_down_kernel(LinearAdaptersArg
   }
 }
 
-// ------------------------------------------------------------------ few rows, bf16
-// A block has 16 outputs of all rows (MT x 16), its 8 waves share out K 64 at a
-// time and are summed in order.  OWN: it makes v itself (at most OWN_V values), beside the others'
-// loads: 1 row, 1280 x 1280, rank 16 in one launch of 4.6 us against two of 2.9 and 4.3.
+// ------------------------------------------------------------------ few rows
+// A block has 16 outputs of all rows (MT x 16), its 8 waves share out K 128 bytes at
+// a time and are summed in order.  OWN: it makes v itself (at most OWN_V values),
+// beside the others' loads: 1 row, bf16 1280 x 1280, rank 16 in one launch of 5.9 us
+// (10.5 a call) against two of 2.9 and 4.3 (14.4 a call).
 constexpr int OWN_V = 64;
-template <int MT, bool OWN>
+template <typename T, int MT, bool OWN>
 __global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a) {
-  constexpr int NW = 8;
+  typedef typename Piece<T>::type P;
+  constexpr int NW = 8, E = 16 / sizeof(T), STEP = 4 * E, U = 2;  // elements of a piece; k of a product; products a turn
   __shared__ float part[NW][MT][256];
   __shared__ __attribute__((aligned(16))) float own_v[OWN ? OWN_V : 4];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, lk = 8 * (lane >> 4);
-  const int n0 = blockIdx.x * 16;
-  const __amdgpu_buffer_rsrc_t wr = make_rsrc((const bf16*)a.w + (long)n0 * a.K, (long)min(16, a.N - n0) * a.K * 2);
-  const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.x, (long)a.M * a.K * 2);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, lk = E * (lane >> 4);
+  const int n0 = blockIdx.x * 16, el = (int)sizeof(T);
+  const __amdgpu_buffer_rsrc_t wr = make_rsrc((const T*)a.w + (long)n0 * a.K, (long)min(16, a.N - n0) * a.K * el);
+  const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.x, (long)a.M * a.K * el);
   f32x4 acc[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int k0 = wave * 64; k0 < a.K; k0 += NW * 64) {
-    bf16x8 wv[2], xv[2][MT];
+  for (int k0 = wave * U * STEP; k0 < a.K; k0 += NW * U * STEP) {
+    P wv[U], xv[U][MT];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int k = k0 + 32 * j + lk;
-      wv[j] = buf_load16(wr, k < a.K ? (lr * a.K + k) * 2 : OOB);
+    for (int j = 0; j < U; ++j) {
+      const int k = k0 + STEP * j + lk;
+      wv[j] = __builtin_bit_cast(P, buf_load16(wr, k < a.K ? (lr * a.K + k) * el : OOB));
 #pragma unroll
-      for (int t = 0; t < MT; ++t) xv[j][t] = buf_load16(xr, k < a.K ? ((16 * t + lr) * a.K + k) * 2 : OOB);
+      for (int t = 0; t < MT; ++t) xv[j][t] = __builtin_bit_cast(P, buf_load16(xr, k < a.K ? ((16 * t + lr) * a.K + k) * el : OOB));
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < U; ++j)
 #pragma unroll
       for (int t = 0; t < MT; ++t) acc[t] = mfma16(wv[j], xv[j][t], acc[t]);  // (outputs 4 (lane / 16) + i of row lane % 16)
   }
@@ -233,7 +248,7 @@ __global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a
     for (int id = wave; id < a.M * per; id += NW) {
       const int m = id / per, r0 = (id - m * per) * 4, c = adapter_of(a, m);
       if (c < 0) continue;
-      const float4 v = down_four<bf16>(a, m, c, r0, lane);
+      const float4 v = down_four<T>(a, m, c, r0, lane);
       if (lane == 0) *(float4*)(own_v + m * a.rank + r0) = v;
     }
   }
@@ -248,7 +263,7 @@ __global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a
     const int c = adapter_of(a, m);
     if (c >= 0) {
       const float* v = OWN ? own_v + m * a.rank : a.scratch + (long)m * a.rank;
-      const bf16* u = (const bf16*)a.up + ((long)c * a.N + n) * a.rank;
+      const T* u = (const T*)a.up + ((long)c * a.N + n) * a.rank;
       for (int r = 0; r < a.rank; r += 8) {
         float uv[8], vv[8];
         load8f(u + r, uv);
@@ -257,24 +272,29 @@ __global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a
         for (int e = 0; e < 8; ++e) s = fmaf(uv[e], vv[e], s);
       }
     }
-    ((bf16*)a.out)[(long)m * a.out_ld + n] = (bf16)s;
+    ((T*)a.out)[(long)m * a.out_ld + n] = from_f<T>(s);
   }
 }
 
-// ------------------------------------------------------------------ fp32: the adapters' part
-// A block has 8 rows: their v to LDS, then a thread per output column of all 8; rows
-// of one adapter share the loads of its `up`.
+// ------------------------------------------------------------------ many rows, fp32: the adapters' part
+// A block has 8 rows, a thread per output column of all 8; rows of one adapter share
+// the loads of its `up`.  OWN: the block makes their v first (6144 x 320 x 320, rank
+// 8: 17 us, two launches of 7.4 and 10); else it comes from scratch, and blocks in y
+// share out the columns.
 constexpr int F32_ROWS = 8;
+template <bool OWN>
 __global__ __launch_bounds__(256) void adapters_f32_kernel(LinearAdaptersArgs a) {
   constexpr int MR = F32_ROWS;
-  extern __shared__ __attribute__((aligned(16))) float v[];  // [MR, rank]
+  extern __shared__ __attribute__((aligned(16))) float own_v[];  // [MR, rank]
   const int m0 = blockIdx.x * MR, rows = min(MR, a.M - m0), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = a.rank / 4;
-  for (int id = wave; id < rows * per; id += 4) {
-    const int i = id / per, r0 = (id - i * per) * 4, c = adapter_of(a, m0 + i);
-    if (c < 0) continue;
-    const float4 f = down_four<float>(a, m0 + i, c, r0, lane);
-    if (lane == 0) *(float4*)(v + i * a.rank + r0) = f;
-  }
+  const float* v = OWN ? own_v : a.scratch + (long)m0 * a.rank;
+  if constexpr (OWN)
+    for (int id = wave; id < rows * per; id += 4) {
+      const int i = id / per, r0 = (id - i * per) * 4, c = adapter_of(a, m0 + i);
+      if (c < 0) continue;
+      const float4 f = down_four<float>(a, m0 + i, c, r0, lane);
+      if (lane == 0) *(float4*)(own_v + i * a.rank + r0) = f;
+    }
   int c[MR], all = 0;
 #pragma unroll
   for (int i = 0; i < MR; ++i) {
@@ -282,7 +302,7 @@ __global__ __launch_bounds__(256) void adapters_f32_kernel(LinearAdaptersArgs a)
     all |= (c[i] >= 0) << i;
   }
   __syncthreads();
-  for (int n = threadIdx.x; n < a.N; n += 256) {
+  for (int n = blockIdx.y * 256 + threadIdx.x; n < a.N; n += 256 * gridDim.y) {
     float s[MR];
 #pragma unroll
     for (int i = 0; i < MR; ++i) s[i] = 0.f;
@@ -312,10 +332,14 @@ __global__ __launch_bounds__(256) void adapters_f32_kernel(LinearAdaptersArgs a)
 }
 
 // ------------------------------------------------------------------ launch
-constexpr int FEW = 64;  // rows of the few-row kernel
+constexpr int FEW = 64;  // rows the few-row kernel is built for
+// fp32 blocks make their own v once they fill the card (below that its rows take a
+// block long: 64 x 1280 rows of rank 128 some 40 us in 8 blocks)
+constexpr int OWN_ROWS = 256 * F32_ROWS;
 
 long linear_adapters_scratch_floats(DType dt, int M, int rank) {
-  return dt != BF16 || (M <= FEW && (long)M * rank <= OWN_V) ? 0 : (long)M * rank;
+  if (M <= FEW) return (long)M * rank <= OWN_V ? 0 : (long)M * rank;
+  return dt != BF16 && M >= OWN_ROWS ? 0 : (long)M * rank;
 }
 
 // 64 rows a block once that gives every CU one, else 32.  An index per row may bring
@@ -330,24 +354,30 @@ static void launch_down(const LinearAdaptersArgs& a, hipStream_t s) {
     adapters_down_kernel<2, RT><<<dim3((unsigned)((a.M + 63) / 64), y), 256, 0, s>>>(a);
 }
 
-template <int MT>
-static void launch_rows(const LinearAdaptersArgs& a, hipStream_t s) {
+template <typename T>
+static void launch_down_rows(const LinearAdaptersArgs& a, hipStream_t s) {
+  adapters_down_rows_kernel<T><<<dim3((unsigned)(((long)a.M * (a.rank / 4) + 3) / 4)), dim3(256), 0, s>>>(a);
+}
+
+template <typename T, int MT>
+static void launch_few(const LinearAdaptersArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((a.N + 15) / 16));
   if ((long)a.M * a.rank <= OWN_V)
-    adapters_rows_kernel<MT, true><<<grid, 512, 0, s>>>(a);
+    adapters_rows_kernel<T, MT, true><<<grid, 512, 0, s>>>(a);
   else {
-    adapters_down_rows_kernel<<<dim3((unsigned)(((long)a.M * (a.rank / 4) + 3) / 4)), dim3(256), 0, s>>>(a);
-    adapters_rows_kernel<MT, false><<<grid, 512, 0, s>>>(a);
+    launch_down_rows<T>(a, s);
+    adapters_rows_kernel<T, MT, false><<<grid, 512, 0, s>>>(a);
   }
+}
+template <typename T>
+static hipError_t launch_rows(const LinearAdaptersArgs& a, hipStream_t s) {
+  if (a.M <= 16) launch_few<T, 1>(a, s);
+  else if (a.M <= 32) launch_few<T, 2>(a, s);
+  else launch_few<T, 4>(a, s);
+  return hipGetLastError();
 }
 
 static hipError_t launch_bf16(const LinearAdaptersArgs& a, hipStream_t s) {
-  if (a.M <= FEW) {
-    if (a.M <= 16) launch_rows<1>(a, s);
-    else if (a.M <= 32) launch_rows<2>(a, s);
-    else launch_rows<4>(a, s);
-    return hipGetLastError();
-  }
   if (a.rank <= 32) launch_down<1>(a, s);
   else if (a.rank <= 64) launch_down<2>(a, s);
   else launch_down<4>(a, s);
@@ -386,7 +416,13 @@ static hipError_t launch_bf16(const LinearAdaptersArgs& a, hipStream_t s) {
 }
 
 static hipError_t launch_f32(const LinearAdaptersArgs& a, hipStream_t s) {
-  adapters_f32_kernel<<<dim3((unsigned)((a.M + F32_ROWS - 1) / F32_ROWS)), dim3(256), (unsigned)(F32_ROWS * a.rank * 4), s>>>(a);
+  const unsigned blocks = (unsigned)((a.M + F32_ROWS - 1) / F32_ROWS);
+  if (a.M >= OWN_ROWS) {
+    adapters_f32_kernel<true><<<dim3(blocks), 256, (unsigned)(F32_ROWS * a.rank * 4), s>>>(a);
+  } else {
+    launch_down_rows<float>(a, s);
+    adapters_f32_kernel<false><<<dim3(blocks, (unsigned)((a.N + 255) / 256)), 256, 0, s>>>(a);
+  }
   GemmArgs g;
   memset(&g, 0, sizeof(g));
   g.M = a.M;
@@ -413,6 +449,9 @@ static hipError_t launch_f32(const LinearAdaptersArgs& a, hipStream_t s) {
 
 hipError_t launch_linear_adapters(DType dt, const LinearAdaptersArgs& a, hipStream_t s) {
   if (a.M <= 0 || a.N <= 0) return hipSuccess;
+  // (33 to 64 rows of more than 2048 bf16 channels are better off in tiles: 64 x 4096
+  // x 4096 18 us against 23; 64 x 1280 x 1280 13.5 against 13.2)
+  if (a.M <= 32 || (a.M <= FEW && (dt != BF16 || a.K <= 2048))) return dt == BF16 ? launch_rows<bf16>(a, s) : launch_rows<float>(a, s);
   return dt == BF16 ? launch_bf16(a, s) : launch_f32(a, s);
 }
 

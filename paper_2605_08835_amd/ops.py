@@ -466,7 +466,7 @@ def linear_adapters(x, w, down, up, index, scale=None, bias=None, out=None):
         out_ld = _row_stride(out, "out")
     L, t = lib(), _TYPE[dt]
     floats, scratch = 0, None
-    if t == SD_BF16 and M * rank > 64:  # (fp32 and fewer need none)
+    if M * rank > 64:  # (fewer need none)
         floats = L.synerdiff_op_linear_adapters_scratch_floats(t, M, rank)
         if floats > 0:
             scratch = x.new_empty(floats, dtype=torch.float32)

@@ -207,6 +207,20 @@ def test_text_attention_texts_do_not_depend_on_their_batch(ops, mode, dt):  # no
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 48, 64, 96, 192])
+def test_text_attention_bits_do_not_depend_on_the_longest_text(ops, d, dt):  # noqa: F811
+    """Texts of up to 128 tokens alone, and with a max_len (or a text) past that."""
+    q, k, v, hi, kw, texts = _case(d, dt, 2, 2, d, [128, 70, 64, 5], reach=20, mask=0.2)
+    for mode in (dict(), dict(causal=True), dict(causal=True, cap=9.0)):
+        first = ops.text_attention(q, k, v, hi, **kw, **mode)
+        _check(first, q, k, v, texts, dt, f"{(d, dt, mode)}", **kw, **mode)
+        for most in (129, 300):
+            assert torch.equal(ops.text_attention(q, k, v, most, **kw, **mode), first), (most, mode)
+        free = {i: kw[i] for i in kw if i != "bias"}
+        assert torch.equal(ops.text_attention(q, k, v, hi, **free, **mode), ops.text_attention(q, k, v, 300, **free, **mode)), mode
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_text_attention_layouts(ops, dt):  # noqa: F811
     """Pieces of one projection, shared heads of stride 0, masks as bytes."""
     q, k, v, hi, kw, texts = _case(8, dt, 4, 2, 40, [90, 33], mask=0.2, pad=True)
