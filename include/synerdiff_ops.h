@@ -290,7 +290,8 @@ sd_status synerdiff_op_cross_attention(int32_t dtype, const void* d_q, int64_t q
  * any weight gives zeros.  A finite bias, lowest value of fp32 included, stays
  * finite: a query whose keys all have it weighs them alike.  Scores, sums and
  * results are fp32 until the result is rounded to dtype; bf16 probabilities
- * are rounded to bf16 (by up to 2^-8 of each) and summed as rounded.
+ * are rounded to bf16 (by up to 2^-8 of each) and summed as rounded, and capped bf16
+ * scores are right to 2^-21 of the cap.
  * Layouts (strides in elements, 0 or more; that of an axis of one element is
  * not looked at).  Packed texts (d_start not NULL, int32 [n + 1], not
  * decreasing): text c is rows start[c] .. start[c + 1] - 1 of [tokens], cut at
@@ -303,7 +304,7 @@ sd_status synerdiff_op_cross_attention(int32_t dtype, const void* d_q, int64_t q
  * start[0], from start[n] on, and past a text's first max_len).
  * Constraints: d a multiple of 8, <= 256; heads a multiple of kv_heads, <=
  * 2^16; n kv_heads <= 2^19 - 8; max_len <= 2^30; q_ld, k_ld, v_ld, o_ld <= 2^23;
- * scale 0 or 2^-60 to 2^60 in size, cap 0 or 2^-20 to 2^60; reach <= 2^24; a grid
+ * scale 0 or 2^-60 to 2^60 in size, cap 0 or 2^-20 to 2^12; reach <= 2^24; a grid
  * of less than 2^32 threads (256 per 128 queries of a head, in chunks of 8); q,
  * k, v, o and their strides at multiples of 16 bytes.  o overlaps nothing.  No
  * workspace.  n = 0 does nothing.  The bits of a query depend on its own text alone. */

@@ -97,7 +97,10 @@ __global__ __launch_bounds__(256) void adapters_down_rows_kernel(LinearAdaptersA
 // the one that is multiplied; MW waves have 32 rows each, the rest share out a tile's
 // k and are summed at the end.  v's two parts go to scratch, [M, rank] each.
 // Chunk c (16 bytes) of a tile's row r lies in slot c ^ (r / 2 % 8): fragment reads of
-// 16 rows are spread over all banks.
+// 16 rows are spread over all banks.  Bound by x's bytes: 196608 x 320, rank 16 20.5 us,
+// 6.1 TB/s (partly from the cache behind the L2s); 16384 x 1280, rank 128 19 us, where every
+// 64 rows read the adapter anew.  Fragments straight from memory, 32 bytes a row at a
+// time, took 33 and 44 us.
 template <int MW, int RT>
 __global__ __launch_bounds__(256, 2) void adapters_down_kernel(LinearAdaptersArgs a) {
   constexpr int NW = 4, KW = NW / MW, BM = 32 * MW, BR = 32 * RT, NS = 3, XI = MW, DI = RT, LPT = XI + DI, STAGE = (BM + BR) * 64;
@@ -278,9 +281,9 @@ __global__ __launch_bounds__(512) void adapters_rows_kernel(LinearAdaptersArgs a
 
 // ------------------------------------------------------------------ many rows, fp32: the adapters' part
 // A block has 8 rows, a thread per output column of all 8; rows of one adapter share
-// the loads of its `up`.  OWN: the block makes their v first (6144 x 320 x 320, rank
-// 8: 17 us, two launches of 7.4 and 10); else it comes from scratch, and blocks in y
-// share out the columns.
+// the loads of its `up`.  OWN: the block makes their v first; else it comes from
+// scratch, and blocks in y share out the columns.  Bound by latencies one after another
+// (index, x and down, up): 6144 x 320 x 320, rank 8 17 us for 8 MB of `out`.
 constexpr int F32_ROWS = 8;
 template <bool OWN>
 __global__ __launch_bounds__(256) void adapters_f32_kernel(LinearAdaptersArgs a) {
@@ -333,22 +336,27 @@ __global__ __launch_bounds__(256) void adapters_f32_kernel(LinearAdaptersArgs a)
 
 // ------------------------------------------------------------------ launch
 constexpr int FEW = 64;  // rows the few-row kernel is built for
-// fp32 blocks make their own v once they fill the card (below that its rows take a
-// block long: 64 x 1280 rows of rank 128 some 40 us in 8 blocks)
-constexpr int OWN_ROWS = 256 * F32_ROWS;
+// fp32 blocks make their own v where they fill the card and the ranks are low, else a
+// launch of its own does (whole calls, us, own and two launches: 65 x 1280 x 1280, rank
+// 128 180 and 58; 1024 x 320 x 320, rank 8 22.7 and 20.8; 2048 rows 29.9 and 29.4, 6144
+// 39.9 and 42.1; 2048 x 1280 x 640, rank 64 160 and 141).
+static bool f32_own(int M, int rank) { return M >= 256 * F32_ROWS && rank <= 16; }
 
 long linear_adapters_scratch_floats(DType dt, int M, int rank) {
   if (M <= FEW) return (long)M * rank <= OWN_V ? 0 : (long)M * rank;
-  return dt != BF16 && M >= OWN_ROWS ? 0 : (long)M * rank;
+  return dt != BF16 && f32_own(M, rank) ? 0 : (long)M * rank;
 }
 
-// 64 rows a block once that gives every CU one, else 32.  An index per row may bring
-// several adapters to a block: up to 4 blocks share them out then (runs of 1 to 77
-// rows, 1872 x 768, rank 16: 10.5 us alone).
+// 64 rows a block for many rows, else 32 (whole calls, us, 32 and 64: 8192 x 640, rank
+// 16 18.9 and 19.0; 12288 x 1280, rank 64 59.6 and 57.8; 32768 x 320, rank 128 58.9 and
+// 40.4; 4096 x 1280, rank 32 30.8 and 31.5).  An index per row may bring several
+// adapters to a block: 4 blocks share them out then (one, and four: 1872 x 768, rank 16,
+// in runs of 40 rows 15.9 and 13.1, in one run 12.6 and 12.5; 512 x 320, rank 32, every row
+// another 28.3 and 16.6).
 template <int RT>
 static void launch_down(const LinearAdaptersArgs& a, hipStream_t s) {
   const unsigned y = (unsigned)((a.rank + 32 * RT - 1) / (32 * RT));
-  if (a.M < 16384)
+  if (a.M <= 8192)
     adapters_down_kernel<1, RT><<<dim3((unsigned)((a.M + 31) / 32), y, a.group < 32 ? 4 : 1), 256, 0, s>>>(a);
   else
     adapters_down_kernel<2, RT><<<dim3((unsigned)((a.M + 63) / 64), y), 256, 0, s>>>(a);
@@ -417,7 +425,7 @@ static hipError_t launch_bf16(const LinearAdaptersArgs& a, hipStream_t s) {
 
 static hipError_t launch_f32(const LinearAdaptersArgs& a, hipStream_t s) {
   const unsigned blocks = (unsigned)((a.M + F32_ROWS - 1) / F32_ROWS);
-  if (a.M >= OWN_ROWS) {
+  if (f32_own(a.M, a.rank)) {
     adapters_f32_kernel<true><<<dim3(blocks), 256, (unsigned)(F32_ROWS * a.rank * 4), s>>>(a);
   } else {
     launch_down_rows<float>(a, s);

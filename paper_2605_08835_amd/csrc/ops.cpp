@@ -441,7 +441,7 @@ sd_status synerdiff_op_text_attention(int32_t dtype, const void* q, int64_t q_ld
   if (!(cap >= 0.f) || cap - cap != 0.f) return op_fail(SD_ERR_INVALID_ARG, "cap must be finite and not negative");
   const float mag = scale < 0.f ? -scale : scale;
   if (scale != 0.f && (mag < 0x1p-60f || mag > 0x1p60f)) return op_fail(SD_ERR_UNSUPPORTED, "scale outside 2^-60 .. 2^60");
-  if (cap != 0.f && (cap < 0x1p-20f || cap > 0x1p60f)) return op_fail(SD_ERR_UNSUPPORTED, "cap outside 2^-20 .. 2^60");
+  if (cap != 0.f && (cap < 0x1p-20f || cap > 0x1p12f)) return op_fail(SD_ERR_UNSUPPORTED, "cap outside 2^-20 .. 2^12");
   if (bias ? reach < 0 || reach > 1 << 24 : reach != 0)
     return op_fail(SD_ERR_INVALID_ARG, "reach is that of a bias, 0 to 2^24");
   if (n == 0 || (start ? tokens : (int64_t)max_len) == 0) return SD_OK;

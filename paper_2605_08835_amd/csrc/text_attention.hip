@@ -144,7 +144,14 @@ __device__ __forceinline__ int v_swz(int r) {
 // SHORT: no text is longer than the two tiles that LDS holds.  They are loaded at
 // once and nothing waits afterwards; a block is as long as its chain of latencies,
 // so four blocks share a CU where registers allow, which leaves fewer for fragments
-// read ahead.  The sums are the same.
+// read ahead.  The sums are the same.  (48 prompts of 5 to 77 tokens, 20 heads, this
+// form and the other, us: 32 channels 8.0 and 12.4, 64 10.9 and 17.0, 128 17.3 and
+// 30.3; 64 texts of 128 tokens 23.0 and 27.3.)
+// What bounds it: a wave's vector instructions (some 9 a score without a cap, 12 with,
+// the exponentials two turns each) and its products one after the other, which only
+// other waves overlap: 6 documents of 500 to 8192 tokens, 16 heads of 128, capped 960 us,
+// 660 TFLOP/s, vector ALU busy 55 %, matrix unit 30 %; 12 texts of 700 to 2500, 10 heads
+// of 80 140 us, 450 TFLOP/s.  Waiting for every fragment where it is used took 1155 and 174.
 template <int D16, bool BIAS, bool CAP, bool SHORT>
 __global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 : 1) void text_bf16_kernel(TextArgs a) {
   constexpr int NW = 4, KT = 64, NJ = D16 / 16, ND = (D16 + 31) / 32, CH = D16 / 8, NI = (CH + NW - 1) / NW, LDR = D16 + 8;
@@ -371,10 +378,12 @@ __global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 :
             for (int j = 0; j < NJ; ++j) kf[kt][j] = k_frag(Kb, kt, j);
           start(s, t, bits);
           if constexpr (!SHORT) __builtin_amdgcn_sched_barrier(0);
+          __builtin_amdgcn_s_setprio(1);  // (before the other waves' softmax: 1133 -> 1118 us on long capped documents)
 #pragma unroll
           for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) s[kt] = mfma32(kf[kt][j], qf[j], s[kt]);
+          __builtin_amdgcn_s_setprio(0);
         }
         bf16x8 vf[2][ND];
 #pragma unroll
@@ -531,6 +540,8 @@ __device__ __forceinline__ float tanh_f32(float x) {
 // the order that makes a lane's share of them four consecutive ones (half lh
 // takes 8 i + 4 lh + [0, 4)); a key's probability meets its V row straight from the
 // register it was computed in, since the two k of an MFMA are the two lane halves' keys.
+// Few texts wait for the tiles of the longest one, a wave's 32 products of 64 cycles
+// a tile at 32 channels: 6 texts of 8 to 231 tokens, 8 heads of 32, capped 24 us.
 template <int D32>
 __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextArgs a) {
   constexpr int NW = 4, KT = 32, NI = D32 / 8, ND = D32 / 32, NT = 64 * NW, LDK = D32 + 4, LDV = D32 + 8;  // (rows apart by banks)
@@ -744,6 +755,7 @@ static void launch_kind(const TextArgs& a, dim3 grid, hipStream_t s) {
 }
 template <int D16>
 static void launch_width(const TextArgs& a, dim3 grid, hipStream_t s) {
+  // (both sides measured: see the kernel)
   if (a.max_len <= 128) launch_kind<D16, true>(a, grid, s);
   else launch_kind<D16, false>(a, grid, s);
 }
@@ -751,7 +763,7 @@ static void launch_width(const TextArgs& a, dim3 grid, hipStream_t s) {
 // The grid of a call (x = 0 past its limits), and how it is dealt (a.chunk, a.chunks).
 static dim3 grid_of(TextArgs& a) {
   const long tiles = a.max_len < 1 ? 1 : ((long)a.max_len + TQ - 1) / TQ;  // (packed rows of no text may still be due zeros)
-  a.chunk = (int)(tiles < 8 ? tiles : 8);
+  a.chunk = (int)(tiles < 8 ? tiles : 8);  // (1, 8, 32: 16 x 512 tokens, 20 heads of 64 39.3, 36.3, 37.4 us; 4 x 4000 426, 406, 402)
   a.chunks = (int)((tiles + a.chunk - 1) / a.chunk);
   const long y = ((long)a.n * a.kv_heads + 7) / 8, x = 8L * a.chunk * a.rep;
   if (y > 65535 || a.chunks > 65535 || (double)x * y * a.chunks * 256 > 4.0e9) return dim3(0);

@@ -44,7 +44,7 @@ ON = dict(n=3)
     (dict(tokens=-1), -1, "token"), (dict(tokens=1 << 31), -1, "token"), (dict(length=A[9]), -1, "lengths"),
     (dict(causal=0), -1, "prefix"), (dict(scale=NAN), -1, "scale"), (dict(scale=-INF), -1, "scale"),
     (dict(scale=1e-30), -2, "scale"), (dict(scale=-1e30), -2, "scale"), (dict(cap=-1.0), -1, "cap"), (dict(cap=NAN), -1, "cap"),
-    (dict(cap=INF), -1, "cap"), (dict(cap=1e-9), -2, "cap"), (dict(reach=-1), -1, "reach"), (dict(reach=(1 << 24) + 1), -1, "reach"),
+    (dict(cap=INF), -1, "cap"), (dict(cap=1e-9), -2, "cap"), (dict(cap=4097.0), -2, "cap"), (dict(reach=-1), -1, "reach"), (dict(reach=(1 << 24) + 1), -1, "reach"),
     (dict(bias=None), -1, "reach"),
     (dict(ON, q_ld=(1 << 23) + 8), -2, "2^23"), (dict(ON, q=None), -1, "NULL"), (dict(ON, k=None), -1, "NULL"),
     (dict(ON, v=None), -1, "NULL"), (dict(ON, o=None), -1, "NULL"), (dict(ON, q_ld=196), -1, "16 bytes"),
@@ -87,7 +87,7 @@ def test_linear_adapters_refusals(lib, over, status, word):
 def test_linear_adapters_scratch(lib):
     f = lib.synerdiff_op_linear_adapters_scratch_floats
     assert f(BF16, 8, 8) == 0 and f(BF16, 9, 8) == 72 and f(BF16, 100, 16) == 1600 and f(F32, 64, 8) == 512
-    assert f(F32, 4, 16) == 0 and f(F32, 65, 8) == 520 and f(F32, 1 << 20, 8) == 0 and f(BF16, 1 << 20, 8) == 1 << 23
+    assert f(F32, 4, 16) == 0 and f(F32, 65, 8) == 520 and f(F32, 1 << 20, 8) == 0 and f(F32, 1 << 20, 24) == 24 << 20 and f(F32, 2047, 8) == 16376 and f(BF16, 1 << 20, 8) == 1 << 23
     assert f(BF16, 0, 8) == 0 and f(2, 10, 16) == 0 and f(BF16, -3, 8) == 0
 
 
