@@ -369,7 +369,8 @@ def text_attention(q, k, v, max_len, start=None, length=None, mask=None, causal=
         _bad("q, k, v [tokens, heads, d] with start, [n, max_len, heads, d] without")
     heads, d = qshape[-2:]
     kv_heads = kshape[-2]
-    if k.dtype is not dt or v.dtype is not dt or kshape != v.shape or kshape[:-2] != qshape[:-2] or kshape[-1] != d:
+    if k.dtype is not dt or v.dtype is not dt or kshape != v.shape or kshape[0] != qshape[0] or kshape[-1] != d or (
+            not packed and kshape[1] != qshape[1]):
         _bad("k and v must have q's type, tokens and width, and one shape")
     qs, ks, vs = q.stride(), k.stride(), v.stride()
     if d > 1 and (qs[-1] != 1 or ks[-1] != 1 or vs[-1] != 1):
@@ -384,7 +385,7 @@ def text_attention(q, k, v, max_len, start=None, length=None, mask=None, causal=
         n, tokens, q_text, k_text, v_text = qshape[0], 0, qs[0], ks[0], vs[0]
         if qshape[1] != max_len:
             _bad("padded q, k, v must be [n, max_len, heads, d]")
-    _int32(max(n, tokens, heads, kv_heads, d, abs(max_len)))
+    _int32(n | tokens | heads | kv_heads | d | abs(max_len))
     start_p = _index(start, n + 1, "start") if packed else None
     length_p = _index(length, n, "length") if length is not None else None
     prefix_p = _index(prefix, n, "prefix") if prefix is not None else None
@@ -445,13 +446,14 @@ def linear_adapters(x, w, down, up, index, scale=None, bias=None, out=None):
     if K == 0:
         _bad("K must be above 0")
     M = x.numel() // K
-    _int32(max(M, K, N, count, rank))
+    _int32(M | K | N | count | rank)
     if index.dtype is not torch.int32 or not index.is_contiguous():
         _bad("index must be int32, contiguous")
-    if index.shape == shape[:-1]:
-        group = 1
-    elif index.shape == shape[:1]:
+    ishape = index.shape
+    if len(ishape) == 1 and ishape[0] == shape[0]:
         group = max(M // shape[0], 1) if shape[0] else 1
+    elif ishape == shape[:-1]:
+        group = 1
     else:
         _bad("index must have one entry per row of x, or per x[i]")
     if scale is not None and (scale.dtype is not torch.float32 or scale.shape != (count,) or not scale.is_contiguous()):
@@ -459,7 +461,7 @@ def linear_adapters(x, w, down, up, index, scale=None, bias=None, out=None):
     if bias is not None and (bias.dtype is not torch.float32 or bias.shape != (N,) or not bias.is_contiguous()):
         _bad("bias must be fp32 [N]")
     if out is None:
-        out, out_ld = x.new_empty(shape[:-1] + (N,)), N
+        out, out_ld = x.new_empty((M, N) if len(shape) == 2 else shape[:-1] + (N,)), N
     else:
         if out.shape != shape[:-1] + (N,) or out.dtype is not dt:
             _bad("out has another shape or type than the result")

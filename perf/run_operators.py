@@ -1,4 +1,5 @@
-"""Runs cases of `perf/operators.py` through the framework's kernels, for a profiler:
+"""Runs cases of `perf/operators.py` and `perf/more_operators.py` through the
+framework's kernels, for a profiler:
 
     rocprofv3 --kernel-trace --stats -f csv -d OUT -o n -- python3 perf/run_operators.py [NAME ...]
 
@@ -11,19 +12,20 @@ sys.path[:0] = [os.path.dirname(os.path.dirname(os.path.abspath(__file__)))]
 
 import torch  # noqa: E402
 
-from perf import operators  # noqa: E402
+from perf import more_operators, operators  # noqa: E402
 
 
 def main(names):
-    operators.own = True
-    for case in operators.listed():
-        if names and case["name"] not in names:
-            continue
-        states = [operators.prepare(case, seed) for seed in range(3)]
-        for i in range(30):
-            operators.run(states[i % 3])
-        torch.cuda.synchronize()
-        print(case["name"], flush=True)
+    for module in (operators, more_operators):
+        module.own = True
+        for case in module.listed():
+            if names and case["name"] not in names:
+                continue
+            states = [module.prepare(case, seed) for seed in range(3)]
+            for i in range(30):
+                module.run(states[i % 3])
+            torch.cuda.synchronize()
+            print(case["name"], flush=True)
 
 
 if __name__ == "__main__":
