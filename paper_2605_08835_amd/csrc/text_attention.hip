@@ -575,7 +575,7 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextAr
     for (int i = 0; i < NI; ++i) {
       const int c = 8 * i + 4 * lh;
       qf[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (r < tx.len && c < d) qf[i] = *(const f32x4*)(Q + c) * qs;
+      if (r < tx.len && c < d) qf[i] = *(const f32x4*)(Q + c);
     }
   }
   f32x16 o[ND];
@@ -644,8 +644,9 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextAr
       }
       const int s1 = slot == 2 ? 0 : slot + 1;
       if (bits && k0 < lim_hi && r0 < tx.len) {
-        // (fragments ahead of their products where registers allow; channels from d on are zeros)
-        f32x16 s = {};
+        // (fragments ahead of their products where registers allow; channels from d on are
+        // zeros; two sums, so that each is half as long a chain of roundings)
+        f32x16 s = {}, s2 = {};
         constexpr int AHEAD = D32 <= 128 ? NI : 4;
 #pragma unroll
         for (int i0 = 0; i0 < NI; i0 += AHEAD) {
@@ -655,8 +656,13 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextAr
 #pragma unroll
           for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s = mfma_f32(kf[i][e], qf[i0 + i][e], s);
+            for (int e = 0; e < 4; e += 2) {
+              s = mfma_f32(kf[i][e], qf[i0 + i][e], s);
+              s2 = mfma_f32(kf[i][e + 1], qf[i0 + i][e + 1], s2);
+            }
         }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (s[i] + s2[i]) * qs;
         // register i: key 8 (i / 4) + 4 lh + i % 4
         if (a.cap > 0.f)
 #pragma unroll
@@ -689,13 +695,22 @@ __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextAr
             for (int i = 0; i < 16; ++i) o[t][i] *= al;
         }
         const float ref = exp_ref(m_run);
+        // (a tile's sums are made apart and added: over the keys one after another, a long
+        // text's roundings would add up)
+        float lt = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float pr = __builtin_amdgcn_exp2f(s[i] - ref);
-          l += pr;
-          const float* vr = &Vs[b][(8 * (i >> 2) + 4 * lh + (i & 3)) * LDV + lq];
+          s[i] = __builtin_amdgcn_exp2f(s[i] - ref);
+          lt += s[i];
+        }
+        l += lt;
 #pragma unroll
-          for (int t = 0; t < ND; ++t) o[t] = mfma_f32(vr[32 * t], pr, o[t]);
+        for (int t = 0; t < ND; ++t) {
+          f32x16 ot = {};
+#pragma unroll
+          for (int i = 0; i < 16; ++i) ot = mfma_f32(Vs[b][(8 * (i >> 2) + 4 * lh + (i & 3)) * LDV + lq + 32 * t], s[i], ot);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[t][i] += ot[i];
         }
         if (a.causal && odd[slot]) {
 #pragma unroll 1
