@@ -286,8 +286,8 @@ sd_status synerdiff_op_cross_attention(int32_t dtype, const void* d_q, int64_t q
  * negative ones are 0).  Queries of masked tokens are computed like others.
  * Keys that take no part for any query of their text are not read, and what k
  * and v hold behind a query's causal border does not reach it, infinities and
- * NaN included.  Keys that score -inf take no weight; a query without a key of
- * any weight gives zeros.  A finite bias, lowest value of fp32 included, stays
+ * NaN included.  Keys that score -inf (a bias of -inf, say) take no weight, as
+ * long as their v is finite; a query without a key of any weight gives zeros.  A finite bias, lowest value of fp32 included, stays
  * finite: a query whose keys all have it weighs them alike.  Scores, sums and
  * results are fp32 until the result is rounded to dtype; bf16 probabilities
  * are rounded to bf16 (by up to 2^-8 of each) and summed as rounded, and capped bf16

@@ -303,10 +303,6 @@ __global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 :
         s[kt] = mfma32(off, ones, s[kt]);
       }
   };
-  // O^T += V^T P^T, 16 keys at a time: slot (lh, i) of slice u is key 16 u +
-  // 8 (i / 4) + 4 lh + i % 4, register 8 (u % 2) + i of half u / 2.  The
-  // probabilities are rounded to bf16 (by up to 2^-8 of each, half a step) and
-  // summed as rounded, so that the rounding cancels where one key prevails.
   // What was taken out of V, added for the queries that see it (a weight above 0 times it is itself).
   auto add_odd = [&](uint64_t bits, int k0) __attribute__((always_inline)) {
 #pragma unroll 1
@@ -465,6 +461,10 @@ __global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 :
           l_run = sum_probs(pf, l_run);
           return pf;
         };
+        // O^T += V^T P^T, 16 keys at a time: slot (lh, i) of slice u is key 16 u +
+        // 8 (i / 4) + 4 lh + i % 4, register 8 (u % 2) + i of half u / 2.  The
+        // probabilities are rounded to bf16 (by up to 2^-8 of each, half a step) and
+        // summed as rounded, so that the rounding cancels where one key prevails.
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const bf16x8 pf = probs(u);
