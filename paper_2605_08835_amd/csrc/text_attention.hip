@@ -541,7 +541,7 @@ __device__ __forceinline__ float tanh_f32(float x) {
 // takes 8 i + 4 lh + [0, 4)); a key's probability meets its V row straight from the
 // register it was computed in, since the two k of an MFMA are the two lane halves' keys.
 // Few texts wait for the tiles of the longest one, a wave's 32 products of 64 cycles
-// a tile at 32 channels: 6 texts of 8 to 231 tokens, 8 heads of 32, capped 24 us.
+// a tile at 32 channels: 6 texts of 8 to 231 tokens, 8 heads of 32, capped 25 us.
 template <int D32>
 __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextArgs a) {
   constexpr int NW = 4, KT = 32, NI = D32 / 8, ND = D32 / 32, NT = 64 * NW, LDK = D32 + 4, LDV = D32 + 8;  // (rows apart by banks)
