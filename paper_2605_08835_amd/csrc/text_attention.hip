@@ -115,6 +115,23 @@ __device__ __forceinline__ bool odd8(uint4 v) {  // an infinity or NaN among eig
 }
 __device__ __forceinline__ bool odd_f(float v) { return !(fabsf(v) < INFINITY); }
 
+__device__ __forceinline__ bool lanes(uint64_t bits) {  // this lane's bit
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_inverse_ballot_w64(bits);
+#else
+  return false;
+#endif
+}
+
+// The larger one, NaN if either is.
+__device__ __forceinline__ float larger(float a, float b) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_elementwise_maximum(a, b);
+#else
+  return a;
+#endif
+}
+
 }  // namespace
 
 // ------------------------------------------------------------------ bf16
@@ -283,25 +300,47 @@ __global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 :
     const bf16x4 lo = read_transposed(at), hi = read_transposed(at + 8 * D16);
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  bf16x8 ones = {};  // B operand of the masks: ones for k = 0
-  if (lh == 0) ones[0] = (bf16)1.0f;
+  // A masked key's score becomes -inf by a select, or (ADD) by a product that adds it,
+  // and by the select only in a wave that the sum leaves with a NaN: 0 times an infinite q
+  // and a term of +inf or NaN are in it.  (us, added and selected: 16 texts of 200 to 512,
+  // 20 heads of 64, no masks 30.1 and 29.4, masks 31.7 and 34.5, masks and bias 36.6 and 39.2;
+  // two causal texts of 3000 and 4000, 16 heads of 128 148 and 140, of 192 355 and 327, masks
+  // at 128 37.5 and 39.9; 8 heads of 256, 1500 and 2000 tokens 235 and 288; 48 prompts with
+  // masks, 20 heads of 64 12.0 and 10.2.)
+  constexpr bool ADD = !CAP && (D16 > 192 || (!SHORT && D16 <= 96));
+  bf16x8 ones = {};  // B operand of that product: ones for k = 0
+  if (ADD && lh == 0) ones[0] = (bf16)1.0f;
   const int sb = TQ - 1 - wave * 32 - lq + 4 * lh;  // strip's element at key 4 lh for this lane's query
 
   // Register r of half kt of a tile's scores: key 32 kt + 8 (r / 4) + 4 lh + r % 4.
-  // What they start from: the term by distance, and -inf for keys that take no part
+  // What they start from: the term by distance, and (ADD) -inf for masked keys
   // (one product of a column of 0 or -inf per key with a row of ones).
   auto start = [&](f32x16 (&s)[2], int b, uint64_t bits) __attribute__((always_inline)) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[kt][r] = BIAS && !CAP ? strip[b][sb + 32 * kt + 8 * (r >> 2) + (r & 3)] : 0.f;
-    if (!CAP && ~bits)
+    if (ADD && mask && ~bits)
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
         bf16x8 off = {};
         if (lh == 0) off[0] = __builtin_bit_cast(bf16, (unsigned short)(bits >> (32 * kt + lq) & 1 ? 0 : 0xFF80));
         s[kt] = mfma32(off, ones, s[kt]);
       }
+  };
+  // -inf for keys that the mask leaves out, whatever their scores became: a select each,
+  // whose lanes are made of two bits on the scalar unit.
+  auto leave_out = [&](f32x16 (&s)[2], uint64_t bits) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      const uint32_t w = (uint32_t)(bits >> (32 * kt));
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int c = 8 * (r >> 2) + (r & 3);
+        const uint32_t lo = (uint32_t)((int)(w << (31 - c)) >> 31), hi = (uint32_t)((int)(w << (27 - c)) >> 31);
+        s[kt][r] = lanes(lo | (uint64_t)hi << 32) ? s[kt][r] : -INFINITY;
+      }
+    }
   };
   // What was taken out of V, added for the queries that see it (a weight above 0 times it is itself).
   auto add_odd = [&](uint64_t bits, int k0) __attribute__((always_inline)) {
@@ -387,31 +426,39 @@ __global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 :
 #pragma unroll
           for (int i = 0; i < ND; ++i) vf[u][i] = v_frag(Vb, u, i);
         if constexpr (!SHORT) __builtin_amdgcn_sched_barrier(0);
-        const bool part = k0 + KT > lim_lo || (CAP && ~bits);
-        const bool late = CAP && !BIAS && !part;  // whole tiles without a term: the cap is taken with the exponents
+        const bool part = k0 + KT > lim_lo, gaps = mask && ~bits;
+        const bool late = CAP && !BIAS && !part && !gaps;  // whole tiles without a term: the cap is taken with the exponents
         if (CAP && !late)
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               s[kt][r] = capped(s[kt][r], BIAS ? c_out + strip[t][sb + 32 * kt + 8 * (r >> 2) + (r & 3)] : c_out);
-        // the causal border, and for capped scores the keys that take no part
+        // the causal border and the text's end
         if (part) {
           const int left = lim - k0 - 4 * lh;
-          const uint64_t w = bits >> (4 * lh);
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
               const int c = 32 * kt + 8 * (r >> 2) + (r & 3);
-              if (c >= left || (CAP && !(w >> c & 1))) s[kt][r] = -INFINITY;
+              if (c >= left) s[kt][r] = -INFINITY;
             }
         }
-        float v = s[0][0];
+        if (!ADD && gaps) leave_out(s, bits);
+        auto largest = [&] {
+          float v = s[0][0];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+          for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) v = fmaxf(v, s[kt][r]);
+            for (int r = 0; r < 16; ++r) v = ADD ? larger(v, s[kt][r]) : fmaxf(v, s[kt][r]);
+          return v;
+        };
+        float v = largest();
+        if (ADD && gaps && __any(v != v)) {
+          leave_out(s, bits);
+          v = largest();
+        }
         const float2 h = half_swap(v);
         float mt = fmaxf(h.x, h.y);
         if constexpr (!CAP) mt *= sl2;

@@ -308,3 +308,36 @@ def test_text_attention_streams_and_graphs(ops):  # noqa: F811
             for i in arrays:
                 kw[i].copy_(arrays[i])
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("wild", [math.inf, NAN])
+@pytest.mark.parametrize("n,d", [(77, 64), (128, 40), (200, 64), (150, 256)])
+def test_text_attention_masked_keys_with_any_bias(ops, n, d, wild, dt):  # noqa: F811
+    """A key that the mask leaves out takes no part, whatever the bias holds at its distance."""
+    far = n // 2  # keys from here on are masked, and to those alone lead distances of as much
+    q, k, v, hi, kw, texts = _case(n, dt, 2, 1, d, [n], reach=n)
+    kw["mask"] = torch.arange(n, device="cuda") < far
+    bias = kw["bias"].clone()
+    bias[:, n + far:] = wild
+    for cap in (None, 5.0):
+        for how in (dict(), dict(causal=True, prefix=torch.tensor([n], dtype=torch.int32, device="cuda"))):
+            clean = ops.text_attention(q, k, v, hi, cap=cap, **how, **kw)
+            _check(clean, q, k, v, texts, dt, f"{(n, d, dt, cap)}", cap=cap, **how, **kw)
+            got = ops.text_attention(q, k, v, hi, cap=cap, **how, **dict(kw, bias=bias))
+            assert torch.equal(got, clean), (cap, list(how))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d", [(77, 64), (128, 40), (200, 64), (150, 256)])
+def test_text_attention_masked_keys_and_an_infinite_query(ops, n, d, dt):  # noqa: F811
+    """A query whose seen keys all score -inf gives zeros; a masked key is none of them."""
+    q, k, v, hi, kw, texts = _case(n, dt, 2, 1, d, [n], mask=0.3)
+    k[..., 1] = -k[..., 1].abs() - 0.5
+    qb = q.clone()
+    qb[n - 3, :, 1] = math.inf
+    keep = torch.arange(n, device="cuda") != n - 3
+    for how in (dict(), dict(causal=True)):
+        clean = ops.text_attention(q, k, v, hi, **how, **kw)
+        got = ops.text_attention(qb, k, v, hi, **how, **kw)
+        assert torch.equal(got[keep], clean[keep]) and not got[n - 3].any(), list(how)
