@@ -35,6 +35,12 @@ __device__ inline void store8f(bf16* p, const float v[8]) {
   *reinterpret_cast<bf16x8*>(p) = a;
 }
 
+__device__ __forceinline__ bool odd8(uint4 v) {  // an infinity or NaN among eight bf16
+  auto two = [](uint32_t x) { return (x & 0x7F807F80u) + 0x00800080u; };  // (an exponent of ones carries into the sign's place)
+  return ((two(v.x) | two(v.y) | two(v.z) | two(v.w)) & 0x80008000u) != 0;
+}
+__device__ __forceinline__ bool odd_f(float v) { return !(fabsf(v) < INFINITY); }
+
 template <typename T> __device__ inline float to_f(T x) { return (float)x; }
 template <typename T> __device__ inline T from_f(float x) { return (T)x; }
 

@@ -709,16 +709,30 @@ __device__ __forceinline__ void adapter_products(const AdapterArgs& a, f32x16 (&
       bf16x8 b[TN];
 #pragma unroll
       for (int j = 0; j < TN; ++j) b[j] = buf_load16(br, kk < a.rank && nl + 32 * j < a.N ? ((nl + 32 * j) * a.rank + kk) * 2 : OOB);
+      bool looked = false, odd = false;
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
         if (!mine[i]) continue;
         const int at = kk < a.rank && ml + 32 * i < a.M ? ((ml + 32 * i) * a.rank + kk) * 2 : OOB;
         const bf16x8 h = buf_load16(hr, at), l = buf_load16(lor, at);
         const bool whole = mine[i] == ~0ull, on = id[i] == cur;
+        // An infinity in `up` meets v's first part alone: the second may be 0 or of the other sign.
+        if (!looked) {  // (behind the first loads of v)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) odd |= odd8(__builtin_bit_cast(uint4, b[j]));
+          odd = __any(odd);
+          looked = true;
+        }
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
           f32x16 t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j], h, acc[i][j], 0, 0, 0);
-          t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j], l, t, 0, 0, 0);
+          bf16x8 b2 = b[j];
+          if (odd) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (odd_f((float)b2[e])) b2[e] = (bf16)0.f;
+          }
+          t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b2, l, t, 0, 0, 0);
           if (whole) {
             acc[i][j] = t;
           } else {

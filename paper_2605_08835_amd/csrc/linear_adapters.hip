@@ -196,9 +196,10 @@ __global__ __launch_bounds__(256, 2) void adapters_down_kernel(LinearAdaptersArg
               bf16x4 h, l;
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
+                // (bf16's largest value is the first part of what lies past it; an infinity is whole in it)
                 const float v = acc[t][4 * q + e] * f;
-                h[e] = (bf16)v;
-                l[e] = (bf16)(v - (float)h[e]);
+                h[e] = (bf16)(odd_f(v) ? v : fminf(fmaxf(v, -0x1.FEp127f), 0x1.FEp127f));
+                l[e] = (bf16)(odd_f(v) ? 0.f : v - (float)h[e]);
               }
               *(bf16x4*)(hi + r) = h;
               *(bf16x4*)(lo + r) = l;

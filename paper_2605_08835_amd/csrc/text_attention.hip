@@ -109,12 +109,6 @@ __device__ __forceinline__ float term_of(float v, int far, float slope, float un
   return v * LOG2E / unit;
 }
 
-__device__ __forceinline__ bool odd8(uint4 v) {  // an infinity or NaN among eight bf16
-  auto two = [](uint32_t x) { return (x & 0x7F807F80u) + 0x00800080u; };  // (an exponent of ones carries into the sign's place)
-  return ((two(v.x) | two(v.y) | two(v.z) | two(v.w)) & 0x80008000u) != 0;
-}
-__device__ __forceinline__ bool odd_f(float v) { return !(fabsf(v) < INFINITY); }
-
 __device__ __forceinline__ bool lanes(uint64_t bits) {  // this lane's bit
 #if defined(__HIP_DEVICE_COMPILE__)
   return __builtin_amdgcn_inverse_ballot_w64(bits);

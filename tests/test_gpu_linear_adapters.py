@@ -178,3 +178,56 @@ def test_linear_adapters_streams_and_graphs(ops):  # noqa: F811
                 assert torch.equal(out, want[turn % 2])
             assert torch.equal(ops.linear_adapters(x, w, down, up, ix, scale=scale), want[turn % 2])
             torch.cuda.synchronize()
+
+
+def _same(got, y, tol, what):
+    """Infinities and NaN where the definition has them, the rest within `tol`."""
+    got, on = _np(got).reshape(y.shape), np.isfinite(y)
+    assert np.array_equal(got[~on], y[~on], equal_nan=True), what
+    assert np.isfinite(got[on]).all() and (np.abs(got - np.where(on, y, 0))[on] <= tol[on]).all(), what
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(5, 136, 200), (40, 136, 200), (300, 136, 200), (9000, 72, 320)])
+def test_linear_adapters_infinite_elements(ops, M, K, N, dt):  # noqa: F811
+    """One infinity in an adapter or in x gives infinities where the definition does, of its sign, and NaN nowhere."""
+    rank, count = 24, 3
+    x, w, down, up, scale, bias = _case(M, dt, M, K, N, rank, count)
+    x, w, down, up = (t.abs() + 0.25 for t in (x, w, down, up))  # (no sum has infinities of both signs)
+    x[0] = 0
+    x[0, 7] = 1  # (this row's v are single elements of `down`, so bf16 holds them)
+    index = np.arange(M, dtype=np.int32) % (count + 1) - 1
+    index[0] = 1
+    for name in ("down", "up", "x"):
+        for sign, sc in ((1, None), (-1, scale)):
+            t = dict(x=x.clone(), down=down.clone(), up=up.clone())
+            if name == "x":
+                t["x"][M - 1, 5] = sign * math.inf
+            else:
+                t[name][1, 5, 7] = sign * math.inf
+            got = ops.linear_adapters(t["x"], w, t["down"], t["up"], torch.from_numpy(index).cuda(), scale=sc, bias=bias)
+            clean = O.linear_adapters(_np(x), _np(w), _np(down), _np(up), index, None if sc is None else _np(sc), _np(bias))
+            with np.errstate(invalid="ignore"):
+                y = O.linear_adapters(_np(t["x"]), _np(w), _np(t["down"]), _np(t["up"]), index, None if sc is None else _np(sc),
+                                      _np(bias))[0]
+            y[np.isnan(y)] = sign * math.inf if name == "x" else np.nan  # (x's zero row has none)
+            tol = (K + 12) * U32 * clean[1] + ((K + rank + 12) * U32 + 2.0 ** -16) * clean[2]
+            tol = tol + (U16 if dt == "bf16" else U32) * (np.abs(clean[0]) + tol)
+            assert np.isinf(y).any()
+            _same(got, y, tol, f"{(M, K, N, dt, name, sign)}")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [8, 40, 300])
+def test_linear_adapters_largest_v(ops, M, dt):  # noqa: F811
+    """v between bf16's largest value and fp32's."""
+    K, N, rank = 16, 64, 16
+    x, w, down, up, _, _ = _case(M, dt, M, K, N, rank, 2)
+    x[:, :2], down[:] = 1, 0
+    down[0, 3, 0], down[0, 3, 1] = 3.3895e38, 1e36
+    down[1] = -down[0]
+    up /= 16
+    index = np.arange(M, dtype=np.int32) % 2
+    got = ops.linear_adapters(x, w, down, up, torch.from_numpy(index).cuda())
+    assert torch.isfinite(got).all()
+    _check(got, x, w, down, up, index, None, None, dt, f"{(M, dt)}")
