@@ -81,14 +81,18 @@ __device__ __forceinline__ float4 down_four(const LinearAdaptersArgs& a, int m, 
   return make_float4(s[0] * f, s[1] * f, s[2] * f, s[3] * f);
 }
 
+// (M rank / 4 is below 2^31.  The grid is bounded, since its threads in x have to stay
+// below 2^32: a wave takes several parts of many.)
+constexpr unsigned DOWN_BLOCKS = 1u << 20;
 template <typename T>
 __global__ __launch_bounds__(256) void adapters_down_rows_kernel(LinearAdaptersArgs a) {
-  const int per = a.rank / 4, lane = threadIdx.x & 63, id = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= a.M * per) return;
-  const int m = id / per, r0 = (id - m * per) * 4, c = adapter_of(a, m);
-  if (c < 0) return;  // (its v is not read)
-  const float4 v = down_four<T>(a, m, c, r0, lane);
-  if (lane == 0) *(float4*)(a.scratch + (long)m * a.rank + r0) = v;
+  const unsigned per = a.rank / 4, lane = threadIdx.x & 63, all = a.M * per;
+  for (unsigned id = blockIdx.x * 4 + (threadIdx.x >> 6); id < all; id += gridDim.x * 4) {
+    const int m = id / per, r0 = (id - m * per) * 4, c = adapter_of(a, m);
+    if (c < 0) continue;  // (its v is not read)
+    const float4 v = down_four<T>(a, m, c, r0, lane);
+    if (lane == 0) *(float4*)(a.scratch + (long)m * a.rank + r0) = v;
+  }
 }
 
 // ------------------------------------------------------------------ v, many rows
@@ -363,33 +367,39 @@ static void launch_down(const LinearAdaptersArgs& a, hipStream_t s) {
     adapters_down_kernel<2, RT><<<dim3((unsigned)((a.M + 63) / 64), y), 256, 0, s>>>(a);
 }
 
+// (What reads v is not launched where v was not.)
 template <typename T>
-static void launch_down_rows(const LinearAdaptersArgs& a, hipStream_t s) {
-  adapters_down_rows_kernel<T><<<dim3((unsigned)(((long)a.M * (a.rank / 4) + 3) / 4)), dim3(256), 0, s>>>(a);
+static hipError_t launch_down_rows(const LinearAdaptersArgs& a, hipStream_t s) {
+  const long blocks = ((long)a.M * (a.rank / 4) + 3) / 4;
+  adapters_down_rows_kernel<T><<<dim3(blocks < DOWN_BLOCKS ? (unsigned)blocks : DOWN_BLOCKS), dim3(256), 0, s>>>(a);
+  return hipGetLastError();
 }
 
 template <typename T, int MT>
-static void launch_few(const LinearAdaptersArgs& a, hipStream_t s) {
+static hipError_t launch_few(const LinearAdaptersArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((a.N + 15) / 16));
   if ((long)a.M * a.rank <= OWN_V)
     adapters_rows_kernel<T, MT, true><<<grid, 512, 0, s>>>(a);
   else {
-    launch_down_rows<T>(a, s);
+    const hipError_t e = launch_down_rows<T>(a, s);
+    if (e != hipSuccess) return e;
     adapters_rows_kernel<T, MT, false><<<grid, 512, 0, s>>>(a);
   }
+  return hipGetLastError();
 }
 template <typename T>
 static hipError_t launch_rows(const LinearAdaptersArgs& a, hipStream_t s) {
-  if (a.M <= 16) launch_few<T, 1>(a, s);
-  else if (a.M <= 32) launch_few<T, 2>(a, s);
-  else launch_few<T, 4>(a, s);
-  return hipGetLastError();
+  if (a.M <= 16) return launch_few<T, 1>(a, s);
+  if (a.M <= 32) return launch_few<T, 2>(a, s);
+  return launch_few<T, 4>(a, s);
 }
 
 static hipError_t launch_bf16(const LinearAdaptersArgs& a, hipStream_t s) {
   if (a.rank <= 32) launch_down<1>(a, s);
   else if (a.rank <= 64) launch_down<2>(a, s);
   else launch_down<4>(a, s);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   // (rows in parts whose offsets fit 32 bits)
   const long widest = a.K > a.rank ? a.K : a.rank;
   const long step = ((1L << 30) - 1) / widest / 256 * 256;
@@ -429,9 +439,12 @@ static hipError_t launch_f32(const LinearAdaptersArgs& a, hipStream_t s) {
   if (f32_own(a.M, a.rank)) {
     adapters_f32_kernel<true><<<dim3(blocks), 256, (unsigned)(F32_ROWS * a.rank * 4), s>>>(a);
   } else {
-    launch_down_rows<float>(a, s);
+    const hipError_t e = launch_down_rows<float>(a, s);
+    if (e != hipSuccess) return e;
     adapters_f32_kernel<false><<<dim3(blocks, (unsigned)((a.N + 255) / 256)), 256, 0, s>>>(a);
   }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   GemmArgs g;
   memset(&g, 0, sizeof(g));
   g.M = a.M;

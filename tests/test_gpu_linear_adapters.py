@@ -231,3 +231,28 @@ def test_linear_adapters_largest_v(ops, M, dt):  # noqa: F811
     got = ops.linear_adapters(x, w, down, up, torch.from_numpy(index).cuda())
     assert torch.isfinite(got).all()
     _check(got, x, w, down, up, index, None, None, dt, f"{(M, dt)}")
+
+
+def test_linear_adapters_v_past_2_28_values(ops):  # noqa: F811
+    """fp32 rows times rank past 2^28, so that v is made in more than one turn of its grid."""
+    M, K, N, rank = 262400, 8, 8, 1024
+    x, w, down, up, scale, bias = _case(12, "f32", M, K, N, rank, 3)
+    index = _order("runs", M, 3, 12)
+    got = ops.linear_adapters(x, w, down, up, torch.from_numpy(index).cuda(), scale=scale, bias=bias)
+    rows = np.unique(np.concatenate((np.arange(20), np.arange(M - 300, M), np.random.default_rng(2).integers(0, M, 300))))
+    at = torch.from_numpy(rows).cuda()
+    _check(got[at], x[at], w, down, up, index[rows], scale, bias, "f32", "v past 2^28")
+
+
+@pytest.mark.parametrize("K,N,rank", [(1032, 8, 8), (8, 1032, 24)])
+def test_linear_adapters_fp32_past_2_31_elements(ops, K, N, rank):  # noqa: F811
+    """x, or out, past 2^31 elements in fp32, v made by the blocks that use it and by a launch of its own."""
+    M, g = (1 << 21) + 300, _gen(5)
+    rows = np.unique(np.concatenate([np.arange(a - 3, a + 3) for a in (3, 1 << 20, (1 << 31) // 1032, 1 << 21, M - 3)]))
+    at = torch.from_numpy(rows).cuda()
+    x = torch.zeros(M, K, device="cuda")
+    x[at] = torch.randn(len(rows), K, generator=g, device="cuda")
+    _, w, down, up, scale, bias = _case(6, "f32", 1, K, N, rank, 3)
+    index = (torch.arange(M, device="cuda") // 100 % 4 - 1).to(torch.int32)
+    got = ops.linear_adapters(x, w, down, up, index, scale=scale, bias=bias)
+    _check(got[at], x[at], w, down, up, index[at].cpu().numpy(), scale, bias, "f32", f"{(K, N, rank)}")
