@@ -469,14 +469,17 @@ __global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 :
         }
         const float ref = exp_ref(m_run);
         // (the exponent is s sl2 - ref in one rounding; past 2^20 the one that ref
-        // holds of its own product would no longer be a small part of a step)
+        // holds of its own product would no longer be a small part of a step.  Each query by
+        // itself: another's ref may come from a key that this one does not see)
         float mul = sl2;
-        if (!CAP && __any(fabsf(ref) > 0x1p20f)) {
-          mul = 1.f;
+        const bool far = fabsf(ref) > 0x1p20f;
+        if (!CAP && __any(far)) {
+          const float by = far ? sl2 : 1.f;
+          mul = far ? 1.f : sl2;
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[kt][r] *= sl2;
+            for (int r = 0; r < 16; ++r) s[kt][r] *= by;
         }
         if constexpr (CAP) {
           if (late) {

@@ -341,3 +341,19 @@ def test_text_attention_masked_keys_and_an_infinite_query(ops, n, d, dt):  # noq
         clean = ops.text_attention(q, k, v, hi, **how, **kw)
         got = ops.text_attention(qb, k, v, hi, **how, **kw)
         assert torch.equal(got[keep], clean[keep]) and not got[n - 3].any(), list(how)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [math.inf, 1e30])
+@pytest.mark.parametrize("n", [128, 200])
+def test_text_attention_keys_behind_the_border_leave_the_bits(ops, n, value, dt):  # noqa: F811
+    """An infinite or huge key changes no bit of the queries before it, those of its own wave among them."""
+    q, k, v, hi, kw, texts = _case(n, dt, 4, 1, 64, [n])
+    q, k = 6 + q / 20, 8 + k / 20  # scores of some thousands, a few apart
+    at = n - 10
+    kb = k.clone()
+    kb[at, 0, 2] = value
+    clean = ops.text_attention(q, k, v, hi, causal=True, scale=1.0, **kw)
+    got = ops.text_attention(q, kb, v, hi, causal=True, scale=1.0, **kw)
+    assert torch.isfinite(clean).all() and torch.equal(got[:at], clean[:at])
+    assert not torch.equal(got[at:], clean[at:])
