@@ -99,9 +99,10 @@ __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, bf16* lds, int o
 
 // dma16 in asm, so that the compiler does not know of it: it cannot tell which LDS
 // reads the load concerns, and in the loops that use this one it waited for it at the
-// next one, a tile too early.  Whoever reads
-// waits (vmcnt 0, then a barrier); no register is written.  (The five wait states are
-// those between a vector instruction that wrote a resource word and its use here.)
+// next one, a tile too early.  Whoever reads waits (vmcnt 0, then a barrier).  m0, the
+// LDS address, is put back: the compiler does not let asm declare it as written, and
+// keeps one of its own for dma16.  (The five wait states are those between a vector
+// instruction that wrote a resource word and its use here.)
 typedef int rsrc4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ rsrc4 resource(const void* base, long bytes) {
   const uint64_t b = (uint64_t)base;
@@ -115,7 +116,9 @@ __device__ __forceinline__ rsrc4 resource(const void* base, long bytes) {
 __device__ __forceinline__ void to_lds16(rsrc4 r, bf16* to, int off) {
 #if defined(__HIP_DEVICE_COMPILE__)
   const int m = __builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) bf16*)to);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m), "v"(off), "s"(r) : "memory");
+  int keep;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(keep) : "s"(m), "v"(off), "s"(r) : "memory");
 #endif
 }
 
