@@ -256,3 +256,25 @@ def test_linear_adapters_fp32_past_2_31_elements(ops, K, N, rank):  # noqa: F811
     index = (torch.arange(M, device="cuda") // 100 % 4 - 1).to(torch.int32)
     got = ops.linear_adapters(x, w, down, up, index, scale=scale, bias=bias)
     _check(got[at], x[at], w, down, up, index[at].cpu().numpy(), scale, bias, "f32", f"{(K, N, rank)}")
+
+
+@pytest.mark.parametrize("M,K,N,rank", [(4, 8, 64, 8), (9, 8, 64, 8), (60, 16, 40, 16), (65, 8, 64, 8), (700, 8, 320, 16),
+                                        (3000, 8, 64, 8), (3000, 16, 64, 24)])
+def test_linear_adapters_fp32_v(ops, M, K, N, rank):  # noqa: F811
+    """fp32 layers keep v in fp32: the adapter's part is as near as its sums' roundings allow."""
+    x, w, down, up, scale, _ = _case(M + rank, "f32", M, K, N, rank, 3)
+    w.zero_()
+    index = _order("runs", M, 3, M)
+    got = _np(ops.linear_adapters(x, w, down, up, torch.from_numpy(index).cuda(), scale=scale))
+    y, _, t = O.linear_adapters(_np(x), _np(w), _np(down), _np(up), index, _np(scale))
+    # K, then rank, products and sums (fused or not, at most a rounding each), the scale, the sum with W x = 0 and the store
+    tol = (K + rank + 4) * U32 * t
+    _close(got, y, tol, f"{(M, K, N, rank)}")
+    if K > 8 or M < 60:
+        return
+    # (two bf16 parts of v, off by up to 2^-17 of it, would not pass at these sizes: 28 U32 at most is below 2^-19)
+    v = np.stack([_np(scale)[c] * (_np(down)[c] @ r) if c >= 0 else np.zeros(rank) for c, r in zip(index, _np(x))])
+    hi = torch.from_numpy(v).float().bfloat16().double().numpy()
+    parts = hi + torch.from_numpy(v - hi).float().bfloat16().double().numpy()
+    z = np.stack([_np(up)[c] @ p if c >= 0 else np.zeros(N) for c, p in zip(index, parts)])
+    assert (np.abs(z - y) > tol).any()
