@@ -22,11 +22,6 @@ __device__ __forceinline__ float2 half_swap(float v) {  // (v of lanes l and l ^
 #endif
 }
 
-// LDS row of V: a multiple of 16 channels whose four rows a transposing read
-// takes lie in different banks (an odd number of 32-byte units, or a row that
-// fills a multiple of 64 but not of 128 or 256 bytes).
-__host__ __device__ constexpr int v_row(int d16) { return d16 * 2 % 128 == 0 ? d16 + 16 : d16; }
-
 // Four keys (LDS rows) of one channel for each lane of a group of 16: lane i
 // names the 8 bytes of row i / 4, channels 4 (i % 4) on, and gets channel i of rows 0 to 3.
 __device__ __forceinline__ bf16x4 read_transposed(const bf16* p) {

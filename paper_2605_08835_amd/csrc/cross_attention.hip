@@ -357,6 +357,11 @@ namespace {
 
 constexpr int KT = 64;  // keys per tile
 
+// LDS row of V: a multiple of 16 channels whose four rows a transposing read
+// takes lie in different banks (an odd number of 32-byte units, or a row that
+// fills a multiple of 64 but not of 128 or 256 bytes).
+__host__ __device__ constexpr int v_row(int d16) { return d16 * 2 % 128 == 0 ? d16 + 16 : d16; }
+
 }  // namespace
 
 // D16: head width rounded up to a width the kernel is built for.  SF: d < D16,

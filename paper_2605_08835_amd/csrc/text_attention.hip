@@ -12,8 +12,6 @@
 // same along a diagonal: a tile's 64 x 128 values are 191, kept in LDS.
 // Tiles wholly behind the causal border are passed over, and keys that a mask or
 // the text's end leaves out are never read.
-#include <type_traits>
-
 #include "attention_tile.h"
 #include "device_common.h"
 #include "kernels.h"
@@ -284,8 +282,8 @@ __global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 :
   // some of its low bits turned, so both addresses are one xor and a constant away.
   constexpr int KL = k_low(CH), VL = v_low(CH);
   const int k_at = lq * D16 + (lh ^ k_swz<CH>(lq)) * 8;
-  const int v_row = 4 * lh + ((lane & 15) >> 2);
-  const int v_at = v_row * D16 + ((((lane & 16) >> 3) + ((lane & 3) >> 1)) ^ v_swz<CH>(v_row)) * 8 + 4 * (lane & 1);
+  const int vr0 = 4 * lh + ((lane & 15) >> 2);
+  const int v_at = vr0 * D16 + ((((lane & 16) >> 3) + ((lane & 3) >> 1)) ^ v_swz<CH>(vr0)) * 8 + 4 * (lane & 1);
   auto k_frag = [&](const bf16* Kb, int kt, int j) __attribute__((always_inline)) {
     return *(const bf16x8*)(Kb + (k_at ^ ((2 * j & KL) * 8)) + (2 * j & ~KL) * 8 + kt * 32 * D16);
   };
