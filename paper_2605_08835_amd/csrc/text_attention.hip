@@ -153,16 +153,20 @@ __device__ __forceinline__ int v_swz(int r) {
 // SHORT: no text is longer than the two tiles that LDS holds.  They are loaded at
 // once and nothing waits afterwards; a block is as long as its chain of latencies,
 // so four blocks share a CU where registers allow, which leaves fewer for fragments
-// read ahead.  The sums are the same.  (48 prompts of 5 to 77 tokens, 20 heads, this
-// form and the other, us: 32 channels 8.0 and 12.4, 64 10.9 and 17.0, 128 17.3 and
-// 30.3; 64 texts of 128 tokens 23.0 and 27.3.)
+// read ahead, and three for capped scores without a term, whose exponents all live at
+// once.  The sums are the same.  (us, kernels of 20 heads, this form and the other; causal
+// prompts of 5 to 77 tokens, 48 of them: 32 channels 7.9 and 8.8, 64 9.1 and 11.8, 128 16.9
+// and 18.0, 256 48 and 57; capped 9.3 and 11.4, 12.2 and 13.1 (four blocks: 16.0), 18.6 and
+// 19.7, 68 and 84; 64 texts of 128 tokens 15.0 and 16.3, 18.1 and 19.4, 33.9 and 33.6, 102 and
+// 143; capped 18.4 and 19.1, 21.8 and 22.0 (four blocks: 33.2), 35.4 and 35.6, 143 and 199;
+// 192 channels 72.5 and 69.4, else as 128.)
 // What bounds it: a wave's vector instructions (some 9 a score without a cap, 12 with,
 // the exponentials two turns each) and its products one after the other, which only
 // other waves overlap: 6 documents of 500 to 8192 tokens, 16 heads of 128, capped 960 us,
 // 660 TFLOP/s, vector ALU busy 55 %, matrix unit 30 %; 12 texts of 700 to 2500, 10 heads
 // of 80 140 us, 450 TFLOP/s.  Waiting for every fragment where it is used took 1155 and 174.
 template <int D16, bool BIAS, bool CAP, bool SHORT>
-__global__ __launch_bounds__(256, D16 <= 64 ? (SHORT ? 4 : 3) : D16 <= 128 ? 2 : 1) void text_bf16_kernel(TextArgs a) {
+__global__ __launch_bounds__(256, D16 <= 64 ? (SHORT && (BIAS || !CAP) ? 4 : 3) : D16 <= 128 ? 2 : 1) void text_bf16_kernel(TextArgs a) {
   constexpr int NW = 4, KT = 64, NJ = D16 / 16, ND = (D16 + 31) / 32, CH = D16 / 8, NI = (CH + NW - 1) / NW, LDR = D16 + 8;
   constexpr int TILE = KT * D16;
   static_assert(NW * 32 * LDR <= 4 * TILE, "the result's rows take the place of the tiles");
