@@ -357,14 +357,17 @@ long linear_adapters_scratch_floats(DType dt, int M, int rank) {
 // 40.4; 4096 x 1280, rank 32 30.8 and 31.5).  An index per row may bring several
 // adapters to a block: 4 blocks share them out then (one, and four: 1872 x 768, rank 16,
 // in runs of 40 rows 15.9 and 13.1, in one run 12.6 and 12.5; 512 x 320, rank 32, every row
-// another 28.3 and 16.6).
+// another 28.3 and 16.6; 12288 x 320, rank 16, in runs of 40 20.0 and 17.1, every row
+// another 36.8 and 25.5, in one run 14.9 and 14.8; 32768 x 640, rank 32, in runs of 40
+// 59 and 55, in one run 43.9 and 43.7), up to 32768 rows (196608 x 320, rank 16, in runs of
+// 40 126 and 138, of 4096 112 and 116).
 template <int RT>
 static void launch_down(const LinearAdaptersArgs& a, hipStream_t s) {
   const unsigned y = (unsigned)((a.rank + 32 * RT - 1) / (32 * RT));
   if (a.M <= 8192)
     adapters_down_kernel<1, RT><<<dim3((unsigned)((a.M + 31) / 32), y, a.group < 32 ? 4 : 1), 256, 0, s>>>(a);
   else
-    adapters_down_kernel<2, RT><<<dim3((unsigned)((a.M + 63) / 64), y), 256, 0, s>>>(a);
+    adapters_down_kernel<2, RT><<<dim3((unsigned)((a.M + 63) / 64), y, a.group < 32 && a.M <= 32768 ? 4 : 1), 256, 0, s>>>(a);
 }
 
 // (What reads v is not launched where v was not.)
