@@ -286,12 +286,15 @@ sd_status synerdiff_op_cross_attention(int32_t dtype, const void* d_q, int64_t q
  * negative ones are 0).  Queries of masked tokens are computed like others.
  * Keys that take no part for any query of their text are not read, and what k
  * and v hold behind a query's causal border does not reach it, infinities and
- * NaN included.  Keys that score -inf (a bias of -inf, say) take no weight, as
- * long as their v is finite; a query without a key of any weight gives zeros.  A finite bias, lowest value of fp32 included, stays
- * finite: a query whose keys all have it weighs them alike.  Scores, sums and
- * results are fp32 until the result is rounded to dtype; bf16 probabilities
- * are rounded to bf16 (by up to 2^-8 of each) and summed as rounded, and capped bf16
- * scores are right to 2^-21 of the cap.
+ * NaN included; nor does what bias holds at the distance of a key that takes no part.
+ * Keys that score -inf (a bias of -inf, say) take no weight, as long as their v is
+ * finite; a query without a key of any weight gives zeros.  (An infinite v under a
+ * weight that fp32 does not hold may give NaN.  A scale of 0 is one for finite q and k.)
+ * A finite bias, lowest value of fp32 included, stays finite: a query whose keys all
+ * have it weighs them alike.  Scores, sums and results are fp32 until the result is
+ * rounded to dtype; sums over keys, of weights up to 2^8, come before the division, so
+ * values of v up to 2^90 are safe.  bf16 probabilities are rounded to bf16 (by up to 2^-8
+ * of each) and summed as rounded, and capped bf16 scores are right to 2^-21 of the cap.
  * Layouts (strides in elements, 0 or more; that of an axis of one element is
  * not looked at).  Packed texts (d_start not NULL, int32 [n + 1], not
  * decreasing): text c is rows start[c] .. start[c + 1] - 1 of [tokens], cut at
@@ -328,7 +331,7 @@ sd_status synerdiff_op_text_attention(int32_t dtype, const void* d_q, int64_t q_
  * on no other row and on no other adapter than its own, whatever they hold.
  * Narrower adapters are padded with zeros.  Sums are fp32; v is fp32 for fp32
  * and for up to 32 rows (64 up to K = 2048), else held to 2^-17 of it (two bf16
- * parts; below 2^-110 less).  Any order of indices is right; runs of 32 rows or
+ * parts; below 2^-110 less).  Infinities give what the formula gives.  Any order of indices is right; runs of 32 rows or
  * more of one adapter are fast.
  * Constraints: K, N, rank multiples of 8; K, N <= 2^20, rank <= 1024; w, up[c] and
  * down[c] below 2^31 bytes; M <= 2^26, M N < 2^35, M rank < 2^33; all

@@ -101,10 +101,10 @@ __global__ __launch_bounds__(256) void adapters_down_rows_kernel(LinearAdaptersA
 // the one that is multiplied; MW waves have 32 rows each, the rest share out a tile's
 // k and are summed at the end.  v's two parts go to scratch, [M, rank] each.
 // Chunk c (16 bytes) of a tile's row r lies in slot c ^ (r / 2 % 8): fragment reads of
-// 16 rows are spread over all banks.  Bound by x's bytes: 196608 x 320, rank 16 20.5 us,
-// 6.1 TB/s (partly from the cache behind the L2s); 16384 x 1280, rank 128 19 us, where every
-// 64 rows read the adapter anew.  Fragments straight from memory, 32 bytes a row at a
-// time, took 33 and 44 us.
+// 16 rows are spread over all banks.  Bound by x's bytes: 196608 x 320, rank 16 32 us, 3.9
+// TB/s on inputs that change (20.5 on the same ones, partly from the cache behind the L2s);
+// 16384 x 1280, rank 128 24 us (19), where every 64 rows read the adapter anew.  Fragments
+// straight from memory, 32 bytes a row at a time, took 33 and 44 us on the same inputs.
 template <int MW, int RT>
 __global__ __launch_bounds__(256, 2) void adapters_down_kernel(LinearAdaptersArgs a) {
   constexpr int NW = 4, KW = NW / MW, BM = 32 * MW, BR = 32 * RT, NS = 3, XI = MW, DI = RT, LPT = XI + DI, STAGE = (BM + BR) * 64;
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256, 2) void adapters_down_kernel(LinearAdaptersArg
 // ------------------------------------------------------------------ few rows
 // A block has 16 outputs of all rows (MT x 16), its 8 waves share out K 128 bytes at
 // a time and are summed in order.  OWN: it makes v itself (at most OWN_V values),
-// beside the others' loads: 1 row, bf16 1280 x 1280, rank 16 in one launch of 5.9 us
+// beside the others' loads: 1 row, bf16 1280 x 1280, rank 16 in one launch of 6.0 us
 // (10.5 a call) against two of 2.9 and 4.3 (14.4 a call).
 constexpr int OWN_V = 64;
 template <typename T, int MT, bool OWN>

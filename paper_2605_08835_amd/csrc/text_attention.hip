@@ -147,9 +147,8 @@ __device__ __forceinline__ int v_swz(int r) {
 
 // D16: head width rounded up to a width the kernel is built for.  BIAS: there is
 // a term by distance.  CAP: scores are capped.  Tiles of 64 keys go from memory
-// straight to LDS.  While a tile's probabilities are formed, the next tile's scores
-// are multiplied: the two do not depend on each other, and the matrix unit would
-// wait for the vector ALU otherwise.
+// straight to LDS, one tile ahead of the one in work; a tile's K fragments, and the first
+// half of V's, are read ahead of the products that use them.
 // SHORT: no text is longer than the two tiles that LDS holds.  They are loaded at
 // once and nothing waits afterwards; a block is as long as its chain of latencies,
 // so four blocks share a CU where registers allow, which leaves fewer for fragments
@@ -162,9 +161,14 @@ __device__ __forceinline__ int v_swz(int r) {
 // 192 channels 72.5 and 69.4, else as 128.)
 // What bounds it: a wave's vector instructions (some 9 a score without a cap, 12 with,
 // the exponentials two turns each) and its products one after the other, which only
-// other waves overlap: 6 documents of 500 to 8192 tokens, 16 heads of 128, capped 960 us,
-// 660 TFLOP/s, vector ALU busy 55 %, matrix unit 30 %; 12 texts of 700 to 2500, 10 heads
-// of 80 140 us, 450 TFLOP/s.  Waiting for every fragment where it is used took 1155 and 174.
+// other waves overlap.  30 calls after each other on inputs that change: 6 documents of
+// 500 to 8192 tokens, 16 heads of 128 on 4, capped 1331 us, 476 TFLOP/s, vector ALU busy
+// 61 %, matrix unit 34 % (the clock falls under it: 1046 us between other work); 12 texts
+// of 700 to 2500, 10 heads of 80 175 us, 359 TFLOP/s, 45 %, 26 % and a third of the time
+// waiting for the next tile.  (Waiting for every fragment where it is used cost a quarter more.)
+// Registers: one wave per SIMD past 128 channels.  At 256 every form spills 15 to 101 of
+// them, and is far off for it: 8 heads on 4 over the documents above, capped 3696 us, 171
+// TFLOP/s.  At 64 the SHORT forms with a term spill 2.  No other form does.
 template <int D16, bool BIAS, bool CAP, bool SHORT>
 __global__ __launch_bounds__(256, D16 <= 64 ? (SHORT && (BIAS || !CAP) ? 4 : 3) : D16 <= 128 ? 2 : 1) void text_bf16_kernel(TextArgs a) {
   constexpr int NW = 4, KT = 64, NJ = D16 / 16, ND = (D16 + 31) / 32, CH = D16 / 8, NI = (CH + NW - 1) / NW, LDR = D16 + 8;
@@ -587,7 +591,8 @@ __device__ __forceinline__ float tanh_f32(float x) {
 // takes 8 i + 4 lh + [0, 4)); a key's probability meets its V row straight from the
 // register it was computed in, since the two k of an MFMA are the two lane halves' keys.
 // Few texts wait for the tiles of the longest one, a wave's 32 products of 64 cycles
-// a tile at 32 channels: 6 texts of 8 to 231 tokens, 8 heads of 32, capped 25 us.
+// a tile at 32 channels: 6 texts of 8 to 231 tokens, 8 heads of 32, capped 25.8 us; one
+// text of 4000, 8 heads of 64, causal 354 us.  One wave per SIMD past 64 channels.
 template <int D32>
 __global__ __launch_bounds__(256, D32 <= 64 ? 2 : 1) void text_f32_kernel(TextArgs a) {
   constexpr int NW = 4, KT = 32, NI = D32 / 8, ND = D32 / 32, NT = 64 * NW, LDK = D32 + 4, LDV = D32 + 8;  // (rows apart by banks)
